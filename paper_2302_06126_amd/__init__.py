@@ -22,7 +22,7 @@ from ._abi import (TAG_BF16, TAG_F32, TagError, check, tag_decision, tag_feature
 __all__ = ["Graph", "Model", "tag_graph_plan", "tag_graph_build", "tag_graph_get_info", "tag_graph_export",
            "tag_graph_destroy", "tag_gnn_workspace", "tag_gnn_forward", "tag_gnn_decide_workspace",
            "tag_gnn_decide", "tag_last_error", "tag_version", "tag_profile_begin", "tag_profile_end",
-           "forward", "decide", "TagError",
+           "forward", "decide", "scores", "tag_gnn_scores", "TagError",
            "TAG_F32", "TAG_BF16"]
 
 
@@ -132,6 +132,13 @@ def tag_gnn_decide(handle, dims, weights, n_replicas, E_op, E_dev, slices, n_que
     return _abi.load().tag_gnn_decide(handle, C.byref(dims), C.byref(weights), n_replicas, E_op, E_dev,
                                       C.byref(slices), n_query, q_rep, q_graph, q_op, argmax, best, prior,
                                       decision, workspace, ws_bytes, stream)
+
+
+def tag_gnn_scores(handle, dims, weights, n_replicas, E_op, E_dev, slices, n_query, q_rep, q_graph, q_op, scores,
+                   workspace, ws_bytes, stream) -> int:
+    return _abi.load().tag_gnn_scores(handle, C.byref(dims), C.byref(weights), n_replicas, E_op, E_dev,
+                                      C.byref(slices), n_query, q_rep, q_graph, q_op, scores, workspace, ws_bytes,
+                                      stream)
 
 
 # --------------------------------------------------------- convenience ----
@@ -310,6 +317,22 @@ class Decide:
         self.best = torch.empty(Q, dtype=torch.float32, device=dev)
         self.prior = torch.empty((Q, self.S), dtype=torch.float32, device=dev) if want_prior else None
         self.decision = torch.empty((Q, C.sizeof(tag_decision)), dtype=torch.uint8, device=dev)
+        self.score = None
+
+    def scores(self, E_op, E_dev, stream=None):
+        """Raw scores [Q, S] before the softmax (-inf for an out-of-range
+        query), for ``policy.Constrain`` and ``policy.Balance``; the tensor is
+        this object's, like the outputs of a call."""
+        if self.score is None:
+            torch = _torch()
+            self.score = torch.empty((self.Q, self.S), dtype=torch.float32, device=self.graph.device)
+            if stream is not None:   # (memory of the current stream)
+                stream.wait_stream(torch.cuda.current_stream())
+        st = tag_gnn_scores(self.graph.handle, self.model.dims, self.model.weights, self.R, _ptr(E_op), _ptr(E_dev),
+                            self.slices, self.Q, _ptr(self.q[0]), _ptr(self.q[1]), _ptr(self.q[2]), _ptr(self.score),
+                            _ptr(self.ws), self.ws_bytes, _stream(stream))
+        check(st, "tag_gnn_scores")
+        return self.score
 
     def __call__(self, E_op, E_dev, stream=None):
         st = tag_gnn_decide(self.graph.handle, self.model.dims, self.model.weights, self.R, _ptr(E_op), _ptr(E_dev),
@@ -338,6 +361,13 @@ def decide(graph: Graph, model: Model, E_op, E_dev, masks, options, q_rep, q_gra
     with _OnStream(stream):
         d(E_op, E_dev, stream)
     return d.results()
+
+
+def scores(graph: Graph, model: Model, E_op, E_dev, masks, options, q_rep, q_graph, q_op, stream=None):
+    """Raw scores [Q, S] of the decision head (device tensor)."""
+    d = Decide(graph, model, int(E_op.shape[0]), masks, options, q_rep, q_graph, q_op, want_prior=False)
+    with _OnStream(stream):
+        return d.scores(E_op, E_dev, stream)
 
 
 def decide_full(graph: Graph, model: Model, E_op, E_dev, q_rep, q_graph, q_op, want_prior: bool = True,

@@ -33,6 +33,9 @@ SEARCH_EXPORTS = ("tag_search_problem_create", "tag_search_problem_destroy", "ta
                   "tag_search_run_workspace", "tag_search_run", "tag_simulate", "tag_simulate_batch",
                   "tag_search_set_model", "tag_search_link_features")
 
+# include/tag_policy.h
+EXPORTS += ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace", "tag_balance")
+
 # include/tag_train.h
 TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step")
 
@@ -92,6 +95,12 @@ class tag_grads(C.Structure):
 class tag_train_batch(C.Structure):
     _fields_ = [("n_query", C.c_int32), ("query_rep", _PF), ("query_graph", _PF), ("query_op", _PF),
                 ("target", _PF)]
+
+
+class tag_constraints(C.Structure):
+    _fields_ = [("allow", _PF), ("allow_stride", C.c_int64), ("bias", _PF), ("bias_stride", C.c_int64),
+                ("history", _PF), ("history_stride", C.c_int64), ("n_history", C.c_int32), ("history_len", _PF),
+                ("repetition", _PF), ("presence", _PF), ("frequency", _PF)]
 
 
 class tag_search_problem_desc(C.Structure):
@@ -205,6 +214,18 @@ def load() -> C.CDLL:
     lib.tag_gnn_decide_noalloc.argtypes = [vp, C.POINTER(tag_model_dims), C.POINTER(tag_weights), S, vp, vp,
                                            C.POINTER(tag_slices), S, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.tag_gnn_decide_noalloc.restype = S
+    # include/tag_policy.h
+    lib.tag_gnn_scores.argtypes = [vp, C.POINTER(tag_model_dims), C.POINTER(tag_weights), S, vp, vp,
+                                   C.POINTER(tag_slices), S, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.tag_constrain_workspace.argtypes = [S, S, szp]
+    lib.tag_constrain.argtypes = [S, S, S, vp, C.c_int64, C.POINTER(tag_constraints), vp, C.c_int64, vp, C.c_int64,
+                                  vp, vp, vp, C.c_size_t, vp]
+    lib.tag_balance_workspace.argtypes = [S, S, szp]
+    lib.tag_balance.argtypes = [S, S, S, vp, C.c_int64, vp, S, vp, C.c_float, vp, C.c_int64, S, vp, vp, vp, vp,
+                                C.c_size_t, vp]
+    for name in ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace",
+                 "tag_balance"):
+        getattr(lib, name).restype = S
     for name in SEARCH_EXPORTS:
         if name not in ("tag_search_problem_destroy", "tag_mcts_destroy"):
             getattr(lib, name).restype = S

@@ -16,6 +16,7 @@
 #include <string>
 
 #include "gemm_small.hpp"
+#include "../../include/tag_policy.h"
 #include "tag_internal.hpp"
 
 namespace tag {
@@ -38,6 +39,7 @@ struct DecArgs {
     float *best, *prior;
     tag_decision *dec;
     int32_t bound;       // dec_slice leaves a bound of |u[rg][h][a]| over a in t's row of rg's first device
+    int32_t raw;         // the raw scores alone, in prior: no softmax, argmax or decision (tag_gnn_scores)
 };
 
 // u[rg][h][a] = sum_{j in mask_a} t[dev(rg, j)][h] + P[h][2F + opt_a] (+ b1[h])
@@ -213,6 +215,7 @@ __device__ __forceinline__ void write_decision(const DecArgs &A, int32_t q, int3
 // q whose raw scores are already in A.prior (when it is given).
 __device__ __forceinline__ void finish_query(const DecArgs &A, int32_t q, int32_t g, float m, int32_t im, float z,
                                              float *red_m, int32_t *red_i, float *red_z) {
+    if (A.raw) return;
     red_m[threadIdx.x] = m; red_i[threadIdx.x] = im; red_z[threadIdx.x] = z;
     __syncthreads();
     for (int off = kScoreThreads / 2; off > 0; off >>= 1) {
@@ -241,13 +244,14 @@ __device__ __forceinline__ void finish_query(const DecArgs &A, int32_t q, int32_
 }
 
 __device__ __forceinline__ void invalid_query(const DecArgs &A, int32_t q) {
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && !A.raw) {
         A.argmax[q] = -1;
         A.best[q] = __builtin_nanf("");
         if (A.dec) A.dec[q] = tag_decision{0, 0, 0, 0, 0};
     }
     if (A.prior)
-        for (int32_t a = threadIdx.x; a < A.S; a += blockDim.x) A.prior[(int64_t)q * A.S + a] = 0.f;
+        for (int32_t a = threadIdx.x; a < A.S; a += blockDim.x)
+            A.prior[(int64_t)q * A.S + a] = A.raw ? -INFINITY : 0.f;
 }
 
 // one query by 256 threads (vq: Hx floats)
@@ -501,6 +505,10 @@ __global__ void __launch_bounds__(kScoreThreads) dec_score_group(DecArgs A) {
     for (int i = threadIdx.x >> 6; i < nq; i += kScoreThreads / 64) {
         if ((done >> i) & 1u) continue;
         const int32_t q = q0 + i;
+        if (A.raw) {
+            for (int32_t a = lane; a < S; a += 64) A.prior[(int64_t)q * S + a] = ss[i * S + a];
+            continue;
+        }
         float m = -INFINITY;
         int32_t im = INT32_MAX;
         for (int32_t a = lane; a < S; a += 64)
@@ -582,7 +590,7 @@ tag_status decide_run(const tag_graph *g, const tag_model_dims *dims, const tag_
                       const float *E_op, const float *E_dev, const tag_slices *slices, int32_t n_query,
                       const int32_t *query_rep, const int32_t *query_graph, const int32_t *query_op,
                       int32_t *argmax, float *best_score, float *prior, tag_decision *decision, void *workspace,
-                      size_t ws_bytes, void *hip_stream, const char *ws_what) {
+                      size_t ws_bytes, void *hip_stream, const char *ws_what, bool raw = false) {
     if (!g || !dims || !w || !E_op || !E_dev || !slices) TAG_FAIL(TAG_EINVAL, "NULL argument");
     if (dims->f != 64 && dims->f != 128 && dims->f != 256) TAG_FAIL(TAG_ESHAPE, "f must be 64, 128 or 256");
     if (dims->dec_hidden < 0 || dims->dec_hidden > 1024) TAG_FAIL(TAG_ESHAPE, "dec_hidden must be in [0, 1024]");
@@ -590,8 +598,9 @@ tag_status decide_run(const tag_graph *g, const tag_model_dims *dims, const tag_
     if (slices->n_slices < 1 || !slices->mask || !slices->option) TAG_FAIL(TAG_EINVAL, "empty or NULL slice table");
     if (n_query < 0) TAG_FAIL(TAG_EINVAL, "n_query must be >= 0");
     if (n_query == 0) return TAG_OK;
-    if (!query_rep || !query_graph || !query_op || !argmax || !best_score)
-        TAG_FAIL(TAG_EINVAL, "query arrays, argmax and best_score must be non-NULL");
+    if (!query_rep || !query_graph || !query_op || (raw ? !prior : !argmax || !best_score))
+        TAG_FAIL(TAG_EINVAL, raw ? "query arrays and scores must be non-NULL"
+                                 : "query arrays, argmax and best_score must be non-NULL");
     if (!w->dec_w2 || !w->dec_b2 || (dims->dec_hidden > 0 && (!w->dec_w1 || !w->dec_b1)))
         TAG_FAIL(TAG_EINVAL, "decoder weights must be non-NULL");
     if (!workspace) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL");
@@ -614,6 +623,7 @@ tag_status decide_run(const tag_graph *g, const tag_model_dims *dims, const tag_
     A.q_rep = query_rep; A.q_graph = query_graph; A.q_op = query_op;
     A.t = L.t; A.u = L.u; A.v = L.v;
     A.argmax = argmax; A.best = best_score; A.prior = prior; A.dec = decision;
+    A.raw = raw;
     // (one query per candidate, as a search asks, has nothing to share: 8,192 of them, H = 64, 320 us with four
     // queries per block, 328 in groups)
     const bool group = A.Q >= kGroupMinQ && A.Q >= 2 * (int64_t)A.R && H > 0 && H <= kGroupMaxH && A.S <= kGroupMaxS;
@@ -631,7 +641,7 @@ tag_status decide_run(const tag_graph *g, const tag_model_dims *dims, const tag_
     else
         dec_score<1><<<(unsigned)A.Q, kScoreThreads, sizeof(float) * (Hx + H), stream>>>(A);
     prof_end(TAG_STAGE_DECIDE, stream);
-    return launch_status("tag_gnn_decide");
+    return launch_status(raw ? "tag_gnn_scores" : "tag_gnn_decide");
 }
 
 // Static scratch of the allocation-free entry point: one copy per GPU the
@@ -674,6 +684,17 @@ extern "C" tag_status tag_gnn_decide(const tag_graph *g, const tag_model_dims *d
     return decide_run(g, dims, w, n_replicas, E_op, E_dev, slices, n_query, query_rep, query_graph, query_op,
                       argmax, best_score, prior, decision, workspace, ws_bytes, hip_stream,
                       "decide workspace too small (see tag_gnn_decide_workspace)");
+}
+
+extern "C" tag_status tag_gnn_scores(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w,
+                                     int32_t n_replicas, const float *E_op, const float *E_dev,
+                                     const tag_slices *slices, int32_t n_query, const int32_t *query_rep,
+                                     const int32_t *query_graph, const int32_t *query_op, float *scores,
+                                     void *workspace, size_t ws_bytes, void *hip_stream) {
+    clear_error();
+    return decide_run(g, dims, w, n_replicas, E_op, E_dev, slices, n_query, query_rep, query_graph, query_op,
+                      nullptr, nullptr, scores, nullptr, workspace, ws_bytes, hip_stream,
+                      "decide workspace too small (see tag_gnn_decide_workspace)", true);
 }
 
 extern "C" size_t tag_gnn_decide_noalloc_max_bytes(void) { return kDecideScratchBytes; }
