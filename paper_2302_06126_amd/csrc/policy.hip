@@ -40,10 +40,10 @@ __device__ __forceinline__ float penalised(float y, int32_t taken, float rep, fl
 
 // One row by NT threads, VPT columns each (kWhole), or one part of a row of
 // NT * VPT columns: its maximum and sum (kPart), and in a second launch its
-// outputs, from all of the row's records (kFinish).  The history's counts of
-// the row's (part's) columns are LDS counters that its threads fill, so its
-// length is not bounded; y is formed in the order that the header gives, each
-// operation rounded.
+// outputs, from all of the row's records (kFinish).  Every load that does not
+// wait for another is issued first.  The history's counts of the row's (part's)
+// columns are LDS counters that its threads fill, so its length is not bounded;
+// y is formed in the order that the header gives, each operation rounded.
 template <typename T, int NT, int VPT, bool VEC, int PASS>
 __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
 #pragma clang fp contract(off)   // (the same bits from the forms for aligned and for other rows)
@@ -60,25 +60,38 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
     const tag_constraints &C = A.c;
     int32_t *cnt = counts + Team::row() * W;
     const T *xr = static_cast<const T *>(A.x) + q * A.xs;
-    float y[VPT];
+    float y[VPT], b[VPT];
+    uint32_t ok[NV];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         load4<T, VEC>(xr, c0 + 4 * (tid + NT * k), A.S, -INFINITY, *reinterpret_cast<float(*)[4]>(y + 4 * k));
+    if (C.bias) {
+        const float *br = C.bias + q * C.bias_stride;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            load4<float, VEC>(br, c0 + 4 * (tid + NT * k), A.S, 0.f, *reinterpret_cast<float(*)[4]>(b + 4 * k));
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const int64_t c = c0 + 4 * (tid + NT * k);
+        ok[k] = c < A.S ? (C.allow ? C.allow[q * C.allow_stride + (c >> 5)] >> (c & 31) : 15u) : 0u;
+        if (c + 4 > A.S && c < A.S) ok[k] &= (1u << (A.S - c)) - 1u;   // (columns past the end)
+    }
     if (C.history) {
+        int32_t n = C.n_history;
+        if (C.history_len) n = min(n, max(C.history_len[q], 0));
+        const float rep = C.repetition ? C.repetition[q] : 1.f, pre = C.presence ? C.presence[q] : 0.f,
+                    frq = C.frequency ? C.frequency[q] : 0.f;
+        const int32_t *h = C.history + q * C.history_stride;
+        const uint32_t span = (uint32_t)min((int64_t)W, A.S - c0);
 #pragma unroll
         for (int k = 0; k < NV; ++k) *reinterpret_cast<int4 *>(cnt + 4 * (tid + NT * k)) = int4{0, 0, 0, 0};
         Team::sync();
-        int32_t n = C.n_history;
-        if (C.history_len) n = min(n, max(C.history_len[q], 0));
-        const int32_t *h = C.history + q * C.history_stride;
-        const uint32_t span = (uint32_t)min((int64_t)W, A.S - c0);
         for (int32_t t = tid; t < n; t += NT) {
             const int64_t a = (int64_t)h[t] - c0;
             if (a >= 0 && a < span) atomicAdd(cnt + a, 1);
         }
         Team::sync();
-        const float rep = C.repetition ? C.repetition[q] : 1.f, pre = C.presence ? C.presence[q] : 0.f,
-                    frq = C.frequency ? C.frequency[q] : 0.f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int4 n4 = *reinterpret_cast<const int4 *>(cnt + 4 * (tid + NT * k));
@@ -90,86 +103,69 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
         }
     }
     if (C.bias) {
-        const float *br = C.bias + q * C.bias_stride;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float b[4];
-            load4<float, VEC>(br, c0 + 4 * (tid + NT * k), A.S, 0.f, b);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[4 * k + i] += b[i];
-        }
+        for (int k = 0; k < VPT; ++k) y[k] += b[k];
     }
-    if (C.allow) {
-        const uint32_t *ar = C.allow + q * C.allow_stride;
+    RowMax mx{-INFINITY, INT32_MAX};
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int64_t c = c0 + 4 * (tid + NT * k);
-            const uint32_t bits = c < A.S ? ar[c >> 5] >> (c & 31) : 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (!((bits >> i) & 1u)) y[4 * k + i] = -INFINITY;
-        }
+    for (int k = 0; k < VPT; ++k) {
+        if (!((ok[k / 4] >> (k % 4)) & 1u)) y[k] = -INFINITY;
+        if (PASS != kFinish && y[k] > mx.m) mx = RowMax{y[k], (int32_t)c0 + 4 * (tid + NT * (k / 4)) + k % 4};
     }
-    RowMax mx{-INFINITY, INT32_MAX, 0};
     float z = 0.f;
     if (PASS != kFinish) {
 #pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-            const int32_t c = (int32_t)c0 + 4 * (tid + NT * (k / 4)) + k % 4;
-            const bool in = c < A.S;   // (columns past the end hold -inf or a NaN of inf - inf)
-            if (in && y[k] > mx.m) { mx.m = y[k]; mx.at = c; }
-            if (in && y[k] != y[k]) mx.nan = 1;
-        }
-        mx = Team::reduce(mx, RowMax::join);
+        for (int k = 0; k < VPT; ++k)
+            if (y[k] != y[k]) mx.at = -2;
+        mx = Team::max(mx);
     } else {
         // the row's records, joined in the same order by every part
-        float m = -INFINITY;
         const float *rec = A.rec + q * A.chunks * 4;
         for (int32_t i = tid; i < A.chunks; i += NT) {
             const float4 r = *reinterpret_cast<const float4 *>(rec + 4 * (int64_t)i);
-            mx = RowMax::join(mx, RowMax{r.x, __float_as_int(r.z), __float_as_int(r.w)});
+            const int32_t at = __float_as_int(r.z);
+            const bool nan = mx.at == -2 || at == -2;
+            if (r.x > mx.m) mx = RowMax{r.x, at};   // (a thread's records go up in columns)
+            if (nan) mx.at = -2;
         }
-        mx = Team::reduce(mx, RowMax::join);
-        m = mx.m;
+        mx = Team::max(mx);
         for (int32_t i = tid; i < A.chunks; i += NT) {
             const float4 r = *reinterpret_cast<const float4 *>(rec + 4 * (int64_t)i);
-            if (r.x > -INFINITY) z = fmaf(r.y, exp_neg(r.x - m), z);
+            if (r.x > -INFINITY) z = fmaf(r.y, exp_neg(r.x - mx.m), z);
         }
-        z = Team::reduce(RowSum{z}, RowSum::join).s;
     }
-    const bool none = !(mx.m > -INFINITY);
-#pragma unroll
-    for (int k = 0; k < VPT && PASS != kFinish; ++k) {
-        const int32_t c = (int32_t)c0 + 4 * (tid + NT * (k / 4)) + k % 4;
-        if (c < A.S && !none) z += exp_neg(y[k] - mx.m);
-    }
-    if (PASS != kFinish) z = Team::reduce(RowSum{z}, RowSum::join).s;
-    if (!live) return;   // (after the last barrier)
-    if (PASS == kPart) {
-        if (tid == 0)
-            *reinterpret_cast<float4 *>(A.rec + item * 4) = float4{mx.m, z, __int_as_float(mx.at), __int_as_float(mx.nan)};
-        return;
-    }
-    if (A.out) {
+    const bool none = !(mx.m > -INFINITY), nan = mx.at == -2;
+    if (PASS != kPart && A.out && live) {
         T *o = static_cast<T *>(A.out) + q * A.os;
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             store4<T, VEC>(o, c0 + 4 * (tid + NT * k), A.S, *reinterpret_cast<float(*)[4]>(y + 4 * k));
     }
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+        y[k] = none ? 0.f : exp_neg(y[k] - mx.m);
+        if (PASS != kFinish) z += y[k];
+    }
+    z = Team::sum(z);
+    if (!live) return;   // (after the last barrier)
+    if (PASS == kPart) {
+        if (tid == 0) *reinterpret_cast<float4 *>(A.rec + item * 4) = float4{mx.m, z, __int_as_float(mx.at), 0.f};
+        return;
+    }
     if (A.prior) {
-        const float inv = mx.nan ? __builtin_nanf("") : none ? 0.f : 1.f / z;
+        const float inv = nan ? __builtin_nanf("") : none ? 0.f : 1.f / z;
         float *p = A.prior + q * A.ps;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (none ? 1.f : exp_neg(y[4 * k + i] - mx.m)) * inv;
+            for (int i = 0; i < 4; ++i) v[i] = y[4 * k + i] * inv;
             store4<float, VEC>(p, c0 + 4 * (tid + NT * k), A.S, v);
         }
     }
     if (part == 0 && tid == 0) {
-        A.argmax[q] = mx.nan || none ? -1 : mx.at;
-        A.best[q] = mx.nan ? __builtin_nanf("") : mx.m;
+        A.argmax[q] = nan || none ? -1 : mx.at;
+        A.best[q] = nan ? __builtin_nanf("") : mx.m;
     }
 }
 
@@ -188,7 +184,7 @@ void launch_con_pass(const ConArgs &A, bool vec, int64_t items, hipStream_t st) 
 template <typename T>
 void launch_constrain(const ConArgs &A, bool vec, hipStream_t st) {
     if (A.S <= 64) launch_con_pass<T, 16, 4, kWhole>(A, vec, A.Q, st);
-    else if (A.S <= 256) launch_con_pass<T, 64, 4, kWhole>(A, vec, A.Q, st);
+    else if (A.S <= 256) launch_con_pass<T, 16, 16, kWhole>(A, vec, A.Q, st);
     else if (A.S <= 1024) launch_con_pass<T, 64, 16, kWhole>(A, vec, A.Q, st);
     else if (A.S <= 4096) launch_con_pass<T, 256, 16, kWhole>(A, vec, A.Q, st);
     else if (A.S <= kConWhole) launch_con_pass<T, 512, 16, kWhole>(A, vec, A.Q, st);
@@ -291,8 +287,9 @@ namespace {
 
 // -------------------------------------------------------------------- balance
 constexpr int kBalMaxS = 16384;
-constexpr int kBalBlocks = 2048;   // blocks that walk the rows
-constexpr int kBalSpan = 256;      // slices per counting block
+constexpr int kBalParts = 256;      // blocks that count decisions
+constexpr int kBalGrad = 4096;      // blocks that walk the rows for their gradients, at most
+constexpr int kBalSpan = 64;        // slices per merging block
 
 struct BalArgs {
     int32_t Q, S, M;
@@ -309,140 +306,135 @@ struct BalArgs {
     float *load;
     // workspace
     int32_t *arg;        // [Q] argmax; -1: not used, -2: used with a NaN
-    double *part;        // [counting blocks][64] their slices' part of n load
-    double *total;       // load [64], centre, n
-    double *lpart;       // [kBalBlocks] sums over rows of sum_a p_a (h_a - centre)
-    int32_t *done;       // [2] blocks that are through
+    int32_t *hist;       // [parts][S] counts of one block's rows
+    int32_t *used;       // [parts] its used rows
+    double *part;        // [merging blocks][64] their slices' part of n load
+    double *total;       // centre of h, n
+    float *h;            // [S] less the centre
+    double *lpart;       // [grad blocks] sums over rows of sum_a p_a h_a
+    int32_t parts, lparts;
 };
 
 __device__ __forceinline__ uint64_t device_bits(int32_t M) { return M >= 64 ? ~0ull : (1ull << M) - 1ull; }
 
-// Each used row's argmax.
+// Each used row's argmax, and how often the block's rows chose each slice.
 template <typename T, int NT, int VPT, bool VEC>
-__global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_argmax(BalArgs A) {
-    using Team = RowTeam<NT>;
+__global__ void __launch_bounds__(1024) bal_argmax(BalArgs A) {
+    using Team = RowTeam<NT, 1024>;
+    extern __shared__ int32_t hist[];   // [S], then the used rows
+    for (int i = threadIdx.x; i <= A.S; i += 1024) hist[i] = 0;
+    __syncthreads();
     const int tid = Team::tid();
-    if (blockIdx.x == 0 && threadIdx.x < 2) A.done[threadIdx.x] = 0;
+    // (every thread of the block takes every turn: teams of several wavefronts meet in barriers)
     for (int64_t base = (int64_t)blockIdx.x * Team::kRows; base < A.Q; base += (int64_t)gridDim.x * Team::kRows) {
         const int64_t q0 = base + Team::row(), q = q0 < A.Q ? q0 : A.Q - 1;
         const bool use = !A.use || A.use[q] != 0;
         const T *xr = static_cast<const T *>(A.x) + q * A.xs;
-        RowMax mx{-INFINITY, INT32_MAX, 0};
+        RowMax mx{-INFINITY, INT32_MAX};
         if (use) {
+            float v[VPT];
+            bool nan = false;
 #pragma unroll
-            for (int k = 0; k < VPT / 4; ++k) {
-                const int32_t c = 4 * (tid + NT * k);
-                float v[4];
-                load4<T, VEC>(xr, c, A.S, -INFINITY, v);
+            for (int k = 0; k < VPT / 4; ++k)
+                load4<T, VEC>(xr, 4 * (tid + NT * k), A.S, -INFINITY, *reinterpret_cast<float(*)[4]>(v + 4 * k));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (v[i] > mx.m) { mx.m = v[i]; mx.at = c + i; }
-                    if (v[i] != v[i]) mx.nan = 1;
-                }
+            for (int k = 0; k < VPT; ++k) {
+                if (v[k] > mx.m) mx = RowMax{v[k], 4 * (tid + NT * (k / 4)) + k % 4};
+                nan = nan || v[k] != v[k];
             }
+            if (nan) mx.at = -2;
         }
-        mx = Team::reduce(mx, RowMax::join);
-        if (tid == 0 && q0 < A.Q) A.arg[q] = mx.nan ? -2 : (mx.m > -INFINITY ? mx.at : -1);
+        mx = Team::max(mx);
+        if (tid == 0 && q0 < A.Q) {
+            const int32_t at = mx.at == INT32_MAX ? -1 : mx.at;
+            A.arg[q] = at;
+            if (at >= 0) atomicAdd(hist + at, 1);
+            if (at != -1) atomicAdd(hist + A.S, 1);
+        }
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < A.S; i += 1024) A.hist[(int64_t)blockIdx.x * A.S + i] = hist[i];
+    if (threadIdx.x == 0) A.used[blockIdx.x] = hist[A.S];
 }
 
-// the last block to get here (every thread of it): it sees what the others wrote before
-__device__ __forceinline__ bool last_block(int32_t *done) {
-    __shared__ int32_t mine;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) mine = atomicAdd(done, 1);
-    __syncthreads();
-    const bool last = mine == (int32_t)gridDim.x - 1;
-    if (last) __threadfence();
-    return last;
-}
-
-// Counts of kBalSpan slices per block over all rows' argmaxes (LDS counters; a
-// wavefront first joins its lanes that agree with one of them, twice, since the
-// decisions of a batch crowd on few slices), and their part of the loads; the
-// last block through adds those up in block order.
+// Counts of kBalSpan slices per block over the parts, and their part of the loads.
 __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
-    __shared__ int32_t cnt[kBalSpan], used;
-    const int t = threadIdx.x, lane = t & 63;
-    const int32_t s0 = blockIdx.x * kBalSpan;
-    if (t < kBalSpan) cnt[t] = 0;
-    if (t == 0) used = 0;
-    __syncthreads();
+    __shared__ int32_t sub[16][kBalSpan], cnt[kBalSpan];
+    __shared__ uint64_t mask[kBalSpan];
+    const int t = threadIdx.x, c = t & 63, g = t >> 6, s = blockIdx.x * kBalSpan + c;
     int32_t n = 0;
-    for (int64_t base = 0; base < A.Q; base += 1024) {
-        int32_t a = base + t < A.Q ? A.arg[base + t] : -1;
-        n += a != -1;
-        a -= s0;
-        bool want = a >= 0 && a < kBalSpan;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const uint64_t some = __ballot(want);
-            if (!some) break;
-            const int first = __ffsll((unsigned long long)some) - 1;
-            const bool same = want && a == __shfl(a, first, 64);
-            const uint64_t who = __ballot(same);
-            if (lane == first) atomicAdd(cnt + a, __popcll(who));
-            want = want && !same;
-        }
-        if (want) atomicAdd(cnt + a, 1);
-    }
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-    if (lane == 0) atomicAdd(&used, n);
+    if (s < A.S)
+        for (int p = g; p < A.parts; p += 16) n += A.hist[(int64_t)p * A.S + s];
+    sub[g][c] = n;
+    if (g == 0) mask[c] = s < A.S ? A.mask[s] & device_bits(A.M) : 0;
     __syncthreads();
-    if (t < kBalSpan && s0 + t < A.S) A.count[s0 + t] = cnt[t];
-    // 16 threads per device
-    const int d = t >> 4;
-    const uint64_t valid = device_bits(A.M);
-    double w = 0.0;
-    for (int i = t & 15; i < kBalSpan && s0 + i < A.S; i += 16) {
-        const uint64_t m = A.mask[s0 + i] & valid;
-        if ((m >> d) & 1ull) w += (double)cnt[i] / (double)__popcll(m);
+    if (g == 0) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) n += sub[i][c];
+        cnt[c] = n;
+        if (s < A.S) A.count[s] = n;
     }
-    for (int o = 8; o > 0; o >>= 1) w += __shfl_xor(w, o, 16);
-    if ((t & 15) == 0) A.part[(int64_t)blockIdx.x * 64 + d] = w;
-    if (!last_block(A.done)) return;
+    __syncthreads();
+    if (t < 64) {   // device t
+        double w = 0.0;
+        for (int i = 0; i < kBalSpan; ++i)
+            if ((mask[i] >> t) & 1ull) w += (double)cnt[i] / (double)__popcll(mask[i]);
+        A.part[(int64_t)blockIdx.x * 64 + t] = w;
+    }
+}
+
+// Loads from the merging blocks' parts (in their order), then h of every slice.
+__global__ void __launch_bounds__(1024) bal_shares(BalArgs A) {
+    __shared__ double load[64], sub[16][64], centre;
+    __shared__ int32_t used;
+    const int t = threadIdx.x, d = t & 63, g = t >> 6, nb = (A.S + kBalSpan - 1) / kBalSpan;
+    if (t == 0) used = 0;
+    double s = 0.0;
+    for (int b = g; b < nb; b += 16) s += A.part[(int64_t)b * 64 + d];
+    sub[g][d] = s;
+    __syncthreads();
+    if (t < A.parts) atomicAdd(&used, A.used[t]);
+    __syncthreads();
     if (t < 64) {
-        double s = 0.0;
-        for (int b = 0; b < (int)gridDim.x; ++b)
-            s += __hip_atomic_load(A.part + (int64_t)b * 64 + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += sub[i][t];
         s = used > 0 ? s / (double)used : 0.0;
+        load[t] = s;
         if (t < A.M) A.load[t] = (float)s;
-        A.total[t] = s;
-        // centre of h: its mean over the decisions taken (softmax gradients do not see a shift of h, and
+        // centre of h: its mean over the decisions taken (the softmax's gradient does not see a shift of h, and
         // what is left of h rounds less)
         double c = s * s;
         for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
-        if (t == 0) { A.total[64] = c; A.total[65] = (double)used; }
+        if (t == 0) { centre = c; A.total[0] = c; A.total[1] = (double)used; }
+    }
+    __syncthreads();
+    const uint64_t valid = device_bits(A.M);
+    for (int i = t; i < A.S; i += 1024) {
+        uint64_t m = A.mask[i] & valid;
+        const double pop = (double)__popcll(m);
+        double w = 0.0;
+        while (m) {
+            w += load[__ffsll((unsigned long long)m) - 1];
+            m &= m - 1;
+        }
+        A.h[i] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
     }
 }
 
-// Gradient rows and the loss: each thread keeps h of its columns for every row
-// that its block walks.
+// Gradient rows, and the block's sum of the rows' losses: each thread keeps h of
+// its columns for every row that its block walks.
 template <typename T, int NT, int VPT, bool VEC>
 __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
 #pragma clang fp contract(off)   // (the same bits from the forms for aligned and for other rows)
     using Team = RowTeam<NT>;
-    __shared__ double load[66], lred[RowTeam<NT>::kBlock];
+    __shared__ double lrow[RowTeam<NT>::kRows];
     const int tid = Team::tid();
-    for (int i = threadIdx.x; i < 66; i += Team::kBlock) load[i] = A.total[i];
-    __syncthreads();
-    const double n = load[65], centre = load[64];
+    const double n = A.total[1];
     const float scale = n > 0.0 ? (float)((double)A.coef * A.M / n) : 0.f;
-    const uint64_t valid = device_bits(A.M);
     float h[VPT];
 #pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-        const int32_t c = 4 * (tid + NT * (k / 4)) + k % 4;
-        uint64_t m = c < A.S ? A.mask[c] & valid : 0;
-        const double pop = (double)__popcll(m);
-        double s = 0.0;
-        while (m) {
-            s += load[__ffsll((unsigned long long)m) - 1];
-            m &= m - 1;
-        }
-        h[k] = (float)((pop > 0.0 ? s / pop : 0.0) - centre);
-    }
+    for (int k = 0; k < VPT / 4; ++k)
+        load4<float, true>(A.h, 4 * (tid + NT * k), A.S, 0.f, *reinterpret_cast<float(*)[4]>(h + 4 * k));
     double lsum = 0.0;
     for (int64_t base = (int64_t)blockIdx.x * Team::kRows; base < A.Q; base += (int64_t)gridDim.x * Team::kRows) {
         const int64_t q0 = base + Team::row(), q = q0 < A.Q ? q0 : A.Q - 1;
@@ -451,26 +443,25 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
         const T *xr = static_cast<const T *>(A.x) + q * A.xs;
         T *gr = static_cast<T *>(A.grad) + q * A.gs;
         float x[VPT];
-        float m = -INFINITY;
+        RowMax mx{-INFINITY, 0};
         if (arg != -1) {
 #pragma unroll
-            for (int k = 0; k < VPT / 4; ++k) {
+            for (int k = 0; k < VPT / 4; ++k)
                 load4<T, VEC>(xr, 4 * (tid + NT * k), A.S, -INFINITY, *reinterpret_cast<float(*)[4]>(x + 4 * k));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) m = x[4 * k + i] > m ? x[4 * k + i] : m;
-            }
+            for (int k = 0; k < VPT; ++k) mx.m = x[k] > mx.m ? x[k] : mx.m;
         }
-        m = Team::reduce(RowMax{m, 0, 0}, RowMax::join).m;
-        float z = 0.f, e = 0.f;
+        const float m = Team::max(mx).m;
+        Two r{0.f, 0.f};
         if (arg != -1) {
 #pragma unroll
             for (int k = 0; k < VPT; ++k) {
                 x[k] = exp_neg(x[k] - m);
-                z += x[k];
-                e = fmaf(x[k], h[k], e);
+                r.s += x[k];
+                r.t = fmaf(x[k], h[k], r.t);
             }
         }
-        const RowSum2 r = Team::reduce(RowSum2{z, e}, RowSum2::join);
+        r = Team::sum(r);
         if (!live) continue;
         if (arg == -1) {
             if (!A.accumulate) {
@@ -481,7 +472,7 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
             continue;
         }
         const float inv = 1.f / r.s, mean = r.t * inv, f = scale * inv;
-        if (tid == 0) lsum += (double)mean;
+        lsum += (double)mean;
 #pragma unroll
         for (int k = 0; k < VPT / 4; ++k) {
             float v[4];
@@ -494,43 +485,48 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
             store4<T, VEC>(gr, 4 * (tid + NT * k), A.S, v);
         }
     }
-    // the block's sum, then (the last block) all of them, in a fixed order
-    lred[threadIdx.x] = lsum;
+    if (tid == 0) lrow[Team::row()] = lsum;
     __syncthreads();
     if (threadIdx.x == 0) {
         double s = 0.0;
-        for (int r = 0; r < Team::kRows; ++r) s += lred[r * NT];
+        for (int r = 0; r < Team::kRows; ++r) s += lrow[r];
         A.lpart[blockIdx.x] = s;
     }
-    if (!last_block(A.done + 1)) return;
+}
+
+// the blocks' sums, in a fixed order (a launch of its own: a fence in every
+// gradient block, for the last one to add them up, took five times the kernel)
+__global__ void __launch_bounds__(256) bal_loss(BalArgs A) {
+    __shared__ double red[4];
     double s = 0.0;
-    for (int b = threadIdx.x; b < (int)gridDim.x; b += Team::kBlock)
-        s += __hip_atomic_load(A.lpart + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    lred[threadIdx.x] = s;
+    for (int b = threadIdx.x; b < A.lparts; b += 256) s += A.lpart[b];
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    for (int o = Team::kBlock / 2; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) lred[threadIdx.x] += lred[threadIdx.x + o];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) A.loss[0] = n > 0.0 ? (float)((double)A.coef * A.M * (lred[0] / n + centre)) : 0.f;
+    const double n = A.total[1];
+    if (threadIdx.x == 0)
+        A.loss[0] = n > 0.0 ? (float)((double)A.coef * A.M * ((red[0] + red[1] + red[2] + red[3]) / n + A.total[0])) : 0.f;
 }
 
 template <typename T, int NT, int VPT>
 void launch_bal(const BalArgs &A, bool vec, hipStream_t st) {
-    using Team = RowTeam<NT>;
-    const unsigned grid = (unsigned)std::min<int64_t>(kBalBlocks, (A.Q + Team::kRows - 1) / Team::kRows);
-    const unsigned cgrid = (unsigned)((A.S + kBalSpan - 1) / kBalSpan);
-    if (vec) bal_argmax<T, NT, VPT, true><<<grid, Team::kBlock, 0, st>>>(A);
-    else bal_argmax<T, NT, VPT, false><<<grid, Team::kBlock, 0, st>>>(A);
-    bal_count<<<cgrid, 1024, 0, st>>>(A);
-    if (vec) bal_grad<T, NT, VPT, true><<<grid, Team::kBlock, 0, st>>>(A);
-    else bal_grad<T, NT, VPT, false><<<grid, Team::kBlock, 0, st>>>(A);
+    const size_t lds = sizeof(int32_t) * (A.S + 1);
+    if (vec) bal_argmax<T, NT, VPT, true><<<A.parts, 1024, lds, st>>>(A);
+    else bal_argmax<T, NT, VPT, false><<<A.parts, 1024, lds, st>>>(A);
+    bal_count<<<(A.S + kBalSpan - 1) / kBalSpan, 1024, 0, st>>>(A);
+    bal_shares<<<1, 1024, 0, st>>>(A);
+    if (vec) bal_grad<T, NT, VPT, true><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
+    else bal_grad<T, NT, VPT, false><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
+    bal_loss<<<1, 256, 0, st>>>(A);
 }
+
+// threads per row
+int bal_team(int32_t S) { return S <= 256 ? 16 : S <= 1024 ? 64 : S <= 4096 ? 256 : 1024; }
 
 template <typename T>
 void launch_balance(const BalArgs &A, bool vec, hipStream_t st) {
     if (A.S <= 64) launch_bal<T, 16, 4>(A, vec, st);
-    else if (A.S <= 256) launch_bal<T, 64, 4>(A, vec, st);
+    else if (A.S <= 256) launch_bal<T, 16, 16>(A, vec, st);
     else if (A.S <= 1024) launch_bal<T, 64, 16>(A, vec, st);
     else if (A.S <= 4096) launch_bal<T, 256, 16>(A, vec, st);
     else launch_bal<T, 1024, 16>(A, vec, st);
@@ -538,11 +534,16 @@ void launch_balance(const BalArgs &A, bool vec, hipStream_t st) {
 
 size_t carve_bal(int32_t Q, int32_t S, void *base, BalArgs *A) {
     Carver c(base);
-    A->done = c.take<int32_t>(2);
-    A->total = c.take<double>(66);
+    const int64_t team = bal_team(S), rows = 1024 / team, grad_rows = team < 256 ? 256 / team : 1;
+    A->parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kBalParts, (Q + rows - 1) / rows));
+    A->lparts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kBalGrad, (Q + grad_rows - 1) / grad_rows));
+    A->total = c.take<double>(2);
     A->part = c.take<double>((size_t)((S + kBalSpan - 1) / kBalSpan) * 64);
-    A->lpart = c.take<double>(kBalBlocks);
+    A->lpart = c.take<double>(A->lparts);
+    A->h = c.take<float>(S);
     A->arg = c.take<int32_t>((size_t)std::max(Q, 1));
+    A->used = c.take<int32_t>(A->parts);
+    A->hist = c.take<int32_t>((size_t)A->parts * S);
     return c.used;
 }
 

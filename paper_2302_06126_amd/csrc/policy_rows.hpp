@@ -60,11 +60,61 @@ __device__ __forceinline__ void store4(T *row, int64_t c, int64_t n, const float
     }
 }
 
-// The threads of one row: NT of them, 256 / NT rows to a block of 256 threads
-// (a row of 512 or more is a block of its own).
-template <int NT>
+// One step of a reduction over 2^k lanes that ends with the result in each of
+// them: within 16 lanes by register permutations (two of quads, two mirrors:
+// lanes that agree already stand in for one another), beyond by swaps of halves.
+// fmaxf-like ops only: commutative, both lanes of a pair get the same bits.
+template <int STEP>
+__device__ __forceinline__ int other_lane(int v) {
+    constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+    return __builtin_amdgcn_update_dpp(v, v, ctrl, 0xf, 0xf, true);
+}
+template <int LANES, typename Op>
+__device__ __forceinline__ float lanes_reduce(float v, Op op) {
+    v = op(v, __int_as_float(other_lane<0>(__float_as_int(v))));
+    v = op(v, __int_as_float(other_lane<1>(__float_as_int(v))));
+    v = op(v, __int_as_float(other_lane<2>(__float_as_int(v))));
+    v = op(v, __int_as_float(other_lane<3>(__float_as_int(v))));
+    if constexpr (LANES == 64) {
+        auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+        auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
+    return v;
+}
+template <int LANES>
+__device__ __forceinline__ int lanes_min(int v) {
+    v = min(v, other_lane<0>(v));
+    v = min(v, other_lane<1>(v));
+    v = min(v, other_lane<2>(v));
+    v = min(v, other_lane<3>(v));
+    if constexpr (LANES == 64) {
+        auto a = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+        v = min((int)a[0], (int)a[1]);
+        auto b = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+        v = min((int)b[0], (int)b[1]);
+    }
+    return v;
+}
+
+// A row's maximum (not NaN) and its lowest column; at: -2 if a NaN is among the
+// values, INT32_MAX if every value is -inf.
+struct RowMax {
+    float m;
+    int32_t at;
+};
+struct Two {
+    float s, t;
+};
+
+// The threads of one row: NT of them (16, 64 or whole wavefronts), BLOCK / NT
+// rows to a block.  The reductions' results reach every thread of the row, and
+// are the same bits in every call.
+template <int NT, int BLOCK = (NT < 256 ? 256 : NT)>
 struct RowTeam {
-    static constexpr int kBlock = NT < 256 ? 256 : NT, kRows = kBlock / NT, kW = NT < 64 ? NT : 64, kWaves = (NT + 63) / 64;
+    static_assert(NT == 16 || NT % 64 == 0, "teams of 16 lanes or of wavefronts");
+    static constexpr int kBlock = BLOCK, kRows = BLOCK / NT, kL = NT < 64 ? NT : 64, kWaves = (NT + 63) / 64;
     static __device__ __forceinline__ int tid() { return threadIdx.x % NT; }
     static __device__ __forceinline__ int row() { return threadIdx.x / NT; }
     // LDS written by the row's threads is read by others of them after this
@@ -76,48 +126,49 @@ struct RowTeam {
             __builtin_amdgcn_wave_barrier();
         }
     }
-    // op: commutative and associative up to rounding; the same tree in every call
-    template <typename V, typename Op>
-    static __device__ __forceinline__ V reduce(V v, Op op) {
-#pragma unroll
-        for (int o = kW / 2; o > 0; o >>= 1) v = op(v, V::shuffle(v, o, kW));
-        if constexpr (kWaves > 1) {
-            __shared__ V part[kWaves];
+    // of each thread's own maximum and column
+    static __device__ __forceinline__ RowMax max(RowMax v) {
+        const float m = lanes_reduce<kL>(v.m, [](float a, float b) { return a > b ? a : b; });
+        int at = lanes_min<kL>(v.at == -2 || v.m == m ? v.at : INT32_MAX);
+        if constexpr (kWaves == 1) {
+            return RowMax{m, at};
+        } else {
+            __shared__ RowMax part[kBlock / 64];
+            const int w = threadIdx.x >> 6, w0 = w / kWaves * kWaves;
             __syncthreads();   // an earlier reduction's reads are done
-            if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+            if ((threadIdx.x & 63) == 0) part[w] = RowMax{m, at};
             __syncthreads();
-            v = part[0];
+            RowMax r = part[w0];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) v = op(v, part[w]);
+            for (int i = 1; i < kWaves; ++i) {
+                const RowMax o = part[w0 + i];
+                const bool nan = r.at == -2 || o.at == -2;
+                const bool second = o.m > r.m || (o.m == r.m && o.at < r.at);
+                r = second ? o : r;
+                if (nan) r.at = -2;
+            }
+            return r;
+        }
+    }
+    static __device__ __forceinline__ Two sum(Two v) {
+        auto add = [](float a, float b) { return a + b; };
+        v = Two{lanes_reduce<kL>(v.s, add), lanes_reduce<kL>(v.t, add)};
+        if constexpr (kWaves > 1) {
+            __shared__ Two part[kBlock / 64];
+            const int w = threadIdx.x >> 6, w0 = w / kWaves * kWaves;
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) part[w] = v;
+            __syncthreads();
+            v = part[w0];
+#pragma unroll
+            for (int i = 1; i < kWaves; ++i) {
+                v.s += part[w0 + i].s;
+                v.t += part[w0 + i].t;
+            }
         }
         return v;
     }
-};
-
-// the maximum and its lowest column; nan: a NaN was among the values
-struct RowMax {
-    float m;
-    int32_t at;
-    int32_t nan;
-    static __device__ __forceinline__ RowMax shuffle(const RowMax &v, int o, int w) {
-        return RowMax{__shfl_xor(v.m, o, w), __shfl_xor(v.at, o, w), __shfl_xor(v.nan, o, w)};
-    }
-    static __device__ __forceinline__ RowMax join(const RowMax &a, const RowMax &b) {
-        const bool second = b.m > a.m || (b.m == a.m && b.at < a.at);
-        return RowMax{second ? b.m : a.m, second ? b.at : a.at, a.nan | b.nan};
-    }
-};
-struct RowSum {
-    float s;
-    static __device__ __forceinline__ RowSum shuffle(const RowSum &v, int o, int w) { return RowSum{__shfl_xor(v.s, o, w)}; }
-    static __device__ __forceinline__ RowSum join(const RowSum &a, const RowSum &b) { return RowSum{a.s + b.s}; }
-};
-struct RowSum2 {
-    float s, t;
-    static __device__ __forceinline__ RowSum2 shuffle(const RowSum2 &v, int o, int w) {
-        return RowSum2{__shfl_xor(v.s, o, w), __shfl_xor(v.t, o, w)};
-    }
-    static __device__ __forceinline__ RowSum2 join(const RowSum2 &a, const RowSum2 &b) { return RowSum2{a.s + b.s, a.t + b.t}; }
+    static __device__ __forceinline__ float sum(float v) { return sum(Two{v, 0.f}).s; }
 };
 
 }  // namespace tag
