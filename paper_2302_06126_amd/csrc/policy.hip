@@ -317,11 +317,11 @@ struct BalArgs {
 
 __device__ __forceinline__ uint64_t device_bits(int32_t M) { return M >= 64 ? ~0ull : (1ull << M) - 1ull; }
 
-// Each used row's argmax, and how often the block's rows chose each slice.
+// Each used row's argmax (into arg), and how often the block's rows chose each
+// slice: hist [S], then the used rows.
 template <typename T, int NT, int VPT, bool VEC>
-__global__ void __launch_bounds__(1024) bal_argmax(BalArgs A) {
+__device__ __forceinline__ void rows_argmax(const BalArgs &A, int32_t *hist) {
     using Team = RowTeam<NT, 1024>;
-    extern __shared__ int32_t hist[];   // [S], then the used rows
     for (int i = threadIdx.x; i <= A.S; i += 1024) hist[i] = 0;
     __syncthreads();
     const int tid = Team::tid();
@@ -353,88 +353,109 @@ __global__ void __launch_bounds__(1024) bal_argmax(BalArgs A) {
         }
     }
     __syncthreads();
+}
+
+template <typename T, int NT, int VPT, bool VEC>
+__global__ void __launch_bounds__(1024) bal_argmax(BalArgs A) {
+    extern __shared__ int32_t hist[];
+    rows_argmax<T, NT, VPT, VEC>(A, hist);
     for (int i = threadIdx.x; i < A.S; i += 1024) A.hist[(int64_t)blockIdx.x * A.S + i] = hist[i];
     if (threadIdx.x == 0) A.used[blockIdx.x] = hist[A.S];
 }
 
 // Counts of kBalSpan slices per block over the parts, and their part of the loads.
 __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
-    __shared__ int32_t sub[16][kBalSpan], cnt[kBalSpan];
+    __shared__ int32_t sub[16][kBalSpan];
     __shared__ uint64_t mask[kBalSpan];
+    __shared__ double each[kBalSpan], dev[16][64];   // what a slice gives each of its devices
     const int t = threadIdx.x, c = t & 63, g = t >> 6, s = blockIdx.x * kBalSpan + c;
+    uint64_t m = 0;
+    if (g == 0 && s < A.S) m = A.mask[s] & device_bits(A.M);
+    int32_t v[kBalParts / 16];
+#pragma unroll
+    for (int i = 0; i < kBalParts / 16; ++i) {
+        const int p = g + 16 * i;
+        v[i] = s < A.S && p < A.parts ? A.hist[(int64_t)p * A.S + s] : 0;
+    }
     int32_t n = 0;
-    if (s < A.S)
-        for (int p = g; p < A.parts; p += 16) n += A.hist[(int64_t)p * A.S + s];
+#pragma unroll
+    for (int i = 0; i < kBalParts / 16; ++i) n += v[i];
     sub[g][c] = n;
-    if (g == 0) mask[c] = s < A.S ? A.mask[s] & device_bits(A.M) : 0;
     __syncthreads();
     if (g == 0) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) n += sub[i][c];
-        cnt[c] = n;
         if (s < A.S) A.count[s] = n;
+        mask[c] = m;
+        each[c] = m ? (double)n / (double)__popcll(m) : 0.0;
     }
     __syncthreads();
-    if (t < 64) {   // device t
-        double w = 0.0;
-        for (int i = 0; i < kBalSpan; ++i)
-            if ((mask[i] >> t) & 1ull) w += (double)cnt[i] / (double)__popcll(mask[i]);
-        A.part[(int64_t)blockIdx.x * 64 + t] = w;
+    double w = 0.0;   // device c, four slices per wavefront
+#pragma unroll
+    for (int i = 4 * g; i < 4 * g + 4; ++i) w += (mask[i] >> c) & 1ull ? each[i] : 0.0;
+    dev[g][c] = w;
+    __syncthreads();
+    if (g == 0) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) w += dev[i][c];
+        A.part[(int64_t)blockIdx.x * 64 + c] = w;
     }
 }
 
-// Loads from the merging blocks' parts (in their order), then h of every slice.
+// Loads from the merging blocks' parts (in their order, by every block), then h of
+// 1,024 slices per block.
 __global__ void __launch_bounds__(1024) bal_shares(BalArgs A) {
     __shared__ double load[64], sub[16][64], centre;
     __shared__ int32_t used;
     const int t = threadIdx.x, d = t & 63, g = t >> 6, nb = (A.S + kBalSpan - 1) / kBalSpan;
-    if (t == 0) used = 0;
+    const int32_t mine = t < A.parts ? A.used[t] : 0;
+    const int32_t slice = blockIdx.x * 1024 + t;
+    uint64_t m = slice < A.S ? A.mask[slice] & device_bits(A.M) : 0;
+    double p[kBalMaxS / kBalSpan / 16];
+#pragma unroll
+    for (int i = 0; i < kBalMaxS / kBalSpan / 16; ++i) {
+        const int b = g + 16 * i;
+        p[i] = b < nb ? A.part[(int64_t)b * 64 + d] : 0.0;
+    }
     double s = 0.0;
-    for (int b = g; b < nb; b += 16) s += A.part[(int64_t)b * 64 + d];
+#pragma unroll
+    for (int i = 0; i < kBalMaxS / kBalSpan / 16; ++i) s += p[i];
+    if (t == 0) used = 0;
     sub[g][d] = s;
     __syncthreads();
-    if (t < A.parts) atomicAdd(&used, A.used[t]);
+    if (mine) atomicAdd(&used, mine);
     __syncthreads();
     if (t < 64) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) s += sub[i][t];
         s = used > 0 ? s / (double)used : 0.0;
         load[t] = s;
-        if (t < A.M) A.load[t] = (float)s;
+        if (blockIdx.x == 0 && t < A.M) A.load[t] = (float)s;
         // centre of h: its mean over the decisions taken (the softmax's gradient does not see a shift of h, and
         // what is left of h rounds less)
         double c = s * s;
         for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
-        if (t == 0) { centre = c; A.total[0] = c; A.total[1] = (double)used; }
+        if (t == 0) centre = c;
+        if (t == 0 && blockIdx.x == 0) { A.total[0] = c; A.total[1] = (double)used; }
     }
     __syncthreads();
-    const uint64_t valid = device_bits(A.M);
-    for (int i = t; i < A.S; i += 1024) {
-        uint64_t m = A.mask[i] & valid;
-        const double pop = (double)__popcll(m);
-        double w = 0.0;
-        while (m) {
-            w += load[__ffsll((unsigned long long)m) - 1];
-            m &= m - 1;
-        }
-        A.h[i] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
-    }
+    const double pop = (double)__popcll(m);
+    double w = 0.0;
+    for (; m; m &= m - 1) w += load[__ffsll((unsigned long long)m) - 1];
+    if (slice < A.S) A.h[slice] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
 }
 
-// Gradient rows, and the block's sum of the rows' losses: each thread keeps h of
-// its columns for every row that its block walks.
-template <typename T, int NT, int VPT, bool VEC>
-__global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
+// Gradient rows of the block's teams: each thread keeps h of its columns for
+// every row.  Returns the sum of the team's rows' losses.
+template <typename T, int NT, int VPT, bool VEC, int BLOCK>
+__device__ __forceinline__ double rows_grad(const BalArgs &A, const float *hs, float scale) {
 #pragma clang fp contract(off)   // (the same bits from the forms for aligned and for other rows)
-    using Team = RowTeam<NT>;
-    __shared__ double lrow[RowTeam<NT>::kRows];
+    using Team = RowTeam<NT, BLOCK>;
     const int tid = Team::tid();
-    const double n = A.total[1];
-    const float scale = n > 0.0 ? (float)((double)A.coef * A.M / n) : 0.f;
     float h[VPT];
 #pragma unroll
     for (int k = 0; k < VPT / 4; ++k)
-        load4<float, true>(A.h, 4 * (tid + NT * k), A.S, 0.f, *reinterpret_cast<float(*)[4]>(h + 4 * k));
+        load4<float, true>(hs, 4 * (tid + NT * k), A.S, 0.f, *reinterpret_cast<float(*)[4]>(h + 4 * k));
     double lsum = 0.0;
     for (int64_t base = (int64_t)blockIdx.x * Team::kRows; base < A.Q; base += (int64_t)gridDim.x * Team::kRows) {
         const int64_t q0 = base + Team::row(), q = q0 < A.Q ? q0 : A.Q - 1;
@@ -485,7 +506,23 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
             store4<T, VEC>(gr, 4 * (tid + NT * k), A.S, v);
         }
     }
-    if (tid == 0) lrow[Team::row()] = lsum;
+    return lsum;
+}
+
+__device__ __forceinline__ float row_scale(const BalArgs &A, double n) {
+    return n > 0.0 ? (float)((double)A.coef * A.M / n) : 0.f;
+}
+__device__ __forceinline__ float total_loss(const BalArgs &A, double sum, double n, double centre) {
+    return n > 0.0 ? (float)((double)A.coef * A.M * (sum / n + centre)) : 0.f;
+}
+
+// Gradient rows, and the block's sum of the rows' losses.
+template <typename T, int NT, int VPT, bool VEC>
+__global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
+    using Team = RowTeam<NT>;
+    __shared__ double lrow[Team::kRows];
+    const double lsum = rows_grad<T, NT, VPT, VEC, Team::kBlock>(A, A.h, row_scale(A, A.total[1]));
+    if (Team::tid() == 0) lrow[Team::row()] = lsum;
     __syncthreads();
     if (threadIdx.x == 0) {
         double s = 0.0;
@@ -494,30 +531,94 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
     }
 }
 
+// Few rows: everything in one block, the scores' second reading from its cache.
+constexpr int kBalSmallS = 1024;   // slices whose masks it keeps in LDS
+constexpr int kBalSmallTurns = 8;  // turns that its teams take over the rows, at most
+template <typename T, int NT, int VPT, bool VEC>
+__global__ void __launch_bounds__(1024) bal_small(BalArgs A) {
+    using Team = RowTeam<NT, 1024>;
+    __shared__ int32_t hist[kBalSmallS + 1];
+    __shared__ uint64_t mask[kBalSmallS];
+    __shared__ double each[kBalSmallS], load[64], sub[16][64], centre, lrow[Team::kRows];
+    __shared__ __attribute__((aligned(16))) float h[kBalSmallS];
+    const int t = threadIdx.x, d = t & 63, g = t >> 6;
+    const uint64_t m = t < A.S ? A.mask[t] & device_bits(A.M) : 0;
+    rows_argmax<T, NT, VPT, VEC>(A, hist);
+    const int32_t used = hist[A.S];
+    const double pop = (double)__popcll(m);
+    mask[t] = m;
+    each[t] = m ? (double)hist[t] / pop : 0.0;   // (m = 0 past the slices)
+    if (t < A.S) A.count[t] = hist[t];
+    __syncthreads();
+    double s = 0.0;
+    for (int i = g; i < A.S; i += 16) s += (mask[i] >> d) & 1ull ? each[i] : 0.0;
+    sub[g][d] = s;
+    __syncthreads();
+    if (t < 64) {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) s += sub[i][t];
+        s = used > 0 ? s / (double)used : 0.0;
+        load[t] = s;
+        if (t < A.M) A.load[t] = (float)s;
+        double c = s * s;   // (as in bal_shares)
+        for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+        if (t == 0) centre = c;
+    }
+    __syncthreads();
+    double w = 0.0;
+    for (uint64_t r = m; r; r &= r - 1) w += load[__ffsll((unsigned long long)r) - 1];
+    h[t] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
+    __syncthreads();
+    const double lsum = rows_grad<T, NT, VPT, VEC, 1024>(A, h, row_scale(A, (double)used));
+    if (Team::tid() == 0) lrow[Team::row()] = lsum;
+    __syncthreads();
+    if (t < 64) {
+        double l = t < Team::kRows ? lrow[t] : 0.0;
+        for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+        if (t == 0) A.loss[0] = total_loss(A, l, (double)used, centre);
+    }
+}
+
 // the blocks' sums, in a fixed order (a launch of its own: a fence in every
 // gradient block, for the last one to add them up, took five times the kernel)
-__global__ void __launch_bounds__(256) bal_loss(BalArgs A) {
-    __shared__ double red[4];
+__global__ void __launch_bounds__(1024) bal_loss(BalArgs A) {
+    __shared__ double red[16];
+    const double n = A.total[1], centre = A.total[0];
+    double v[kBalGrad / 1024];
+#pragma unroll
+    for (int i = 0; i < kBalGrad / 1024; ++i) {
+        const int b = threadIdx.x + 1024 * i;
+        v[i] = b < A.lparts ? A.lpart[b] : 0.0;
+    }
     double s = 0.0;
-    for (int b = threadIdx.x; b < A.lparts; b += 256) s += A.lpart[b];
+#pragma unroll
+    for (int i = 0; i < kBalGrad / 1024; ++i) s += v[i];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
-    const double n = A.total[1];
-    if (threadIdx.x == 0)
-        A.loss[0] = n > 0.0 ? (float)((double)A.coef * A.M * ((red[0] + red[1] + red[2] + red[3]) / n + A.total[0])) : 0.f;
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w) s += red[w];
+        A.loss[0] = total_loss(A, s, n, centre);
+    }
 }
 
 template <typename T, int NT, int VPT>
 void launch_bal(const BalArgs &A, bool vec, hipStream_t st) {
+    if constexpr (NT <= 64) {
+        if (A.Q <= kBalSmallTurns * (1024 / NT)) {
+            if (vec) bal_small<T, NT, VPT, true><<<1, 1024, 0, st>>>(A);
+            else bal_small<T, NT, VPT, false><<<1, 1024, 0, st>>>(A);
+            return;
+        }
+    }
     const size_t lds = sizeof(int32_t) * (A.S + 1);
     if (vec) bal_argmax<T, NT, VPT, true><<<A.parts, 1024, lds, st>>>(A);
     else bal_argmax<T, NT, VPT, false><<<A.parts, 1024, lds, st>>>(A);
     bal_count<<<(A.S + kBalSpan - 1) / kBalSpan, 1024, 0, st>>>(A);
-    bal_shares<<<1, 1024, 0, st>>>(A);
+    bal_shares<<<(A.S + 1023) / 1024, 1024, 0, st>>>(A);
     if (vec) bal_grad<T, NT, VPT, true><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
     else bal_grad<T, NT, VPT, false><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
-    bal_loss<<<1, 256, 0, st>>>(A);
+    bal_loss<<<1, 1024, 0, st>>>(A);
 }
 
 // threads per row

@@ -17,7 +17,7 @@ import contextlib
 
 import numpy as np
 
-from . import _abi, _ptr, _stream, _torch
+from . import _abi, _ptr, _torch
 from ._abi import C, TAG_BF16, TAG_F32, check, tag_constraints
 
 __all__ = ["Constrain", "Balance"]
@@ -35,6 +35,11 @@ def _current(device):
     """Makes `device` the current one while its kernels are launched."""
     torch = _torch()
     return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _raw_stream(stream, device) -> int:
+    """The given stream's handle, or that of `device`'s current one."""
+    return int(stream.cuda_stream) if stream is not None else _torch()._C._cuda_getCurrentRawStream(device.index)
 
 
 def _dtype(dtype) -> int:
@@ -126,7 +131,7 @@ class Constrain:
         with _current(dev):
             check(_abi.load().tag_constrain(Q, S, self._code, _ptr(scores), xs, C.byref(c), _ptr(self.scores), S,
                                             _ptr(self.prior), S, _ptr(self.argmax), _ptr(self.best), _ptr(self.ws),
-                                            self.ws_bytes, _stream(stream)), "tag_constrain")
+                                            self.ws_bytes, _raw_stream(stream, dev)), "tag_constrain")
         out = (self.prior, self.argmax, self.best)
         return out if self.scores is None else out + (self.scores,)
 
@@ -163,6 +168,6 @@ class Balance:
         with _current(self.device):
             check(_abi.load().tag_balance(self.Q, self.S, self._code, _ptr(scores), xs, _ptr(self.masks), self.M, u,
                                           float(coef), _ptr(self.grad), self.S, 0, _ptr(self.loss), _ptr(self.count),
-                                          _ptr(self.load), _ptr(self.ws), self.ws_bytes, _stream(stream)),
+                                          _ptr(self.load), _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device)),
                   "tag_balance")
         return self.loss
