@@ -37,7 +37,9 @@ SEARCH_EXPORTS = ("tag_search_problem_create", "tag_search_problem_destroy", "ta
 EXPORTS += ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace", "tag_balance")
 
 # include/tag_train.h
-TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step")
+TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step",
+                 # include/tag_optim.h
+                 "tag_orthogonalise_workspace", "tag_orthogonalise", "tag_muon_workspace", "tag_muon_step")
 
 # kernel stages (include/tag_profile.h)
 STAGE_NAMES = ("graph_build", "encode", "transform", "agg_op_op", "agg_op_dev", "agg_dev_op", "agg_dev_merge",
@@ -101,6 +103,28 @@ class tag_constraints(C.Structure):
     _fields_ = [("allow", _PF), ("allow_stride", C.c_int64), ("bias", _PF), ("bias_stride", C.c_int64),
                 ("history", _PF), ("history_stride", C.c_int64), ("n_history", C.c_int32), ("history_len", _PF),
                 ("repetition", _PF), ("presence", _PF), ("frequency", _PF)]
+
+
+class tag_newton_schulz(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("a", C.c_float), ("b", C.c_float), ("c", C.c_float), ("eps", C.c_float)]
+
+
+class tag_matrices(C.Structure):
+    _fields_ = [("base", _PF), ("row_stride", C.c_int64), ("matrix_stride", C.c_int64)]
+
+
+class tag_ortho_group(C.Structure):
+    _fields_ = [("count", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("in", tag_matrices),
+                ("out", tag_matrices)]
+
+
+class tag_muon_group(C.Structure):
+    _fields_ = [("count", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("plain", C.c_int32),
+                ("w", tag_matrices), ("g", tag_matrices), ("m", tag_matrices)]
+
+
+class tag_muon_options(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32)]
 
 
 class tag_search_problem_desc(C.Structure):
@@ -202,6 +226,13 @@ def load() -> C.CDLL:
     lib.tag_train_step.argtypes = [vp, C.POINTER(tag_model_dims), C.POINTER(tag_weights), C.POINTER(tag_features),
                                    C.POINTER(tag_slices), C.POINTER(tag_train_batch), C.POINTER(tag_grads),
                                    C.c_float, vp, vp, C.c_size_t, vp]
+    # include/tag_optim.h
+    lib.tag_orthogonalise_workspace.argtypes = [C.POINTER(tag_ortho_group), S, szp]
+    lib.tag_orthogonalise.argtypes = [C.POINTER(tag_ortho_group), S, S, C.POINTER(tag_newton_schulz), vp, C.c_size_t,
+                                      vp]
+    lib.tag_muon_workspace.argtypes = [C.POINTER(tag_muon_group), S, szp]
+    lib.tag_muon_step.argtypes = [C.POINTER(tag_muon_group), S, C.POINTER(tag_newton_schulz),
+                                  C.POINTER(tag_muon_options), vp, C.c_size_t, vp]
     for name in TRAIN_EXPORTS:
         getattr(lib, name).restype = S
     lib.tag_gnn_decide_full_workspace.argtypes = [vp, C.POINTER(tag_model_dims), S, S, szp]

@@ -1,0 +1,679 @@
+// Orthogonalised optimiser step (include/tag_optim.h): Newton-Schulz products on
+// the matrix cores, around them the momentum and the update.
+//
+// A step of the iteration is three products of n x n by K: A = X X^T, A A and
+// B X (n <= m; 2 n^2 m + 2 n^3 + 2 n^2 m flops, the first two symmetric, so
+// half of their tiles are computed and written twice).  The 15 products of five
+// steps depend on one another, so each is one launch over all matrices of all
+// groups, and its epilogue forms the next operand: nothing but products runs in
+// between.
+//
+// Operands.  Every matrix of the iteration has entries of magnitude <= 3.5 (X),
+// 12.25 (A) or 15 (B) (checked on the host for the coefficients), so it is held
+// as 2^12 times its value in two fp16 parts, hi = fp16(x) and lo = fp16(x - hi):
+// each rounding leaves at most 2^-11 of what it rounds, so the pair holds x to
+// 2^-22 of it (2^-24.7 root mean square; fp32's own rounding 2^-25.4).  A product
+// is hi hi' + hi lo' + lo hi' (what is left out, lo lo', is below 2^-22 of it,
+// 2^-24.8 root mean square): three fp16 matrix instructions instead of the six
+// that exact bf16 splits need, or of fp32 ones at a sixteenth of the rate.  bf16 matrices take hi hi' alone; X keeps both parts, since the
+// a X term carries its error through every step.
+//
+// Layout.  The operands lie in the order in which a 32x32x16 instruction takes
+// them ("fragments": 32 rows x 16 k, lane l holds 8 consecutive k of row l % 32,
+// k / 8 % 2 = l / 32; 1 KiB), fragment (r, k) of a plane at (r kf + k) KiB, so a
+// tile's k-step is a few contiguous runs, goes from memory into LDS by direct
+// loads, and every LDS access is lane-linear (no bank conflicts).  Rows and
+// columns are padded with zeros to multiples of 64.  X is kept in both orders
+// (X for A, X^T for B X): a lane of the accumulators holds four consecutive rows
+// of a column, which is the operand order of the transpose; the other order goes
+// through LDS.
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "../../include/tag_optim.h"
+#include "agg_common.hpp"
+
+namespace tag {
+namespace {
+
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+
+constexpr float kScale = 4096.f, kInvScale = 1.f / 4096.f;
+constexpr int kMaxGroups = 16;      // groups of one set of launches
+constexpr int kFrag = 512;          // elements of a fragment
+constexpr int kSumChunk = 8192;     // elements per sum-of-squares block
+
+struct Arr {
+    void *p;
+    int64_t row, mat;
+};
+
+struct NsGroup {
+    int32_t count, rows, cols;
+    int32_t n, m, np, mp;        // n <= m, padded to multiples of 64
+    int32_t trans;               // rows > cols
+    int32_t plain;
+    int32_t chunks;              // sum-of-squares blocks per matrix
+    Arr in, out, mom;            // in / out, or g / w and the momentum
+    uint16_t *ops;               // operands of the group's matrices
+    int64_t ops_stride;          // elements per matrix
+    double *part;                // [count][chunks]
+    float factor;                // of O(u) in the update
+};
+
+struct NsBatch {
+    NsGroup g[kMaxGroups];
+    int32_t first[kMaxGroups + 1];   // first block of each group
+    int32_t n_groups;
+    float a, b, c, eps;
+    int32_t cur;                 // which of the two X buffers is read
+    // update
+    float lr, momentum, decay;
+    int32_t nesterov;
+};
+
+// operands of a matrix: X and X^T of both buffers (hi, lo planes), A, B
+__device__ __forceinline__ uint16_t *x_plane(const NsGroup &G, int mat, int buf, int t, int plane) {
+    return G.ops + mat * G.ops_stride + (int64_t)(buf * 4 + t * 2 + plane) * G.np * G.mp;
+}
+__device__ __forceinline__ uint16_t *s_plane(const NsGroup &G, int mat, int which, int plane) {
+    return G.ops + mat * G.ops_stride + (int64_t)8 * G.np * G.mp + (int64_t)(which * 2 + plane) * G.np * G.np;
+}
+
+// group of a block, and the block's number within it
+__device__ __forceinline__ int find_group(const NsBatch &B, int32_t &bid) {
+    int g = 0;
+    while (g + 1 < B.n_groups && bid >= B.first[g + 1]) ++g;
+    bid -= B.first[g];
+    return g;
+}
+
+// two parts of 2^12 x
+__device__ __forceinline__ void split2(float x0, float x1, unsigned &hi, unsigned &lo) {
+    const h2 h = h2{(_Float16)x0, (_Float16)x1};
+    const h2 l = h2{(_Float16)(x0 - (float)h.x), (_Float16)(x1 - (float)h.y)};
+    hi = __builtin_bit_cast(unsigned, h);
+    lo = __builtin_bit_cast(unsigned, l);
+}
+__device__ __forceinline__ float join2(unsigned hi, unsigned lo, int i) {
+    const h2 h = __builtin_bit_cast(h2, hi), l = __builtin_bit_cast(h2, lo);
+    return (float)h[i] + (float)l[i];
+}
+
+template <typename T>
+__device__ __forceinline__ float get(const T *p);
+template <>
+__device__ __forceinline__ float get<float>(const float *p) { return *p; }
+template <>
+__device__ __forceinline__ float get<uint16_t>(const uint16_t *p) { return bf2f(*p); }
+
+// ------------------------------------------------------- momentum and norms
+// Sums of squares of u per kSumChunk elements (in 64 bits: a gradient's squares
+// leave the range of fp32), with the momentum update on the way; plain groups
+// are finished here.
+template <typename T, bool MUON>
+__global__ void __launch_bounds__(256) ns_norm(NsBatch B) {
+    __shared__ double red[4];
+    int32_t bid = blockIdx.x;
+    const NsGroup &G = B.g[find_group(B, bid)];
+    const int mat = bid / G.chunks, chunk = bid % G.chunks;
+    const int64_t total = (int64_t)G.rows * G.cols, e0 = (int64_t)chunk * kSumChunk;
+    const int64_t e1 = total < e0 + kSumChunk ? total : e0 + kSumChunk;
+    const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
+    float *mom = MUON ? static_cast<float *>(G.mom.p) + mat * G.mom.mat : nullptr;
+    double s = 0.0;
+#pragma unroll 4
+    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
+        const int64_t r = e / G.cols, c = e - r * G.cols;
+        float u = get(in + r * G.in.row + c);
+        if (MUON) {
+            float *mp = mom + r * G.mom.row + c;
+            const float m = B.momentum * *mp + u;
+            *mp = m;
+            u = B.nesterov ? fmaf(B.momentum, m, u) : m;
+            if (G.plain) {
+                float *w = static_cast<float *>(G.out.p) + mat * G.out.mat + r * G.out.row + c;
+                *w = (1.f - B.lr * B.decay) * *w - B.lr * u;
+            }
+        }
+        s += (double)u * (double)u;
+    }
+    if (MUON && G.plain) return;
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) G.part[(int64_t)mat * G.chunks + chunk] = red[0] + red[1] + red[2] + red[3];
+}
+
+// X and X^T of the first buffer: one block per 64 x 64 tile of the padded
+// matrix, through LDS.
+template <typename T, bool MUON>
+__global__ void __launch_bounds__(256) ns_prepare(NsBatch B) {
+    __shared__ float tile[64][65];   // [row of X][column]
+    __shared__ double red[4];
+    int32_t bid = blockIdx.x;
+    const NsGroup &G = B.g[find_group(B, bid)];
+    const int ti = G.np / 64, tj = G.mp / 64, mat = bid / (ti * tj), t = bid % (ti * tj), i0 = t / tj * 64, j0 = t % tj * 64;
+    double s = 0.0;
+    for (int c = threadIdx.x; c < G.chunks; c += 256) s += G.part[(int64_t)mat * G.chunks + c];
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    const double norm = sqrt(red[0] + red[1] + red[2] + red[3]);
+    const double scale = (double)kScale / (norm + (double)B.eps);
+    const bool bad = !(norm < INFINITY);
+    const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
+    const float *mom = MUON ? static_cast<const float *>(G.mom.p) + mat * G.mom.mat : nullptr;
+    const int a = threadIdx.x & 63;
+    for (int b = threadIdx.x >> 6; b < 64; b += 4) {
+        // consecutive threads along the rows of the matrix as it is stored
+        const int li = G.trans ? a : b, lj = G.trans ? b : a, i = i0 + li, j = j0 + lj;
+        float x = 0.f;
+        if (i < G.n && j < G.m) {
+            const int64_t r = G.trans ? j : i, c = G.trans ? i : j;
+            float u = get(in + r * G.in.row + c);
+            if (MUON) {
+                const float m = mom[r * G.mom.row + c];
+                u = B.nesterov ? fmaf(B.momentum, m, u) : m;
+            }
+            x = bad ? __builtin_nanf("") : (float)((double)u * scale);
+        }
+        tile[li][lj] = x;
+    }
+    __syncthreads();
+    // 16-byte pieces: 64 rows x 8 chunks of 8 k, for X then X^T
+    for (int p = threadIdx.x; p < 1024; p += 256) {
+        const int tr = p >> 9, r = p & 63, ch = (p >> 6) & 7;
+        u4v hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int k = 8 * ch + 2 * e;
+            unsigned h, l;
+            if (tr) split2(tile[k][r], tile[k + 1][r], h, l);
+            else split2(tile[r][k], tile[r][k + 1], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        const int row = (tr ? j0 : i0) + r, k = (tr ? i0 : j0) + 8 * ch, kf = (tr ? G.np : G.mp) / 16;
+        const int64_t at = ((int64_t)(row / 32) * kf + k / 16) * kFrag + (row % 32 + 32 * (k / 8 % 2)) * 8;
+        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, tr, 0) + at) = hi;
+        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, tr, 1) + at) = lo;
+    }
+}
+
+// ------------------------------------------------------------------ products
+enum { kGram = 0, kSquare = 1, kApply = 2, kFinal = 3, kUpdate = 4 };
+
+// four consecutive k (k0 + 4 h, h = lane / 32) of row lane % 32 per lane: the
+// half of each 8-k chunk that the lane owns
+__device__ __forceinline__ int64_t frag_at(int64_t rf, int64_t kf, int64_t nk, int g, int lane) {
+    return (rf * nk + kf * 2 + (g >> 1)) * kFrag + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
+}
+__device__ __forceinline__ void store_frag(uint16_t *hi, uint16_t *lo, int64_t rf, int64_t kf, int64_t nk, int lane,
+                                           const float (&v)[16]) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        uint2 h, l;
+        split2(v[4 * g], v[4 * g + 1], h.x, l.x);
+        split2(v[4 * g + 2], v[4 * g + 3], h.y, l.y);
+        const int64_t at = frag_at(rf, kf, nk, g, lane);
+        *reinterpret_cast<uint2 *>(hi + at) = h;
+        *reinterpret_cast<uint2 *>(lo + at) = l;
+    }
+}
+
+// C = R S^T over one tile of T x T outputs per block, R and S operand planes of
+// K/16 fragments per row; four wavefronts of T/2 x T/2.  PARTS = 2: three part
+// products a step, PARTS = 1: the hi planes alone.  The next k-step's fragments
+// are on their way into the other LDS buffer while one is multiplied.
+//
+// The matrix cores round their sums towards minus infinity, a bias that grows
+// with the number of steps where rounding errors grow with its root; with
+// PARTS = 2 every other fragment of k is taken with one operand negated, into
+// accumulators of its own, and subtracted at the end, so the two biases cancel.
+template <int T, int PARTS, int MODE, typename OUT>
+__global__ void __launch_bounds__(256) ns_product(NsBatch B) {
+    constexpr int F = T / 32, W = F / 2, kStep = 4 * F * PARTS, NS = PARTS;   // NS accumulator sets
+    constexpr bool SYM = MODE == kGram || MODE == kSquare;
+    constexpr int kBytes = 2 * kStep * 1024 > 4 * 32 * 33 * 4 ? 2 * kStep * 1024 : 4 * 32 * 33 * 4;
+    __shared__ __attribute__((aligned(1024))) unsigned char sh[kBytes];
+    int32_t bid = (int32_t)xcd_swizzle(blockIdx.x, gridDim.x);
+    const NsGroup &G = B.g[find_group(B, bid)];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
+    const int nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T, tiles = SYM ? nt * (nt + 1) / 2 : nt * mt;
+    const int mat = bid / tiles, t = bid % tiles;
+    int I, J;
+    if (SYM) {   // I <= J, in the order of J
+        J = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+        while (J * (J + 1) / 2 > t) --J;
+        while ((J + 1) * (J + 2) / 2 <= t) ++J;
+        I = t - J * (J + 1) / 2;
+    } else {     // strips of eight rows of tiles
+        const int strip = t / (8 * mt), h = min(8, nt - 8 * strip), r = t - strip * 8 * mt;
+        I = 8 * strip + r % h;
+        J = r / h;
+    }
+    const int K = MODE == kGram ? G.mp : G.np, nk = K / 16;
+    const int rfR = G.np / 32, rfS = (SYM ? G.np : G.mp) / 32;   // row fragments of R and S
+    // each wavefront's fragments of a step, as pointers to its lanes' 16 bytes
+    const uint16_t *src[kStep / 4];
+#pragma unroll
+    for (int i = 0; i < kStep / 4; ++i) {
+        const int f = wave + 4 * i, side = f / (2 * F * PARTS), plane = f / (2 * F) % PARTS, rf = f / 2 % F, kf = f % 2;
+        const uint16_t *p;
+        if (MODE == kGram) p = x_plane(G, mat, B.cur, 0, plane);
+        else if (MODE == kSquare) p = s_plane(G, mat, 0, plane);
+        else p = side ? x_plane(G, mat, B.cur, 1, plane) : s_plane(G, mat, 1, plane);
+        // (row fragments past the matrix: the last one again, its products unused)
+        const int row = min((side ? J : I) * F + rf, (side ? rfS : rfR) - 1);
+        src[i] = p + ((int64_t)row * nk + kf) * kFrag + lane * 8;
+    }
+    auto load = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < kStep / 4; ++i) {
+            load_lds<16>(src[i], sh + (buf * kStep + wave + 4 * i) * 1024);
+            src[i] += 2 * kFrag;
+        }
+    };
+    f16v acc[NS][W][W];
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[s][i][j][e] = 0.f;
+    load(0);
+    const int steps = K / 32;
+    for (int s = 0; s < steps; ++s) {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();   // this step's fragments are there, the last step's reads of the other buffer are done
+        if (s + 1 < steps) load((s + 1) & 1);
+        const h8 *fr = reinterpret_cast<const h8 *>(sh + (s & 1) * kStep * 1024);
+#pragma unroll
+        for (int kf = 0; kf < 2; ++kf) {
+            h8 a[W][PARTS], b[W][PARTS];
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    a[i][p] = fr[((p * F + wi * W + i) * 2 + kf) * 64 + lane];
+                    b[i][p] = fr[(((PARTS + p) * F + wj * W + i) * 2 + kf) * 64 + lane];
+                    if (PARTS == 2 && kf == 1) a[i][p] = -a[i][p];
+                }
+            f16v(&d)[W][W] = acc[PARTS == 2 ? kf : 0];
+            if (PARTS == 2) {
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][PARTS - 1], b[j][0], d[i][j], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < W; ++i)
+#pragma unroll
+                    for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][PARTS - 1], d[i][j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], d[i][j], 0, 0, 0);
+        }
+    }
+    __syncthreads();   // the fragments' LDS is free
+    // lane l of a 32 x 32 block holds column l % 32, rows 8 (e / 4) + 4 (l / 32) + e % 4
+    float *turn = reinterpret_cast<float *>(sh) + wave * 32 * 33;
+    const int half = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int fi = I * F + wi * W + i, fj = J * F + wj * W + j;
+            if (fi >= rfR || fj >= rfS || (SYM && fi > fj)) continue;   // (uniform over the wavefront)
+            float v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = (NS == 2 ? acc[0][i][j][e] - acc[NS - 1][i][j][e] : acc[0][i][j][e]) * kInvScale;
+            if (MODE != kGram) {   // c A A + b A, B X + a X: the term's own order is that of the lane
+                const uint16_t *hi = MODE == kSquare ? s_plane(G, mat, 0, 0) : x_plane(G, mat, B.cur, 1, 0);
+                const uint16_t *lo = MODE == kSquare ? s_plane(G, mat, 0, 1) : x_plane(G, mat, B.cur, 1, 1);
+                const float cv = MODE == kSquare ? B.c : 1.f, ct = MODE == kSquare ? B.b : B.a;
+                const int64_t nkt = G.np / 16;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t at = frag_at(fj, fi, nkt, g, lane);
+                    const uint2 h = *reinterpret_cast<const uint2 *>(hi + at), l = *reinterpret_cast<const uint2 *>(lo + at);
+                    v[4 * g] = fmaf(ct, join2(h.x, l.x, 0), cv * v[4 * g]);
+                    v[4 * g + 1] = fmaf(ct, join2(h.x, l.x, 1), cv * v[4 * g + 1]);
+                    v[4 * g + 2] = fmaf(ct, join2(h.y, l.y, 0), cv * v[4 * g + 2]);
+                    v[4 * g + 3] = fmaf(ct, join2(h.y, l.y, 1), cv * v[4 * g + 3]);
+                }
+            }
+            const bool last = MODE == kFinal || MODE == kUpdate;
+            uint16_t *d0 = nullptr, *d1 = nullptr, *t0 = nullptr, *t1 = nullptr;
+            if (!last) {
+                if (SYM) {
+                    d0 = t0 = s_plane(G, mat, MODE == kSquare, 0);
+                    d1 = t1 = s_plane(G, mat, MODE == kSquare, 1);
+                } else {
+                    d0 = x_plane(G, mat, 1 - B.cur, 1, 0); d1 = x_plane(G, mat, 1 - B.cur, 1, 1);
+                    t0 = x_plane(G, mat, 1 - B.cur, 0, 0); t1 = x_plane(G, mat, 1 - B.cur, 0, 1);
+                }
+                store_frag(d0, d1, fj, fi, G.np / 16, lane, v);
+                if (SYM && fi == fj) continue;
+            }
+            if (!last || G.trans) {   // the other order, through LDS
+#pragma unroll
+                for (int e = 0; e < 16; ++e) turn[(8 * (e >> 2) + 4 * half + (e & 3)) * 33 + col] = v[e];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = turn[col * 33 + 8 * (e >> 2) + 4 * half + (e & 3)];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+            if (!last) {
+                store_frag(t0, t1, fi, fj, (SYM ? G.np : G.mp) / 16, lane, v);
+                continue;
+            }
+            // rows of the result as it is stored: consecutive lanes along them
+            OUT *out = static_cast<OUT *>(G.out.p) + mat * G.out.mat;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int k = 8 * (e >> 2) + 4 * half + (e & 3);
+                const int64_t r = (G.trans ? fj * 32 : fi * 32) + k, c = (G.trans ? fi * 32 : fj * 32) + col;
+                if (r >= G.rows || c >= G.cols) continue;
+                OUT *p = out + r * G.out.row + c;
+                const float o = v[e] * kInvScale;
+                if constexpr (MODE == kUpdate) *p = (1.f - B.lr * B.decay) * *p - B.lr * G.factor * o;
+                else if constexpr (sizeof(OUT) == 2) *p = f2bf(o);
+                else *p = o;
+            }
+        }
+}
+
+// ---------------------------------------------------------------------- host
+int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+
+// workspace of one set of groups, and the pointers into it
+size_t carve_ns(NsGroup *g, int32_t n, void *base) {
+    Carver c(base);
+    for (int i = 0; i < n; ++i) {
+        NsGroup &G = g[i];
+        if (G.plain) continue;
+        G.part = c.take<double>((size_t)G.count * G.chunks);
+        G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np;
+        G.ops = c.take<uint16_t>((size_t)G.count * G.ops_stride);
+    }
+    return c.used;
+}
+
+void shape_ns(NsGroup *G, int32_t count, int32_t rows, int32_t cols, int32_t plain) {
+    G->count = count; G->rows = rows; G->cols = cols; G->plain = plain;
+    G->trans = rows > cols;
+    G->n = std::min(rows, cols); G->m = std::max(rows, cols);
+    G->np = (int32_t)up64(G->n); G->mp = (int32_t)up64(G->m);
+    G->chunks = (int32_t)(((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
+}
+
+constexpr int kMaxSide = 32768;   // rows or columns
+
+tag_status check_shape(int32_t count, int32_t rows, int32_t cols, bool plain) {
+    if (count < 1 || rows < 1 || cols < 1) TAG_FAIL(TAG_EINVAL, "need count, rows and cols >= 1");
+    if (!plain && (rows > kMaxSide || cols > kMaxSide)) TAG_FAIL(TAG_ESHAPE, "at most 32768 rows or columns");
+    // (blocks are counted in 32 bits)
+    const int64_t blocks = std::max((up64(rows) / 64) * (up64(cols) / 64), ((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
+    if (blocks * count > (1 << 26)) TAG_FAIL(TAG_ESHAPE, "too many or too large matrices in a group");
+    return TAG_OK;
+}
+
+tag_status check_array(const tag_matrices &a, int32_t count, int32_t rows, int32_t cols, size_t el, bool written,
+                       const char *what) {
+    if (!a.base) TAG_FAIL(TAG_EINVAL, std::string(what) + " must be non-NULL");
+    if ((uintptr_t)a.base % el) TAG_FAIL(TAG_EINVAL, std::string(what) + " must be aligned to its elements");
+    if ((rows > 1 && a.row_stride < cols) || (count > 1 && a.matrix_stride < 0))
+        TAG_FAIL(TAG_EINVAL, std::string(what) + ": a row stride is below the number of columns, or a stride negative");
+    if (!written || count == 1) return TAG_OK;
+    const int64_t span = (rows - 1) * (rows > 1 ? a.row_stride : 0) + cols;
+    const bool apart = a.matrix_stride >= span;
+    const bool woven = a.matrix_stride >= cols && (rows == 1 || a.row_stride >= (count - 1) * a.matrix_stride + cols);
+    if (!apart && !woven) TAG_FAIL(TAG_EINVAL, std::string(what) + ": its matrices overlap");
+    return TAG_OK;
+}
+
+// the largest |p| over [0, hi] of p(s) = s (a + b s^2 + c s^4), or with `poly` of
+// b t + c t^2 over t in [0, hi^2]: at the ends and where the derivative is zero
+double peak(double a, double b, double c, double hi, bool poly) {
+    double best = 0.0;
+    auto at = [&](double t) {
+        if (!(t >= 0.0 && t <= hi * hi)) return;
+        const double v = poly ? b * t + c * t * t : std::sqrt(t) * (a + b * t + c * t * t);
+        best = std::max(best, std::fabs(v));
+    };
+    at(hi * hi);
+    if (poly) {
+        if (c != 0.0) at(-b / (2.0 * c));
+    } else if (c != 0.0) {   // a + 3 b t + 5 c t^2 = 0
+        const double d = 9.0 * b * b - 20.0 * a * c;
+        if (d >= 0.0) {
+            at((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+            at((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+        }
+    } else if (b != 0.0) {
+        at(-a / (3.0 * b));
+    }
+    return best;
+}
+
+tag_status check_ns(const tag_newton_schulz *ns) {
+    if (!ns) TAG_FAIL(TAG_EINVAL, "the iteration must be non-NULL");
+    if (ns->steps < 1 || ns->steps > 32) TAG_FAIL(TAG_EINVAL, "steps must be in [1, 32]");
+    if (!(ns->eps > 0.f) || !std::isfinite(ns->eps)) TAG_FAIL(TAG_EINVAL, "eps must be positive and finite");
+    if (!std::isfinite(ns->a) || !std::isfinite(ns->b) || !std::isfinite(ns->c))
+        TAG_FAIL(TAG_EINVAL, "coefficients must be finite");
+    double hi = 1.0;
+    for (int i = 0; i < ns->steps; ++i) {
+        if (peak(ns->a, ns->b, ns->c, hi, true) > 15.0)
+            TAG_FAIL(TAG_EINVAL, "coefficients let an eigenvalue of B leave [-15, 15]");
+        hi = peak(ns->a, ns->b, ns->c, hi, false);
+        if (hi > 3.5) TAG_FAIL(TAG_EINVAL, "coefficients let a singular value leave [0, 3.5]");
+    }
+    return TAG_OK;
+}
+
+template <typename Blocks>
+unsigned set_blocks(NsBatch &B, Blocks blocks) {
+    int64_t n = 0;
+    for (int i = 0; i < B.n_groups; ++i) {
+        B.first[i] = (int32_t)n;
+        n += blocks(B.g[i]);
+    }
+    B.first[B.n_groups] = (int32_t)n;
+    return (unsigned)n;
+}
+
+template <int T, int PARTS, typename OUT>
+void launch_product(NsBatch &B, int mode, hipStream_t st) {
+    const unsigned grid = set_blocks(B, [&](const NsGroup &G) -> int64_t {
+        const int64_t nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T;
+        return G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
+    });
+    switch (mode) {
+        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 256, 0, st>>>(B); break;
+        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 256, 0, st>>>(B); break;
+        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 256, 0, st>>>(B); break;
+        case kFinal: ns_product<T, PARTS, kFinal, OUT><<<grid, 256, 0, st>>>(B); break;
+        default:
+            if constexpr (sizeof(OUT) == 4) ns_product<T, PARTS, kUpdate, float><<<grid, 256, 0, st>>>(B);
+    }
+}
+
+// Tiles of 128 x 128 once they fill the chip, else of 64 x 64.
+template <int PARTS, typename OUT>
+void launch_tiles(NsBatch &B, int mode, hipStream_t st) {
+    int64_t n = 0;
+    for (int i = 0; i < B.n_groups; ++i) {
+        const NsGroup &G = B.g[i];
+        const int64_t nt = (G.np + 127) / 128, mt = (G.mp + 127) / 128;
+        n += G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
+    }
+    if (n >= 128) launch_product<128, PARTS, OUT>(B, mode, st);
+    else launch_product<64, PARTS, OUT>(B, mode, st);
+}
+
+template <typename T, bool MUON, int PARTS>
+void run_ns(NsBatch &all, int steps, hipStream_t st) {
+    unsigned grid = set_blocks(all, [](const NsGroup &G) { return (int64_t)G.count * G.chunks; });
+    ns_norm<T, MUON><<<grid, 256, 0, st>>>(all);
+    NsBatch B = all;   // without the plain groups
+    B.n_groups = 0;
+    for (int i = 0; i < all.n_groups; ++i)
+        if (!all.g[i].plain) B.g[B.n_groups++] = all.g[i];
+    if (B.n_groups == 0) return;
+    grid = set_blocks(B, [](const NsGroup &G) { return (int64_t)G.count * (G.np / 64) * (G.mp / 64); });
+    ns_prepare<T, MUON><<<grid, 256, 0, st>>>(B);
+    for (int s = 0; s < steps; ++s) {
+        B.cur = s & 1;
+        launch_tiles<PARTS, T>(B, kGram, st);
+        launch_tiles<PARTS, T>(B, kSquare, st);
+        launch_tiles<PARTS, T>(B, s + 1 < steps ? kApply : MUON ? kUpdate : kFinal, st);
+    }
+}
+
+Arr arr(const tag_matrices &a) { return Arr{a.base, a.row_stride, a.matrix_stride}; }
+
+void fill_ortho(NsBatch &B, const tag_ortho_group *g, int32_t n) {
+    B.n_groups = n;
+    for (int i = 0; i < n; ++i) {
+        B.g[i] = NsGroup{};
+        shape_ns(&B.g[i], g[i].count, g[i].rows, g[i].cols, 0);
+        B.g[i].in = arr(g[i].in);
+        B.g[i].out = arr(g[i].out);
+    }
+}
+
+void fill_muon(NsBatch &B, const tag_muon_group *g, int32_t n) {
+    B.n_groups = n;
+    for (int i = 0; i < n; ++i) {
+        B.g[i] = NsGroup{};
+        shape_ns(&B.g[i], g[i].count, g[i].rows, g[i].cols, g[i].plain != 0);
+        B.g[i].in = arr(g[i].g);
+        B.g[i].out = arr(g[i].w);
+        B.g[i].mom = arr(g[i].m);
+        B.g[i].factor = (float)std::sqrt(std::max(1.0, (double)g[i].rows / g[i].cols));
+    }
+}
+
+// sets of at most kMaxGroups groups run one after the other in the same workspace
+template <typename Group, typename Fill>
+size_t workspace_of(const Group *g, int32_t n, Fill fill) {
+    size_t most = 0;
+    for (int32_t i = 0; i < n; i += kMaxGroups) {
+        NsBatch B{};
+        const int32_t k = std::min(kMaxGroups, n - i);
+        fill(B, g + i, k);
+        most = std::max(most, carve_ns(B.g, k, nullptr));
+    }
+    return most;
+}
+
+tag_status check_ortho_groups(const tag_ortho_group *g, int32_t n, bool arrays, size_t el) {
+    if (!g || n < 1) TAG_FAIL(TAG_EINVAL, "need at least one group");
+    for (int32_t i = 0; i < n; ++i) {
+        tag_status st = check_shape(g[i].count, g[i].rows, g[i].cols, false);
+        if (st == TAG_OK && arrays) st = check_array(g[i].in, g[i].count, g[i].rows, g[i].cols, el, false, "in");
+        if (st == TAG_OK && arrays) st = check_array(g[i].out, g[i].count, g[i].rows, g[i].cols, el, true, "out");
+        if (st != TAG_OK) return st;
+    }
+    return TAG_OK;
+}
+
+tag_status check_muon_groups(const tag_muon_group *g, int32_t n, bool arrays) {
+    if (!g || n < 1) TAG_FAIL(TAG_EINVAL, "need at least one group");
+    for (int32_t i = 0; i < n; ++i) {
+        tag_status st = check_shape(g[i].count, g[i].rows, g[i].cols, g[i].plain != 0);
+        if (st == TAG_OK && arrays) st = check_array(g[i].g, g[i].count, g[i].rows, g[i].cols, 4, false, "g");
+        if (st == TAG_OK && arrays) st = check_array(g[i].w, g[i].count, g[i].rows, g[i].cols, 4, true, "w");
+        if (st == TAG_OK && arrays) st = check_array(g[i].m, g[i].count, g[i].rows, g[i].cols, 4, true, "m");
+        if (st != TAG_OK) return st;
+        if (arrays && (g[i].w.base == g[i].g.base || g[i].w.base == g[i].m.base || g[i].g.base == g[i].m.base))
+            TAG_FAIL(TAG_EINVAL, "w, g and m must be different arrays");
+    }
+    return TAG_OK;
+}
+
+}  // namespace
+}  // namespace tag
+
+using namespace tag;
+
+extern "C" tag_status tag_orthogonalise_workspace(const tag_ortho_group *groups, int32_t n_groups, size_t *bytes) {
+    clear_error();
+    if (!bytes) TAG_FAIL(TAG_EINVAL, "bytes must be non-NULL");
+    const tag_status st = check_ortho_groups(groups, n_groups, false, 4);
+    if (st != TAG_OK) return st;
+    *bytes = workspace_of(groups, n_groups, fill_ortho);
+    return TAG_OK;
+}
+
+extern "C" tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n_groups, int32_t dtype,
+                                        const tag_newton_schulz *ns, void *workspace, size_t ws_bytes,
+                                        void *hip_stream) {
+    clear_error();
+    if (dtype != TAG_F32 && dtype != TAG_BF16) TAG_FAIL(TAG_EINVAL, "dtype must be TAG_F32 or TAG_BF16");
+    tag_status st = check_ortho_groups(groups, n_groups, true, dtype == TAG_BF16 ? 2 : 4);
+    if (st == TAG_OK) st = check_ns(ns);
+    if (st != TAG_OK) return st;
+    if (workspace_of(groups, n_groups, fill_ortho) > ws_bytes)
+        TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_orthogonalise_workspace)");
+    if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    for (int32_t i = 0; i < n_groups; i += kMaxGroups) {
+        NsBatch B{};
+        fill_ortho(B, groups + i, std::min(kMaxGroups, n_groups - i));
+        carve_ns(B.g, B.n_groups, workspace);
+        B.a = ns->a; B.b = ns->b; B.c = ns->c; B.eps = ns->eps;
+        if (dtype == TAG_BF16) run_ns<uint16_t, false, 1>(B, ns->steps, stream);
+        else run_ns<float, false, 2>(B, ns->steps, stream);
+    }
+    return launch_status("tag_orthogonalise");
+}
+
+extern "C" tag_status tag_muon_workspace(const tag_muon_group *groups, int32_t n_groups, size_t *bytes) {
+    clear_error();
+    if (!bytes) TAG_FAIL(TAG_EINVAL, "bytes must be non-NULL");
+    const tag_status st = check_muon_groups(groups, n_groups, false);
+    if (st != TAG_OK) return st;
+    *bytes = workspace_of(groups, n_groups, fill_muon);
+    return TAG_OK;
+}
+
+extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
+                                    const tag_muon_options *options, void *workspace, size_t ws_bytes,
+                                    void *hip_stream) {
+    clear_error();
+    tag_status st = check_muon_groups(groups, n_groups, true);
+    if (st == TAG_OK) st = check_ns(ns);
+    if (st != TAG_OK) return st;
+    if (!options) TAG_FAIL(TAG_EINVAL, "options must be non-NULL");
+    if (!(options->lr >= 0.f) || !std::isfinite(options->lr)) TAG_FAIL(TAG_EINVAL, "lr must be finite and >= 0");
+    if (!(options->momentum >= 0.f && options->momentum < 1.f)) TAG_FAIL(TAG_EINVAL, "momentum must be in [0, 1)");
+    if (!(options->weight_decay >= 0.f) || !std::isfinite(options->weight_decay))
+        TAG_FAIL(TAG_EINVAL, "weight_decay must be finite and >= 0");
+    const size_t need = workspace_of(groups, n_groups, fill_muon);
+    if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_muon_workspace)");
+    if (need && (!workspace || (uintptr_t)workspace % 16))
+        TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    for (int32_t i = 0; i < n_groups; i += kMaxGroups) {
+        NsBatch B{};
+        fill_muon(B, groups + i, std::min(kMaxGroups, n_groups - i));
+        carve_ns(B.g, B.n_groups, workspace);
+        B.a = ns->a; B.b = ns->b; B.c = ns->c; B.eps = ns->eps;
+        B.lr = options->lr; B.momentum = options->momentum; B.decay = options->weight_decay;
+        B.nesterov = options->nesterov != 0;
+        run_ns<float, true, 2>(B, ns->steps, stream);
+    }
+    return launch_status("tag_muon_step");
+}
