@@ -225,24 +225,38 @@ __device__ __forceinline__ void store_frag(uint16_t *hi, uint16_t *lo, int64_t r
     }
 }
 
+// A barrier of the block at which each wavefront has waited for its own direct
+// loads but the last N, and for its LDS reads: LDS that they have filled may be
+// read, LDS that was read may be filled.  (The compiler's own barrier waits for
+// every load in flight.)
+template <int N>
+__device__ __forceinline__ void wait_arrival() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
 // C = R S^T over one tile of T x T outputs per block, R and S operand planes of
-// K/16 fragments per row; four wavefronts of T/2 x T/2.  PARTS = 2: three part
-// products a step, PARTS = 1: the hi planes alone.  The next k-step's fragments
-// are on their way into the other LDS buffer while one is multiplied.
+// K/16 fragments per row.  PARTS = 2: three part products a step, PARTS = 1: the
+// hi planes alone.  Eight wavefronts: four cover the tile (T/2 x T/2 each) for
+// the even fragments of k, four for the odd ones.  Stages of KF fragments of k go
+// through a ring of NB LDS buffers by direct loads, up to NB stages ahead of the
+// products (a stage's products take less time than a load from beyond the L2),
+// and a stage's fragments are read from LDS while the last stage's are
+// multiplied.
 //
 // The matrix cores round their sums towards minus infinity, a bias that grows
-// with the number of steps where rounding errors grow with its root; with
-// PARTS = 2 every other fragment of k is taken with one operand negated, into
-// accumulators of its own, and subtracted at the end, so the two biases cancel.
+// with the number of steps where rounding errors grow with its root; the odd
+// fragments are taken with one operand negated and subtracted at the end, so the
+// two biases cancel.
 template <int T, int PARTS, int MODE, typename OUT>
-__global__ void __launch_bounds__(256) ns_product(NsBatch B) {
-    constexpr int F = T / 32, W = F / 2, kStep = 4 * F * PARTS, NS = PARTS;   // NS accumulator sets
+__global__ void __launch_bounds__(512) ns_product(NsBatch B) {
+    constexpr int F = T / 32, W = F / 2, KF = PARTS == 2 ? 2 : 4, NB = 4;   // (the last stages: cases up to 4)
+    constexpr int kStage = 2 * F * PARTS * KF, L = kStage / 8;   // fragments of a stage, and each wavefront's share
     constexpr bool SYM = MODE == kGram || MODE == kSquare;
-    constexpr int kBytes = 2 * kStep * 1024 > 4 * 32 * 33 * 4 ? 2 * kStep * 1024 : 4 * 32 * 33 * 4;
-    __shared__ __attribute__((aligned(1024))) unsigned char sh[kBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char sh[NB * kStage * 1024];
     int32_t bid = (int32_t)xcd_swizzle(blockIdx.x, gridDim.x);
     const NsGroup &G = B.g[find_group(B, bid)];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kg = wave >> 2, wi = (wave >> 1) & 1, wj = wave & 1;
     const int nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T, tiles = SYM ? nt * (nt + 1) / 2 : nt * mt;
     const int mat = bid / tiles, t = bid % tiles;
     int I, J;
@@ -258,11 +272,11 @@ __global__ void __launch_bounds__(256) ns_product(NsBatch B) {
     }
     const int K = MODE == kGram ? G.mp : G.np, nk = K / 16;
     const int rfR = G.np / 32, rfS = (SYM ? G.np : G.mp) / 32;   // row fragments of R and S
-    // each wavefront's fragments of a step, as pointers to its lanes' 16 bytes
-    const uint16_t *src[kStep / 4];
+    // the wavefront's fragments of a stage, as pointers to its lanes' 16 bytes
+    const uint16_t *src[L];
 #pragma unroll
-    for (int i = 0; i < kStep / 4; ++i) {
-        const int f = wave + 4 * i, side = f / (2 * F * PARTS), plane = f / (2 * F) % PARTS, rf = f / 2 % F, kf = f % 2;
+    for (int i = 0; i < L; ++i) {
+        const int f = wave + 8 * i, side = f / (F * PARTS * KF), plane = f / (F * KF) % PARTS, rf = f / KF % F, kf = f % KF;
         const uint16_t *p;
         if (MODE == kGram) p = x_plane(G, mat, B.cur, 0, plane);
         else if (MODE == kSquare) p = s_plane(G, mat, 0, plane);
@@ -273,68 +287,144 @@ __global__ void __launch_bounds__(256) ns_product(NsBatch B) {
     }
     auto load = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < kStep / 4; ++i) {
-            load_lds<16>(src[i], sh + (buf * kStep + wave + 4 * i) * 1024);
-            src[i] += 2 * kFrag;
+        for (int i = 0; i < L; ++i) {
+            load_lds<16>(src[i], sh + (buf * kStage + wave + 8 * i) * 1024);
+            src[i] += KF * kFrag;
         }
     };
-    f16v acc[NS][W][W];
+    // (one block of accumulators per wavefront: a set for each part product, or for each fragment of a stage, since
+    // consecutive products into one set wait for one another)
+    constexpr int NA = W == 2 ? 1 : PARTS == 2 ? 3 : 2, NK = KF / 2;
+    f16v acc[W][W], more[NA];
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int e = 0; e < 16; ++e) {
 #pragma unroll
-        for (int i = 0; i < W; ++i)
+        for (int i = 0; i < W * W; ++i) acc[i / W][i % W][e] = 0.f;
 #pragma unroll
-            for (int j = 0; j < W; ++j)
+        for (int i = 0; i < NA; ++i) more[i][e] = 0.f;
+    }
+    const unsigned neg = kg ? 0x80008000u : 0u;
+    const int stages = nk / KF;
+    struct Frags {
+        h8 a[NK][W][PARTS], b[NK][W][PARTS];
+    };
+    auto fetch = [&](int s, Frags &f) {
+        const u4v *fr = reinterpret_cast<const u4v *>(sh + (s % NB) * kStage * 1024);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[s][i][j][e] = 0.f;
-    load(0);
-    const int steps = K / 32;
-    for (int s = 0; s < steps; ++s) {
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();   // this step's fragments are there, the last step's reads of the other buffer are done
-        if (s + 1 < steps) load((s + 1) & 1);
-        const h8 *fr = reinterpret_cast<const h8 *>(sh + (s & 1) * kStep * 1024);
-#pragma unroll
-        for (int kf = 0; kf < 2; ++kf) {
-            h8 a[W][PARTS], b[W][PARTS];
+        for (int k = 0; k < NK; ++k)
 #pragma unroll
             for (int i = 0; i < W; ++i)
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
-                    a[i][p] = fr[((p * F + wi * W + i) * 2 + kf) * 64 + lane];
-                    b[i][p] = fr[(((PARTS + p) * F + wj * W + i) * 2 + kf) * 64 + lane];
-                    if (PARTS == 2 && kf == 1) a[i][p] = -a[i][p];
+                    const int kf = 2 * k + kg;
+                    f.a[k][i][p] = __builtin_bit_cast(h8, fr[((p * F + wi * W + i) * KF + kf) * 64 + lane]);
+                    f.b[k][i][p] = __builtin_bit_cast(h8, fr[(((PARTS + p) * F + wj * W + i) * KF + kf) * 64 + lane]);
                 }
-            f16v(&d)[W][W] = acc[PARTS == 2 ? kf : 0];
-            if (PARTS == 2) {
+    };
+    auto multiply = [&](const Frags &f) {
 #pragma unroll
-                for (int i = 0; i < W; ++i)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][PARTS - 1], b[j][0], d[i][j], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < W; ++i)
-#pragma unroll
-                    for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][PARTS - 1], d[i][j], 0, 0, 0);
-            }
+        for (int k = 0; k < NK; ++k) {
+            h8 a[W][PARTS];
 #pragma unroll
             for (int i = 0; i < W; ++i)
 #pragma unroll
-                for (int j = 0; j < W; ++j) d[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][0], b[j][0], d[i][j], 0, 0, 0);
+                for (int p = 0; p < PARTS; ++p)
+                    a[i][p] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, f.a[k][i][p]) ^ neg);
+            auto product = [&](f16v &d, int i, int j, int pa, int pb) {
+                d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][pa], f.b[k][j][pb], d, 0, 0, 0);
+            };
+            if constexpr (W == 1) {
+                if (PARTS == 2) {
+                    product(more[1], 0, 0, PARTS - 1, 0);
+                    product(more[NA - 1], 0, 0, 0, PARTS - 1);
+                }
+                product(PARTS == 2 ? more[0] : more[k % NA], 0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int q = PARTS == 2 ? 0 : 2; q < 3; ++q)
+#pragma unroll
+                    for (int ij = 0; ij < 4; ++ij)
+                        product(acc[ij / 2][ij % 2], ij / 2, ij % 2, q == 0 ? PARTS - 1 : 0, q == 1 ? PARTS - 1 : 0);
+            }
         }
+    };
+#pragma unroll
+    for (int s = 0; s < NB; ++s)
+        if (s < stages) load(s);
+    // While more stages are to be loaded than the ring holds: stage s + 1 has landed for every wavefront (later ones
+    // stay in flight), and every wavefront's reads of stage s are done, so its buffer takes stage s + NB.
+    auto turn_ring = [&](int s, const Frags &now, Frags &next) {
+        wait_arrival<(NB - 2) * L>();
+        load(s % NB);
+        fetch(s + 1, next);
+        __builtin_amdgcn_sched_barrier(0);   // (the reads go out before the products, not between the last of them)
+        multiply(now);
+    };
+    Frags f0, f1;
+    int s = 0;
+    if (stages > NB) {
+        wait_arrival<(NB - 1) * L>();
+        fetch(0, f0);
+        for (; s + 1 + NB < stages; s += 2) {
+            turn_ring(s, f0, f1);
+            turn_ring(s + 1, f1, f0);
+        }
+        if (s + NB < stages) {
+            turn_ring(s, f0, f1);
+            f0 = f1;
+            ++s;
+        }
+        wait_arrival<0>();
+    } else {
+        wait_arrival<0>();
+        fetch(0, f0);
     }
-    __syncthreads();   // the fragments' LDS is free
+    // the last stages are all there
+    switch (stages - s) {
+        case 1: multiply(f0); break;
+        case 2: fetch(s + 1, f1); multiply(f0); multiply(f1); break;
+        case 3: fetch(s + 1, f1); multiply(f0); fetch(s + 2, f0); multiply(f1); multiply(f0); break;
+        default: fetch(s + 1, f1); multiply(f0); fetch(s + 2, f0); multiply(f1); fetch(s + 3, f1); multiply(f0); multiply(f1);
+    }
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][0][e] = PARTS == 2 ? more[0][e] + (more[1][e] + more[NA - 1][e]) : more[0][e] + more[NA - 1][e];
+    }
+    wait_arrival<0>();   // the fragments' LDS is free
+    // the two halves of k meet: each wavefront finishes half of its blocks (T = 64: the even ones finish their one)
+    constexpr int kSend = W == 2 ? 2 : 1, kEnds = W == 2 ? 8 : 4;   // blocks sent, wavefronts that finish
+    float *meet = reinterpret_cast<float *>(sh);
+    if (W == 2 || kg == 1) {
+        float *to = meet + wave % kEnds * kSend * 1024 + lane;
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) to[(j * 16 + e) * 64] = W == 2 ? (kg ? acc[0][j][e] : acc[W - 1][j][e]) : acc[0][0][e];
+    }
+    __syncthreads();
+    if (W == 1 && kg == 1) return;
+    f16v mine[W];
+    {
+        const float *from = meet + (wave ^ 4) % kEnds * kSend * 1024 + lane;
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float o = from[(j * 16 + e) * 64], v = W == 2 && kg ? acc[W - 1][j][e] : acc[0][j][e];
+                mine[j][e] = (kg ? o - v : v - o) * kInvScale;
+            }
+    }
     // lane l of a 32 x 32 block holds column l % 32, rows 8 (e / 4) + 4 (l / 32) + e % 4
-    float *turn = reinterpret_cast<float *>(sh) + wave * 32 * 33;
+    float *turn = meet + kEnds * kSend * 1024 + wave * 32 * 33;   // (past what others may still read)
+    static_assert(kEnds * (kSend * 1024 + 32 * 33) * 4 <= NB * kStage * 1024, "the ring holds both");
     const int half = lane >> 5, col = lane & 31;
 #pragma unroll
-    for (int i = 0; i < W; ++i)
-#pragma unroll
         for (int j = 0; j < W; ++j) {
-            const int fi = I * F + wi * W + i, fj = J * F + wj * W + j;
+            const int fi = I * F + wi * W + kg, fj = J * F + wj * W + j;
             if (fi >= rfR || fj >= rfS || (SYM && fi > fj)) continue;   // (uniform over the wavefront)
             float v[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = (NS == 2 ? acc[0][i][j][e] - acc[NS - 1][i][j][e] : acc[0][i][j][e]) * kInvScale;
+            for (int e = 0; e < 16; ++e) v[e] = mine[j][e];
             if (MODE != kGram) {   // c A A + b A, B X + a X: the term's own order is that of the lane
                 const uint16_t *hi = MODE == kSquare ? s_plane(G, mat, 0, 0) : x_plane(G, mat, B.cur, 1, 0);
                 const uint16_t *lo = MODE == kSquare ? s_plane(G, mat, 0, 1) : x_plane(G, mat, B.cur, 1, 1);
@@ -500,12 +590,12 @@ void launch_product(NsBatch &B, int mode, hipStream_t st) {
         return G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
     });
     switch (mode) {
-        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 256, 0, st>>>(B); break;
-        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 256, 0, st>>>(B); break;
-        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 256, 0, st>>>(B); break;
-        case kFinal: ns_product<T, PARTS, kFinal, OUT><<<grid, 256, 0, st>>>(B); break;
+        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 512, 0, st>>>(B); break;
+        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 512, 0, st>>>(B); break;
+        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 512, 0, st>>>(B); break;
+        case kFinal: ns_product<T, PARTS, kFinal, OUT><<<grid, 512, 0, st>>>(B); break;
         default:
-            if constexpr (sizeof(OUT) == 4) ns_product<T, PARTS, kUpdate, float><<<grid, 256, 0, st>>>(B);
+            if constexpr (sizeof(OUT) == 4) ns_product<T, PARTS, kUpdate, float><<<grid, 512, 0, st>>>(B);
     }
 }
 
