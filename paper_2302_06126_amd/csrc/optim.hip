@@ -207,24 +207,6 @@ __global__ void __launch_bounds__(256) ns_prepare(NsBatch B) {
 // ------------------------------------------------------------------ products
 enum { kGram = 0, kSquare = 1, kApply = 2, kFinal = 3, kUpdate = 4 };
 
-// four consecutive k (k0 + 4 h, h = lane / 32) of row lane % 32 per lane: the
-// half of each 8-k chunk that the lane owns
-__device__ __forceinline__ int64_t frag_at(int64_t rf, int64_t kf, int64_t nk, int g, int lane) {
-    return (rf * nk + kf * 2 + (g >> 1)) * kFrag + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
-}
-__device__ __forceinline__ void store_frag(uint16_t *hi, uint16_t *lo, int64_t rf, int64_t kf, int64_t nk, int lane,
-                                           const float (&v)[16]) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        uint2 h, l;
-        split2(v[4 * g], v[4 * g + 1], h.x, l.x);
-        split2(v[4 * g + 2], v[4 * g + 3], h.y, l.y);
-        const int64_t at = frag_at(rf, kf, nk, g, lane);
-        *reinterpret_cast<uint2 *>(hi + at) = h;
-        *reinterpret_cast<uint2 *>(lo + at) = l;
-    }
-}
-
 // A barrier of the block at which each wavefront has waited for its own direct
 // loads but the last N, and for its LDS reads: LDS that they have filled may be
 // read, LDS that was read may be filled.  (The compiler's own barrier waits for
@@ -355,19 +337,35 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
     // stay in flight), and every wavefront's reads of stage s are done, so its buffer takes stage s + NB.
     auto turn_ring = [&](int s, const Frags &now, Frags &next) {
         wait_arrival<(NB - 2) * L>();
-        load(s % NB);
         fetch(s + 1, next);
-        __builtin_amdgcn_sched_barrier(0);   // (the reads go out before the products, not between the last of them)
+        load(s % NB);
         multiply(now);
+        // the reads go out first, the direct loads between the products
+        constexpr int NM = (W == 2 ? 4 : 1) * NK * (PARTS == 2 ? 3 : 1), M1 = NM / (L + 1);
+        static_assert(L == 2 || L == 4, "two or four direct loads");
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NK * W * PARTS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+        if constexpr (L == 4) {
+            __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, NM - L * M1, 0);
+        __builtin_amdgcn_sched_barrier(0);
     };
     Frags f0, f1;
     int s = 0;
     if (stages > NB) {
         wait_arrival<(NB - 1) * L>();
         fetch(0, f0);
-        for (; s + 1 + NB < stages; s += 2) {
+        for (int pairs = (stages - NB) / 2; pairs > 0; --pairs) {
             turn_ring(s, f0, f1);
             turn_ring(s + 1, f1, f0);
+            s += 2;
         }
         if (s + NB < stages) {
             turn_ring(s, f0, f1);
@@ -390,97 +388,126 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[0][0][e] = PARTS == 2 ? more[0][e] + (more[1][e] + more[NA - 1][e]) : more[0][e] + more[NA - 1][e];
     }
-    wait_arrival<0>();   // the fragments' LDS is free
-    // the two halves of k meet: each wavefront finishes half of its blocks (T = 64: the even ones finish their one)
-    constexpr int kSend = W == 2 ? 2 : 1, kEnds = W == 2 ? 8 : 4;   // blocks sent, wavefronts that finish
-    float *meet = reinterpret_cast<float *>(sh);
-    if (W == 2 || kg == 1) {
-        float *to = meet + wave % kEnds * kSend * 1024 + lane;
+    // What is left goes over the tile in LDS, by pieces of eight consecutive k of a row of the next operand: 64
+    // threads to a fragment.  First in the order of S's rows (the transpose of the tile), with the term of the
+    // iteration itself (c A A + b A, B X + a X), whose operand has that order too and is asked for now.
+    constexpr int P = T + 4, NQ = T * T / 8 / 512, TK = T / 16;
+    static_assert(T * P * 4 <= NB * kStage * 1024, "the ring holds the tile");
+    float *tile = reinterpret_cast<float *>(sh);
+    uint16_t *to[2][2];   // operand written in S's order, in R's; hi, lo
+    const uint16_t *was[2] = {nullptr, nullptr};
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) to[(j * 16 + e) * 64] = W == 2 ? (kg ? acc[0][j][e] : acc[W - 1][j][e]) : acc[0][0][e];
+    for (int pl = 0; pl < 2; ++pl) {
+        if (SYM) to[0][pl] = to[1][pl] = s_plane(G, mat, MODE == kSquare, pl);
+        else { to[0][pl] = x_plane(G, mat, 1 - B.cur, 1, pl); to[1][pl] = x_plane(G, mat, 1 - B.cur, 0, pl); }
+        if (MODE != kGram) was[pl] = MODE == kSquare ? s_plane(G, mat, 0, pl) : x_plane(G, mat, B.cur, 1, pl);
     }
-    __syncthreads();
-    if (W == 1 && kg == 1) return;
-    f16v mine[W];
-    {
-        const float *from = meet + (wave ^ 4) % kEnds * kSend * 1024 + lane;
+    const int prow = (threadIdx.x & 31), pk = 8 * (lane >> 5);   // of a piece, within its fragment
+    auto piece = [&](int q, int &rf, int &kf) {                   // the fragment of a thread's piece
+        const int f = wave + 8 * q;
+        rf = f / TK;
+        kf = f % TK;
+    };
+    u4v old[NQ][2];
+    if (MODE != kGram) {
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float o = from[(j * 16 + e) * 64], v = W == 2 && kg ? acc[W - 1][j][e] : acc[0][j][e];
-                mine[j][e] = (kg ? o - v : v - o) * kInvScale;
-            }
-    }
-    // lane l of a 32 x 32 block holds column l % 32, rows 8 (e / 4) + 4 (l / 32) + e % 4
-    float *turn = meet + kEnds * kSend * 1024 + wave * 32 * 33;   // (past what others may still read)
-    static_assert(kEnds * (kSend * 1024 + 32 * 33) * 4 <= NB * kStage * 1024, "the ring holds both");
-    const int half = lane >> 5, col = lane & 31;
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const int fi = I * F + wi * W + kg, fj = J * F + wj * W + j;
-            if (fi >= rfR || fj >= rfS || (SYM && fi > fj)) continue;   // (uniform over the wavefront)
-            float v[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) v[e] = mine[j][e];
-            if (MODE != kGram) {   // c A A + b A, B X + a X: the term's own order is that of the lane
-                const uint16_t *hi = MODE == kSquare ? s_plane(G, mat, 0, 0) : x_plane(G, mat, B.cur, 1, 0);
-                const uint16_t *lo = MODE == kSquare ? s_plane(G, mat, 0, 1) : x_plane(G, mat, B.cur, 1, 1);
-                const float cv = MODE == kSquare ? B.c : 1.f, ct = MODE == kSquare ? B.b : B.a;
-                const int64_t nkt = G.np / 16;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int64_t at = frag_at(fj, fi, nkt, g, lane);
-                    const uint2 h = *reinterpret_cast<const uint2 *>(hi + at), l = *reinterpret_cast<const uint2 *>(lo + at);
-                    v[4 * g] = fmaf(ct, join2(h.x, l.x, 0), cv * v[4 * g]);
-                    v[4 * g + 1] = fmaf(ct, join2(h.x, l.x, 1), cv * v[4 * g + 1]);
-                    v[4 * g + 2] = fmaf(ct, join2(h.y, l.y, 0), cv * v[4 * g + 2]);
-                    v[4 * g + 3] = fmaf(ct, join2(h.y, l.y, 1), cv * v[4 * g + 3]);
-                }
-            }
-            const bool last = MODE == kFinal || MODE == kUpdate;
-            uint16_t *d0 = nullptr, *d1 = nullptr, *t0 = nullptr, *t1 = nullptr;
-            if (!last) {
-                if (SYM) {
-                    d0 = t0 = s_plane(G, mat, MODE == kSquare, 0);
-                    d1 = t1 = s_plane(G, mat, MODE == kSquare, 1);
-                } else {
-                    d0 = x_plane(G, mat, 1 - B.cur, 1, 0); d1 = x_plane(G, mat, 1 - B.cur, 1, 1);
-                    t0 = x_plane(G, mat, 1 - B.cur, 0, 0); t1 = x_plane(G, mat, 1 - B.cur, 0, 1);
-                }
-                store_frag(d0, d1, fj, fi, G.np / 16, lane, v);
-                if (SYM && fi == fj) continue;
-            }
-            if (!last || G.trans) {   // the other order, through LDS
-#pragma unroll
-                for (int e = 0; e < 16; ++e) turn[(8 * (e >> 2) + 4 * half + (e & 3)) * 33 + col] = v[e];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) v[e] = turn[col * 33 + 8 * (e >> 2) + 4 * half + (e & 3)];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
-            if (!last) {
-                store_frag(t0, t1, fi, fj, (SYM ? G.np : G.mp) / 16, lane, v);
-                continue;
-            }
-            // rows of the result as it is stored: consecutive lanes along them
-            OUT *out = static_cast<OUT *>(G.out.p) + mat * G.out.mat;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int k = 8 * (e >> 2) + 4 * half + (e & 3);
-                const int64_t r = (G.trans ? fj * 32 : fi * 32) + k, c = (G.trans ? fi * 32 : fj * 32) + col;
-                if (r >= G.rows || c >= G.cols) continue;
-                OUT *p = out + r * G.out.row + c;
-                const float o = v[e] * kInvScale;
-                if constexpr (MODE == kUpdate) *p = (1.f - B.lr * B.decay) * *p - B.lr * G.factor * o;
-                else if constexpr (sizeof(OUT) == 2) *p = f2bf(o);
-                else *p = o;
+        for (int q = 0; q < NQ; ++q) {
+            int rf, kf;
+            piece(q, rf, kf);
+            if (J * F + rf < rfS && I * TK + kf < G.np / 16) {
+                const int64_t at = ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8;
+                old[q][0] = *reinterpret_cast<const u4v *>(was[0] + at);
+                old[q][1] = *reinterpret_cast<const u4v *>(was[1] + at);
             }
         }
+    }
+    // the two halves of k meet in the tile: a wavefront puts down the blocks that its counterpart finishes (T = 64:
+    // the odd ones put down theirs).  Lane l of a 32 x 32 block holds column l % 32, rows 8 (e / 4) + 4 (l / 32) + e % 4
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the fragments' LDS is free
+    auto cell = [&](int i, int j, int e) -> float & {
+        return tile[((wi * W + i) * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * P + (wj * W + j) * 32 + (lane & 31)];
+    };
+    if (W == 2 || kg == 1) {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) cell(W == 2 ? 1 - kg : 0, j, e) = W == 2 && !kg ? acc[W - 1][j][e] : acc[0][j][e];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (W == 2 || kg == 0) {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float &c = cell(W == 2 ? kg : 0, j, e);
+                const float o = c, v = W == 2 && kg ? acc[W - 1][j][e] : acc[0][j][e];
+                c = (kg ? o - v : v - o) * kInvScale;
+            }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr bool LAST = MODE == kFinal || MODE == kUpdate;
+    auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8]) {
+        u4v hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            unsigned h, l;
+            split2(v[2 * e], v[2 * e + 1], h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        *reinterpret_cast<u4v *>(d[0] + at) = hi;
+        *reinterpret_cast<u4v *>(d[1] + at) = lo;
+    };
+    {
+        const float cv = MODE == kSquare ? B.c : 1.f, ct = MODE == kSquare ? B.b : B.a;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            int rf, kf;
+            piece(q, rf, kf);
+            if (J * F + rf >= rfS || I * TK + kf >= G.np / 16) continue;
+            float *c = tile + (kf * 16 + pk) * P + rf * 32 + prow, v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = c[e * P];
+                if (MODE != kGram) {
+                    v[e] = fmaf(ct, join2(old[q][0][e / 2], old[q][1][e / 2], e % 2), cv * v[e]);
+                    c[e * P] = v[e];
+                }
+            }
+            if (!LAST) store(to[0], ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8, v);
+        }
+        if (MODE != kGram) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (!LAST) {
+        if (SYM && I == J) return;   // (its own transpose)
+        const int nkR = (SYM ? G.np : G.mp) / 16;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            int rf, kf;
+            piece(q, rf, kf);
+            if (I * F + rf >= rfR || J * TK + kf >= nkR) continue;
+            const float *c = tile + (rf * 32 + prow) * P + kf * 16 + pk;
+            const float4 x = *reinterpret_cast<const float4 *>(c), y = *reinterpret_cast<const float4 *>(c + 4);
+            const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            store(to[1], ((int64_t)(I * F + rf) * nkR + J * TK + kf) * kFrag + lane * 8, v);
+        }
+        return;
+    }
+    // rows of the result as it is stored: consecutive threads along them
+    OUT *out = static_cast<OUT *>(G.out.p) + mat * G.out.mat;
+    const int64_t r0 = (int64_t)(G.trans ? J : I) * T, c0 = (int64_t)(G.trans ? I : J) * T;
+    const int sr = G.trans ? 1 : P, sc = G.trans ? P : 1;
+    const float keep = 1.f - B.lr * B.decay, rate = B.lr * G.factor;
+#pragma unroll 4
+    for (int e = threadIdx.x; e < T * T; e += 512) {
+        const int r = e / T, c = e % T;
+        if (r0 + r >= G.rows || c0 + c >= G.cols) continue;
+        OUT *p = out + (r0 + r) * G.out.row + c0 + c;
+        const float o = tile[r * sr + c * sc] * kInvScale;
+        if constexpr (MODE == kUpdate) *p = keep * *p - rate * o;
+        else if constexpr (sizeof(OUT) == 2) *p = f2bf(o);
+        else *p = o;
+    }
 }
 
 // ---------------------------------------------------------------------- host
