@@ -42,20 +42,23 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 
 constexpr float kScale = 4096.f, kInvScale = 1.f / 4096.f;
-constexpr int kMaxGroups = 16;      // groups of one set of launches
 constexpr int kFrag = 512;          // elements of a fragment
-constexpr int kSumChunk = 8192;     // elements per sum-of-squares block
+constexpr int kSumChunk = 4096;     // elements per sum-of-squares block
+// Groups of one set of launches.  Their tables are kernel arguments, which a
+// launch copies and every block reads from afar: small ones start sooner (15
+// launches of 2.4 KB tables cost 25 us more than of 300 bytes).
+constexpr int kSet = 8, kSetPlain = 16;
 
 struct Arr {
     void *p;
     int64_t row, mat;
 };
 
-struct NsGroup {
+// a group on the host
+struct Group {
     int32_t count, rows, cols;
     int32_t n, m, np, mp;        // n <= m, padded to multiples of 64
-    int32_t trans;               // rows > cols
-    int32_t plain;
+    bool trans, plain;           // rows > cols; no iteration
     int32_t chunks;              // sum-of-squares blocks per matrix
     Arr in, out, mom;            // in / out, or g / w and the momentum
     uint16_t *ops;               // operands of the group's matrices
@@ -64,31 +67,85 @@ struct NsGroup {
     float factor;                // of O(u) in the update
 };
 
-struct NsBatch {
-    NsGroup g[kMaxGroups];
-    int32_t first[kMaxGroups + 1];   // first block of each group
+// what the kernels read of it; first: the group's first block (past the grid for groups that there are not)
+struct NormGroup {
+    Arr in, out, mom;
+    double *part;
+    int32_t rows, cols, chunks, first;
+    int32_t plain, flat;         // flat: four consecutive elements of every array as one access
+};
+struct NormSet {
+    NormGroup g[kSet + kSetPlain];
     int32_t n_groups;
-    float a, b, c, eps;
-    int32_t cur;                 // which of the two X buffers is read
-    // update
     float lr, momentum, decay;
     int32_t nesterov;
 };
+struct PrepGroup {
+    Arr in, mom;
+    const double *part;
+    uint16_t *ops;
+    int64_t ops_stride;
+    int32_t rows, cols, np, mp, chunks, first, flat;
+};
+struct PrepSet {
+    PrepGroup g[kSet];
+    float eps, momentum;
+    int32_t nesterov;
+};
+struct ProductGroup {
+    uint16_t *ops;
+    int64_t ops_stride;
+    int32_t np, mp, first;
+};
+struct ProductSet {
+    ProductGroup g[kSet];
+    float a, b, c;
+    int32_t cur;                 // which of the two X buffers is read
+};
+struct EndGroup {
+    Arr out;
+    int32_t rows, cols;
+    float factor;
+};
+struct SmallGroup {
+    Arr in, out, mom;
+    int32_t rows, cols, mp, first;
+    float factor;
+};
+struct SmallSet {
+    SmallGroup g[kSet];
+    float a, b, c, eps;
+    int32_t steps;
+    float lr, momentum, decay;
+    int32_t nesterov;
+};
+struct EndSet : ProductSet {     // of the last product
+    EndGroup e[kSet];
+    float lr, decay;
+};
 
 // operands of a matrix: X and X^T of both buffers (hi, lo planes), A, B
-__device__ __forceinline__ uint16_t *x_plane(const NsGroup &G, int mat, int buf, int t, int plane) {
-    return G.ops + mat * G.ops_stride + (int64_t)(buf * 4 + t * 2 + plane) * G.np * G.mp;
+template <typename G>
+__device__ __forceinline__ uint16_t *x_plane(const G &g, int mat, int buf, int t, int plane) {
+    return g.ops + mat * g.ops_stride + (int64_t)(buf * 4 + t * 2 + plane) * g.np * g.mp;
 }
-__device__ __forceinline__ uint16_t *s_plane(const NsGroup &G, int mat, int which, int plane) {
-    return G.ops + mat * G.ops_stride + (int64_t)8 * G.np * G.mp + (int64_t)(which * 2 + plane) * G.np * G.np;
+template <typename G>
+__device__ __forceinline__ uint16_t *s_plane(const G &g, int mat, int which, int plane) {
+    return g.ops + mat * g.ops_stride + (int64_t)8 * g.np * g.mp + (int64_t)(which * 2 + plane) * g.np * g.np;
 }
 
-// group of a block, and the block's number within it
-__device__ __forceinline__ int find_group(const NsBatch &B, int32_t &bid) {
-    int g = 0;
-    while (g + 1 < B.n_groups && bid >= B.first[g + 1]) ++g;
-    bid -= B.first[g];
-    return g;
+// group of a block (uniform selects among a few, all read at once)
+template <int N, typename G>
+__device__ __forceinline__ int find_group(const G (&g)[N], int n, int32_t &bid) {
+    int at = 0, first = 0;
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+        const bool in = i < n && bid >= g[i].first;
+        at = in ? i : at;
+        first = in ? g[i].first : first;
+    }
+    bid -= first;
+    return at;
 }
 
 // two parts of 2^12 x
@@ -111,37 +168,77 @@ template <>
 __device__ __forceinline__ float get<uint16_t>(const uint16_t *p) { return bf2f(*p); }
 
 // ------------------------------------------------------- momentum and norms
+// four consecutive elements
+__device__ __forceinline__ float4 get4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 get4(const uint16_t *p) {
+    const uint2 r = *reinterpret_cast<const uint2 *>(p);
+    return float4{__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16),
+                  __uint_as_float(r.y & 0xffff0000u)};
+}
+
 // Sums of squares of u per kSumChunk elements (in 64 bits: a gradient's squares
 // leave the range of fp32), with the momentum update on the way; plain groups
 // are finished here.
 template <typename T, bool MUON>
-__global__ void __launch_bounds__(256) ns_norm(NsBatch B) {
+__global__ void __launch_bounds__(256) ns_norm(NormSet B) {
     __shared__ double red[4];
     int32_t bid = blockIdx.x;
-    const NsGroup &G = B.g[find_group(B, bid)];
+    const NormGroup &G = B.g[find_group(B.g, B.n_groups, bid)];
     const int mat = bid / G.chunks, chunk = bid % G.chunks;
-    const int64_t total = (int64_t)G.rows * G.cols, e0 = (int64_t)chunk * kSumChunk;
-    const int64_t e1 = total < e0 + kSumChunk ? total : e0 + kSumChunk;
     const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
     float *mom = MUON ? static_cast<float *>(G.mom.p) + mat * G.mom.mat : nullptr;
+    float *w = MUON && G.plain ? static_cast<float *>(G.out.p) + mat * G.out.mat : nullptr;
+    const float keep = 1.f - B.lr * B.decay;
+    // the momentum and u of one element, or the whole step of a plain one
+    auto step = [&](float g, float &m, float &wt) {
+        m = fmaf(B.momentum, m, g);
+        const float u = B.nesterov ? fmaf(B.momentum, m, g) : m;
+        wt = keep * wt - B.lr * u;
+        return u;
+    };
     double s = 0.0;
-#pragma unroll 4
-    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
-        const int64_t r = e / G.cols, c = e - r * G.cols;
-        float u = get(in + r * G.in.row + c);
-        if (MUON) {
-            float *mp = mom + r * G.mom.row + c;
-            const float m = B.momentum * *mp + u;
-            *mp = m;
-            u = B.nesterov ? fmaf(B.momentum, m, u) : m;
-            if (G.plain) {
-                float *w = static_cast<float *>(G.out.p) + mat * G.out.mat + r * G.out.row + c;
-                *w = (1.f - B.lr * B.decay) * *w - B.lr * u;
-            }
+    const int64_t total = (int64_t)G.rows * G.cols, e0 = (int64_t)chunk * kSumChunk;
+    constexpr int NV = kSumChunk / 1024;
+    if (G.flat && e0 + kSumChunk <= total) {
+        float4 g[NV], m[NV] = {}, v[NV] = {};
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t e = e0 + 4 * (threadIdx.x + 256 * k);
+            g[k] = get4(in + e);
+            if (MUON) m[k] = get4(mom + e);
+            if (MUON && w) v[k] = get4(w + e);
         }
-        s += (double)u * (double)u;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int64_t e = e0 + 4 * (threadIdx.x + 256 * k);
+            if (MUON) {
+                g[k].x = step(g[k].x, m[k].x, v[k].x); g[k].y = step(g[k].y, m[k].y, v[k].y);
+                g[k].z = step(g[k].z, m[k].z, v[k].z); g[k].w = step(g[k].w, m[k].w, v[k].w);
+                *reinterpret_cast<float4 *>(mom + e) = m[k];
+                if (w) *reinterpret_cast<float4 *>(w + e) = v[k];
+            }
+            s += (double)g[k].x * g[k].x + (double)g[k].y * g[k].y + ((double)g[k].z * g[k].z + (double)g[k].w * g[k].w);
+        }
+    } else {
+        const int64_t e1 = total < e0 + kSumChunk ? total : e0 + kSumChunk;
+#pragma unroll 4
+        for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
+            int64_t r = 0, c = e;
+            if (G.rows > 1) {   // (up to 2^30 elements)
+                r = (uint32_t)e / (uint32_t)G.cols;
+                c = e - r * G.cols;
+            }
+            float u = get(in + r * G.in.row + c);
+            if (MUON) {
+                float *mp = mom + r * G.mom.row + c, m = *mp, wt = w ? w[r * G.out.row + c] : 0.f;
+                u = step(u, m, wt);
+                *mp = m;
+                if (w) w[r * G.out.row + c] = wt;
+            }
+            s += (double)u * (double)u;
+        }
     }
-    if (MUON && G.plain) return;
+    if (MUON && w) return;
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
     __syncthreads();
@@ -149,14 +246,47 @@ __global__ void __launch_bounds__(256) ns_norm(NsBatch B) {
 }
 
 // X and X^T of the first buffer: one block per 64 x 64 tile of the padded
-// matrix, through LDS.
-template <typename T, bool MUON>
-__global__ void __launch_bounds__(256) ns_prepare(NsBatch B) {
-    __shared__ float tile[64][65];   // [row of X][column]
+// matrix (as it is stored), through LDS.  PARTS = 1: X (for A alone) has no lo
+// plane.
+template <typename T, bool MUON, int PARTS>
+__global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
+    __shared__ float tile[64][65];
     __shared__ double red[4];
     int32_t bid = blockIdx.x;
-    const NsGroup &G = B.g[find_group(B, bid)];
-    const int ti = G.np / 64, tj = G.mp / 64, mat = bid / (ti * tj), t = bid % (ti * tj), i0 = t / tj * 64, j0 = t % tj * 64;
+    const PrepGroup &G = B.g[find_group(B.g, kSet, bid)];
+    const bool trans = G.rows > G.cols;
+    const int tr = (trans ? G.mp : G.np) / 64, tc = (trans ? G.np : G.mp) / 64;   // tiles down and along
+    const int mat = bid / (tr * tc), t = bid % (tr * tc), r0 = t / tc * 64, c0 = t % tc * 64;
+    const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
+    const float *mom = MUON ? static_cast<const float *>(G.mom.p) + mat * G.mom.mat : nullptr;
+    // 16 threads to a row of the tile, four columns each
+    const int a = threadIdx.x >> 4, b = (threadIdx.x & 15) * 4;
+    float u[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = r0 + a + 16 * k, c = c0 + b;
+        const T *p = in + (int64_t)r * G.in.row + c;
+        const float *q = MUON ? mom + (int64_t)r * G.mom.row + c : nullptr;
+        float m[4] = {0.f, 0.f, 0.f, 0.f};
+        if (G.flat && r < G.rows && c + 4 <= G.cols) {
+            const float4 x = get4(p);
+            u[k][0] = x.x; u[k][1] = x.y; u[k][2] = x.z; u[k][3] = x.w;
+            if (MUON) {
+                const float4 y = get4(q);
+                m[0] = y.x; m[1] = y.y; m[2] = y.z; m[3] = y.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool is = r < G.rows && c + i < G.cols;
+                u[k][i] = is ? get(p + i) : 0.f;
+                if (MUON) m[i] = is ? q[i] : 0.f;
+            }
+        }
+        if (MUON)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[k][i] = B.nesterov ? fmaf(B.momentum, m[i], u[k][i]) : m[i];
+    }
     double s = 0.0;
     for (int c = threadIdx.x; c < G.chunks; c += 256) s += G.part[(int64_t)mat * G.chunks + c];
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -165,42 +295,33 @@ __global__ void __launch_bounds__(256) ns_prepare(NsBatch B) {
     const double norm = sqrt(red[0] + red[1] + red[2] + red[3]);
     const double scale = (double)kScale / (norm + (double)B.eps);
     const bool bad = !(norm < INFINITY);
-    const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
-    const float *mom = MUON ? static_cast<const float *>(G.mom.p) + mat * G.mom.mat : nullptr;
-    const int a = threadIdx.x & 63;
-    for (int b = threadIdx.x >> 6; b < 64; b += 4) {
-        // consecutive threads along the rows of the matrix as it is stored
-        const int li = G.trans ? a : b, lj = G.trans ? b : a, i = i0 + li, j = j0 + lj;
-        float x = 0.f;
-        if (i < G.n && j < G.m) {
-            const int64_t r = G.trans ? j : i, c = G.trans ? i : j;
-            float u = get(in + r * G.in.row + c);
-            if (MUON) {
-                const float m = mom[r * G.mom.row + c];
-                u = B.nesterov ? fmaf(B.momentum, m, u) : m;
-            }
-            x = bad ? __builtin_nanf("") : (float)((double)u * scale);
-        }
-        tile[li][lj] = x;
-    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            tile[a + 16 * k][b + i] = bad && r0 + a + 16 * k < G.rows && c0 + b + i < G.cols ? __builtin_nanf("")
+                                                                                            : (float)((double)u[k][i] * scale);
     __syncthreads();
-    // 16-byte pieces: 64 rows x 8 chunks of 8 k, for X then X^T
-    for (int p = threadIdx.x; p < 1024; p += 256) {
-        const int tr = p >> 9, r = p & 63, ch = (p >> 6) & 7;
+    // 16-byte pieces: 64 rows x 8 chunks of 8 k, for the stored order and its transpose
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int side = q >> 1, r = threadIdx.x & 63, ch = (threadIdx.x >> 6) + 4 * (q & 1);
         u4v hi, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int k = 8 * ch + 2 * e;
             unsigned h, l;
-            if (tr) split2(tile[k][r], tile[k + 1][r], h, l);
+            if (side) split2(tile[k][r], tile[k + 1][r], h, l);
             else split2(tile[r][k], tile[r][k + 1], h, l);
             hi[e] = h;
             lo[e] = l;
         }
-        const int row = (tr ? j0 : i0) + r, k = (tr ? i0 : j0) + 8 * ch, kf = (tr ? G.np : G.mp) / 16;
+        const int row = (side ? c0 : r0) + r, k = (side ? r0 : c0) + 8 * ch;
+        const bool xt = (side != 0) != trans;   // X has its n <= m rows
+        const int kf = (xt ? G.np : G.mp) / 16;
         const int64_t at = ((int64_t)(row / 32) * kf + k / 16) * kFrag + (row % 32 + 32 * (k / 8 % 2)) * 8;
-        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, tr, 0) + at) = hi;
-        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, tr, 1) + at) = lo;
+        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, xt, 0) + at) = hi;
+        if (PARTS == 2 || xt) *reinterpret_cast<u4v *>(x_plane(G, mat, 0, xt, 1) + at) = lo;
     }
 }
 
@@ -229,14 +350,25 @@ __device__ __forceinline__ void wait_arrival() {
 // with the number of steps where rounding errors grow with its root; the odd
 // fragments are taken with one operand negated and subtracted at the end, so the
 // two biases cancel.
+template <int MODE>
+struct SetOf { typedef ProductSet type; };
+template <>
+struct SetOf<kFinal> { typedef EndSet type; };
+template <>
+struct SetOf<kUpdate> { typedef EndSet type; };
+
 template <int T, int PARTS, int MODE, typename OUT>
-__global__ void __launch_bounds__(512) ns_product(NsBatch B) {
+__global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetOf<MODE>::type B) {
     constexpr int F = T / 32, W = F / 2, KF = PARTS == 2 ? 2 : 4, NB = 4;   // (the last stages: cases up to 4)
     constexpr int kStage = 2 * F * PARTS * KF, L = kStage / 8;   // fragments of a stage, and each wavefront's share
     constexpr bool SYM = MODE == kGram || MODE == kSquare;
     __shared__ __attribute__((aligned(1024))) unsigned char sh[NB * kStage * 1024];
     int32_t bid = (int32_t)xcd_swizzle(blockIdx.x, gridDim.x);
-    const NsGroup &G = B.g[find_group(B, bid)];
+    const int group = find_group(B.g, kSet, bid);
+    ProductGroup G = B.g[0];
+#pragma unroll
+    for (int i = 1; i < kSet; ++i)
+        if (group == i) G = B.g[i];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kg = wave >> 2, wi = (wave >> 1) & 1, wj = wave & 1;
     const int nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T, tiles = SYM ? nt * (nt + 1) / 2 : nt * mt;
@@ -388,6 +520,7 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[0][0][e] = PARTS == 2 ? more[0][e] + (more[1][e] + more[NA - 1][e]) : more[0][e] + more[NA - 1][e];
     }
+    // (PARTS = 1: the lo planes that are read are those of X^T and of A in S's order)
     // What is left goes over the tile in LDS, by pieces of eight consecutive k of a row of the next operand: 64
     // threads to a fragment.  First in the order of S's rows (the transpose of the tile), with the term of the
     // iteration itself (c A A + b A, B X + a X), whose operand has that order too and is asked for now.
@@ -446,7 +579,7 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     constexpr bool LAST = MODE == kFinal || MODE == kUpdate;
-    auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8]) {
+    auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8], bool both) {
         u4v hi, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -456,7 +589,7 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
             lo[e] = l;
         }
         *reinterpret_cast<u4v *>(d[0] + at) = hi;
-        *reinterpret_cast<u4v *>(d[1] + at) = lo;
+        if (both) *reinterpret_cast<u4v *>(d[1] + at) = lo;
     };
     {
         const float cv = MODE == kSquare ? B.c : 1.f, ct = MODE == kSquare ? B.b : B.a;
@@ -474,7 +607,8 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
                     c[e * P] = v[e];
                 }
             }
-            if (!LAST) store(to[0], ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8, v);
+            if (!LAST) store(to[0], ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8, v,
+                             PARTS == 2 || MODE != kSquare);
         }
         if (MODE != kGram) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -489,36 +623,255 @@ __global__ void __launch_bounds__(512) ns_product(NsBatch B) {
             const float *c = tile + (rf * 32 + prow) * P + kf * 16 + pk;
             const float4 x = *reinterpret_cast<const float4 *>(c), y = *reinterpret_cast<const float4 *>(c + 4);
             const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-            store(to[1], ((int64_t)(I * F + rf) * nkR + J * TK + kf) * kFrag + lane * 8, v);
+            store(to[1], ((int64_t)(I * F + rf) * nkR + J * TK + kf) * kFrag + lane * 8, v, PARTS == 2);
         }
         return;
     }
     // rows of the result as it is stored: consecutive threads along them
-    OUT *out = static_cast<OUT *>(G.out.p) + mat * G.out.mat;
-    const int64_t r0 = (int64_t)(G.trans ? J : I) * T, c0 = (int64_t)(G.trans ? I : J) * T;
-    const int sr = G.trans ? 1 : P, sc = G.trans ? P : 1;
-    const float keep = 1.f - B.lr * B.decay, rate = B.lr * G.factor;
+    if constexpr (LAST) {
+        const EndGroup &E = B.e[group];
+        const bool trans = E.rows > E.cols;
+        OUT *out = static_cast<OUT *>(E.out.p) + mat * E.out.mat;
+        const int64_t r0 = (int64_t)(trans ? J : I) * T, c0 = (int64_t)(trans ? I : J) * T;
+        const int sr = trans ? 1 : P, sc = trans ? P : 1;
+        const float keep = 1.f - B.lr * B.decay, rate = B.lr * E.factor;
 #pragma unroll 4
-    for (int e = threadIdx.x; e < T * T; e += 512) {
-        const int r = e / T, c = e % T;
-        if (r0 + r >= G.rows || c0 + c >= G.cols) continue;
-        OUT *p = out + (r0 + r) * G.out.row + c0 + c;
-        const float o = tile[r * sr + c * sc] * kInvScale;
-        if constexpr (MODE == kUpdate) *p = keep * *p - rate * o;
-        else if constexpr (sizeof(OUT) == 2) *p = f2bf(o);
-        else *p = o;
+        for (int e = threadIdx.x; e < T * T; e += 512) {
+            const int r = e / T, c = e % T;
+            if (r0 + r >= E.rows || c0 + c >= E.cols) continue;
+            OUT *p = out + (r0 + r) * E.out.row + c0 + c;
+            const float o = tile[r * sr + c * sc] * kInvScale;
+            if constexpr (MODE == kUpdate) *p = keep * *p - rate * o;
+            else if constexpr (sizeof(OUT) == 2) *p = f2bf(o);
+            else *p = o;
+        }
+    }
+}
+
+// ------------------------------------------------------------- small matrices
+// A matrix of at most 64 by 64 MB: everything in one block, the operands in LDS,
+// one launch instead of 17 (a 64 x 42 matrix: 68 -> 18 us).  Few products, many waits: 16x16x32 instructions
+// (fragments of 16 rows x 32 k, lane l holds 8 consecutive k of row l % 16, k / 8
+// % 4 = l / 16), so that eight wavefronts share the smallest matrix and a block
+// has four values a lane.  What is read is held in registers until every
+// wavefront is through with it, then written over.
+struct Sums {   // of fragments of even and of odd k (one operand negated), of the main and the cross products
+    f4 m[2], x[2];
+    __device__ __forceinline__ Sums() { m[0] = m[1] = x[0] = x[1] = f4{0.f, 0.f, 0.f, 0.f}; }
+    template <int PARTS>
+    __device__ __forceinline__ void add(const h8 (&a)[2], const h8 (&b)[2], int odd) {
+        if (PARTS == 2) {
+            x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1], b[0], x[odd], 0, 0, 0);
+            m[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], m[odd], 0, 0, 0);
+            x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[1], x[odd], 0, 0, 0);
+        } else {
+            m[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], m[odd], 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ f4 total() const { return ((m[0] - m[1]) + (x[0] - x[1])) * kInvScale; }
+};
+
+template <typename T, bool MUON, int PARTS, int MB>
+__global__ void __launch_bounds__(512) ns_small(SmallSet B) {
+    constexpr int kX = 64 * 64 * MB, kA = 64 * 64;   // elements of a plane
+    __shared__ __attribute__((aligned(1024))) uint16_t X[2 * kX], XT[2 * kX], S[2 * kA];
+    __shared__ double red[8];
+    int32_t bid = blockIdx.x;
+    const SmallGroup &G = B.g[find_group(B.g, kSet, bid)];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quad = lane >> 4, col = lane & 15;
+    const bool trans = G.rows > G.cols;
+    const int n = trans ? G.cols : G.rows, m = trans ? G.rows : G.cols, kx = G.mp / 32;   // fragments along a row of X
+    const T *in = static_cast<const T *>(G.in.p) + bid * G.in.mat;
+    float *mom = MUON ? static_cast<float *>(G.mom.p) + bid * G.mom.mat : nullptr;
+    // pieces of eight consecutive j of a row i, 64 threads to a fragment
+    float u[MB][8];
+    double s = 0.0;
+#pragma unroll
+    for (int q = 0; q < MB; ++q) {
+        const int f = wave + 8 * q, i = f / kx * 16 + col, j0 = f % kx * 32 + 8 * quad;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = j0 + e;
+            u[q][e] = 0.f;
+            if (f < 4 * kx && i < n && j < m) {
+                const int64_t r = trans ? j : i, c = trans ? i : j;
+                float g = get(in + r * G.in.row + c);
+                if (MUON) {
+                    float *mp = mom + r * G.mom.row + c;
+                    const float v = fmaf(B.momentum, *mp, g);
+                    *mp = v;
+                    g = B.nesterov ? fmaf(B.momentum, v, g) : v;
+                }
+                u[q][e] = g;
+                s += (double)g * (double)g;
+            }
+        }
+    }
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += red[w];
+    const double norm = sqrt(s), scale = (double)kScale / (norm + (double)B.eps);
+    const bool bad = !(norm < INFINITY);
+#pragma unroll
+    for (int q = 0; q < MB; ++q) {
+        const int f = wave + 8 * q;
+        if (f >= 4 * kx) continue;
+        u4v hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float x0 = (float)((double)u[q][2 * e] * scale), x1 = (float)((double)u[q][2 * e + 1] * scale);
+            if (bad) x0 = x1 = __builtin_nanf("");   // (the padding too: nothing finite is left of such a matrix)
+            unsigned h, l;
+            split2(x0, x1, h, l);
+            hi[e] = h;
+            lo[e] = l;
+        }
+        *reinterpret_cast<u4v *>(X + f * kFrag + lane * 8) = hi;
+        *reinterpret_cast<u4v *>(X + kX + f * kFrag + lane * 8) = lo;
+    }
+    __syncthreads();
+    // X^T: pieces of eight consecutive i of a row j
+#pragma unroll
+    for (int q = 0; q < MB; ++q) {
+        const int f = wave + 8 * q, j = f / 2 * 16 + col, i0 = f % 2 * 32 + 8 * quad;
+        if (f >= 4 * kx) continue;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            u4v v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = i0 + e;
+                const unsigned x = X[p * kX + (i / 16 * kx + j / 32) * kFrag + (i % 16 + 16 * (j / 8 % 4)) * 8 + j % 8];
+                v[e / 2] = e % 2 ? v[e / 2] | x << 16 : x;
+            }
+            *reinterpret_cast<u4v *>(XT + p * kX + f * kFrag + lane * 8) = v;
+        }
+    }
+    __syncthreads();
+    // Lane l of a 16 x 16 block holds column l % 16, rows 4 (l / 16) + 0 .. 3: four consecutive k of a row of the
+    // transpose, half of one of its pieces.  rf: that row's fragment, kb: the block's 16 k.
+    auto at = [&](int rf, int kb, int nk) {
+        const int k = kb * 16 + 4 * quad;
+        return (rf * nk + k / 32) * kFrag + (col + 16 * (k / 8 % 4)) * 8 + k % 8;
+    };
+    auto put = [&](uint16_t *d, int plane, int o, f4 v) {
+        uint2 h, l;
+        split2(v[0], v[1], h.x, l.x);
+        split2(v[2], v[3], h.y, l.y);
+        *reinterpret_cast<uint2 *>(d + o) = h;
+        *reinterpret_cast<uint2 *>(d + plane + o) = l;
+    };
+    auto here = [&](const uint16_t *d, int plane, int o) {   // what stands at a block's place
+        const uint2 h = *reinterpret_cast<const uint2 *>(d + o), l = *reinterpret_cast<const uint2 *>(d + plane + o);
+        return f4{join2(h.x, l.x, 0), join2(h.x, l.x, 1), join2(h.y, l.y, 0), join2(h.y, l.y, 1)};
+    };
+    auto frag = [&](const uint16_t *d, int plane, int f, h8 (&v)[2]) {
+        v[0] = *reinterpret_cast<const h8 *>(d + f * kFrag + lane * 8);
+        if (PARTS == 2) v[1] = *reinterpret_cast<const h8 *>(d + plane + f * kFrag + lane * 8);
+    };
+    auto negated = [&](h8 (&v)[2]) {
+        v[0] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, v[0]) ^ 0x80008000u);
+        if (PARTS == 2) v[1] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, v[1]) ^ 0x80008000u);
+    };
+    const int bi = wave >> 1, bj = wave & 1;   // rows of blocks, and the wavefront's blocks in it: bj, bj + 2, ..
+    // C = R R^T of 64 x 64, R of nk fragments a row
+    auto square = [&](const uint16_t *d, int plane, int nk, f4 (&v)[2]) {
+        Sums c[2];
+        for (int k = 0; k < nk; k += 2) {
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+                h8 a[2], b[2][2];
+                frag(d, plane, bi * nk + k + odd, a);
+                frag(d, plane, bj * nk + k + odd, b[0]);
+                frag(d, plane, (bj + 2) * nk + k + odd, b[1]);
+                if (odd) negated(a);
+                c[0].add<PARTS>(a, b[0], odd);
+                c[1].add<PARTS>(a, b[1], odd);
+            }
+        }
+        v[0] = c[0].total();
+        v[1] = c[1].total();
+    };
+    for (int step = 0; step < B.steps; ++step) {
+        const bool last = step + 1 == B.steps;
+        f4 v[2];
+        square(X, kX, kx, v);   // A = X X^T, every block of it (the two orders of one off the diagonal are two blocks)
+        put(S, kA, at(bj, bi, 2), v[0]);
+        put(S, kA, at(bj + 2, bi, 2), v[1]);
+        __syncthreads();
+        square(S, kA, 2, v);    // B = c A A + b A
+#pragma unroll
+        for (int q = 0; q < 2; ++q) v[q] = B.c * v[q] + B.b * here(S, kA, at(bj + 2 * q, bi, 2));
+        __syncthreads();
+        put(S, kA, at(bj, bi, 2), v[0]);
+        put(S, kA, at(bj + 2, bi, 2), v[1]);
+        __syncthreads();
+        // a X + B X in both orders: rows bi of X, columns bj, bj + 2, ..
+        h8 r[2][2], rn[2];
+        frag(S, kA, bi * 2, r[0]);
+        frag(S, kA, bi * 2 + 1, r[1]);
+        rn[0] = r[1][0];
+        rn[1] = r[1][1];
+        negated(rn);
+        f4 vt[2 * MB], vx[2 * MB];
+#pragma unroll
+        for (int q = 0; q < 2 * MB; ++q) {
+            const int j = bj + 2 * q;
+            if (j >= 2 * kx) continue;
+            h8 x[2][2];
+            frag(XT, kX, j * 2, x[0]);
+            frag(XT, kX, j * 2 + 1, x[1]);
+            Sums t, o;
+            t.add<PARTS>(r[0], x[0], 0);
+            t.add<PARTS>(rn, x[1], 1);
+            vt[q] = t.total() + B.a * here(XT, kX, at(j, bi, 2));
+            if (last) continue;
+            o.add<PARTS>(x[0], r[0], 0);
+            o.add<PARTS>(x[1], rn, 1);
+            vx[q] = o.total() + B.a * here(X, kX, at(bi, j, kx));
+        }
+        __syncthreads();
+        if (!last) {
+#pragma unroll
+            for (int q = 0; q < 2 * MB; ++q) {
+                const int j = bj + 2 * q;
+                if (j >= 2 * kx) continue;
+                put(XT, kX, at(j, bi, 2), vt[q]);
+                put(X, kX, at(bi, j, kx), vx[q]);
+            }
+            __syncthreads();
+            continue;
+        }
+        T *out = static_cast<T *>(G.out.p) + bid * G.out.mat;
+        const float keep = 1.f - B.lr * B.decay, rate = B.lr * G.factor;
+#pragma unroll
+        for (int q = 0; q < 2 * MB; ++q) {
+            const int gj = (bj + 2 * q) * 16 + col;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int gi = bi * 16 + 4 * quad + e;
+                if (gi >= n || gj >= m) continue;
+                T *p = out + (trans ? gj : gi) * G.out.row + (trans ? gi : gj);
+                const float o = vt[q][e] * kInvScale;
+                if constexpr (MUON) *p = keep * *p - rate * o;
+                else if constexpr (sizeof(T) == 2) *p = f2bf(o);
+                else *p = o;
+            }
+        }
     }
 }
 
 // ---------------------------------------------------------------------- host
 int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 
-// workspace of one set of groups, and the pointers into it
-size_t carve_ns(NsGroup *g, int32_t n, void *base) {
+// workspace of one set of matrix groups, and the pointers into it
+size_t carve_ns(Group *g, int32_t n, void *base) {
     Carver c(base);
     for (int i = 0; i < n; ++i) {
-        NsGroup &G = g[i];
-        if (G.plain) continue;
+        Group &G = g[i];
         G.part = c.take<double>((size_t)G.count * G.chunks);
         G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np;
         G.ops = c.take<uint16_t>((size_t)G.count * G.ops_stride);
@@ -526,12 +879,14 @@ size_t carve_ns(NsGroup *g, int32_t n, void *base) {
     return c.used;
 }
 
-void shape_ns(NsGroup *G, int32_t count, int32_t rows, int32_t cols, int32_t plain) {
-    G->count = count; G->rows = rows; G->cols = cols; G->plain = plain;
-    G->trans = rows > cols;
-    G->n = std::min(rows, cols); G->m = std::max(rows, cols);
-    G->np = (int32_t)up64(G->n); G->mp = (int32_t)up64(G->m);
-    G->chunks = (int32_t)(((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
+Group shape_ns(int32_t count, int32_t rows, int32_t cols, bool plain) {
+    Group G{};
+    G.count = count; G.rows = rows; G.cols = cols; G.plain = plain;
+    G.trans = rows > cols;
+    G.n = std::min(rows, cols); G.m = std::max(rows, cols);
+    G.np = (int32_t)up64(G.n); G.mp = (int32_t)up64(G.m);
+    G.chunks = (int32_t)(((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
+    return G;
 }
 
 constexpr int kMaxSide = 32768;   // rows or columns
@@ -599,100 +954,167 @@ tag_status check_ns(const tag_newton_schulz *ns) {
     return TAG_OK;
 }
 
-template <typename Blocks>
-unsigned set_blocks(NsBatch &B, Blocks blocks) {
-    int64_t n = 0;
-    for (int i = 0; i < B.n_groups; ++i) {
-        B.first[i] = (int32_t)n;
-        n += blocks(B.g[i]);
+struct Options {
+    tag_newton_schulz ns;
+    tag_muon_options muon;
+};
+
+// block numbers of a kernel's groups: n of them, the rest past the grid
+template <typename G, typename Blocks>
+unsigned number_blocks(G *g, int32_t n, int32_t room, Blocks blocks) {
+    int64_t first = 0;
+    for (int i = 0; i < room; ++i) {
+        g[i].first = i < n ? (int32_t)first : INT32_MAX;
+        if (i < n) first += blocks(i);
     }
-    B.first[B.n_groups] = (int32_t)n;
-    return (unsigned)n;
+    return (unsigned)first;
+}
+
+bool quads(const Arr &a, size_t el, bool flat, int64_t cols) {   // rows of four-element pieces
+    return (uintptr_t)a.p % (4 * el) == 0 && a.mat % 4 == 0 && (flat ? a.row == cols : a.row % 4 == 0);
+}
+
+int64_t product_tiles(const Group &G, int T, int mode) {
+    const int64_t nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T;
+    return G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
 }
 
 template <int T, int PARTS, typename OUT>
-void launch_product(NsBatch &B, int mode, hipStream_t st) {
-    const unsigned grid = set_blocks(B, [&](const NsGroup &G) -> int64_t {
-        const int64_t nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T;
-        return G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
-    });
+void launch_product(const Group *g, int32_t n, EndSet &B, int mode, hipStream_t st) {
+    const unsigned grid = number_blocks(B.g, n, kSet, [&](int i) { return product_tiles(g[i], T, mode); });
+    const ProductSet &P = B;
     switch (mode) {
-        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 512, 0, st>>>(B); break;
-        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 512, 0, st>>>(B); break;
-        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 512, 0, st>>>(B); break;
+        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 512, 0, st>>>(P); break;
+        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 512, 0, st>>>(P); break;
+        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 512, 0, st>>>(P); break;
         case kFinal: ns_product<T, PARTS, kFinal, OUT><<<grid, 512, 0, st>>>(B); break;
         default:
             if constexpr (sizeof(OUT) == 4) ns_product<T, PARTS, kUpdate, float><<<grid, 512, 0, st>>>(B);
     }
 }
 
-// Tiles of 128 x 128 once they fill the chip, else of 64 x 64.
-template <int PARTS, typename OUT>
-void launch_tiles(NsBatch &B, int mode, hipStream_t st) {
-    int64_t n = 0;
-    for (int i = 0; i < B.n_groups; ++i) {
-        const NsGroup &G = B.g[i];
-        const int64_t nt = (G.np + 127) / 128, mt = (G.mp + 127) / 128;
-        n += G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
-    }
-    if (n >= 128) launch_product<128, PARTS, OUT>(B, mode, st);
-    else launch_product<64, PARTS, OUT>(B, mode, st);
-}
-
+// One set: at most kSet matrix groups (already carved) and kSetPlain plain ones.
 template <typename T, bool MUON, int PARTS>
-void run_ns(NsBatch &all, int steps, hipStream_t st) {
-    unsigned grid = set_blocks(all, [](const NsGroup &G) { return (int64_t)G.count * G.chunks; });
-    ns_norm<T, MUON><<<grid, 256, 0, st>>>(all);
-    NsBatch B = all;   // without the plain groups
-    B.n_groups = 0;
-    for (int i = 0; i < all.n_groups; ++i)
-        if (!all.g[i].plain) B.g[B.n_groups++] = all.g[i];
-    if (B.n_groups == 0) return;
-    grid = set_blocks(B, [](const NsGroup &G) { return (int64_t)G.count * (G.np / 64) * (G.mp / 64); });
-    ns_prepare<T, MUON><<<grid, 256, 0, st>>>(B);
-    for (int s = 0; s < steps; ++s) {
-        B.cur = s & 1;
-        launch_tiles<PARTS, T>(B, kGram, st);
-        launch_tiles<PARTS, T>(B, kSquare, st);
-        launch_tiles<PARTS, T>(B, s + 1 < steps ? kApply : MUON ? kUpdate : kFinal, st);
+void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, const Options &o, hipStream_t st) {
+    NormSet N{};
+    N.lr = o.muon.lr; N.momentum = o.muon.momentum; N.decay = o.muon.weight_decay; N.nesterov = o.muon.nesterov != 0;
+    // matrices of at most 64 x 256 alone: one launch for all of them
+    int32_t wide = 0;
+    for (int i = 0; i < n; ++i) wide = std::max(wide, mats[i].np > 64 ? INT32_MAX : mats[i].mp);
+    const bool small = n > 0 && wide <= 256;
+    const int32_t norms = small ? 0 : n;   // groups that go the way of many launches
+    N.n_groups = norms + n_plain;
+    for (int i = 0; i < N.n_groups; ++i) {
+        const Group &G = i < norms ? mats[i] : plain[i - norms];
+        NormGroup &K = N.g[i];
+        K.in = G.in; K.out = G.out; K.mom = G.mom; K.part = G.part;
+        K.rows = G.rows; K.cols = G.cols; K.chunks = G.chunks; K.plain = G.plain;
+        // (rows one after the other: the elements of a matrix are consecutive)
+        auto flat = [&](const Arr &a, size_t el) { return quads(G.rows > 1 ? a : Arr{a.p, G.cols, a.mat}, el, true, G.cols); };
+        K.flat = flat(G.in, sizeof(T)) && (!MUON || (flat(G.mom, 4) && (!G.plain || flat(G.out, 4))));
     }
-}
-
-Arr arr(const tag_matrices &a) { return Arr{a.base, a.row_stride, a.matrix_stride}; }
-
-void fill_ortho(NsBatch &B, const tag_ortho_group *g, int32_t n) {
-    B.n_groups = n;
+    if (small) {
+        SmallSet S{};
+        S.a = o.ns.a; S.b = o.ns.b; S.c = o.ns.c; S.eps = o.ns.eps; S.steps = o.ns.steps;
+        S.lr = N.lr; S.momentum = N.momentum; S.decay = N.decay; S.nesterov = N.nesterov;
+        for (int i = 0; i < n; ++i) {
+            const Group &G = mats[i];
+            SmallGroup &K = S.g[i];
+            K.in = G.in; K.out = G.out; K.mom = G.mom;
+            K.rows = G.rows; K.cols = G.cols; K.mp = G.mp; K.factor = G.factor;
+        }
+        const unsigned blocks = number_blocks(S.g, n, kSet, [&](int i) { return (int64_t)mats[i].count; });
+        if (wide <= 128) ns_small<T, MUON, PARTS, 2><<<blocks, 512, 0, st>>>(S);
+        else ns_small<T, MUON, PARTS, 4><<<blocks, 512, 0, st>>>(S);
+        if (n_plain == 0) return;
+    }
+    unsigned grid = number_blocks(N.g, N.n_groups, kSet + kSetPlain, [&](int i) {
+        const Group &G = i < norms ? mats[i] : plain[i - norms];
+        return (int64_t)G.count * G.chunks;
+    });
+    ns_norm<T, MUON><<<grid, 256, 0, st>>>(N);
+    if (norms == 0) return;
+    PrepSet P{};
+    P.eps = o.ns.eps; P.momentum = N.momentum; P.nesterov = N.nesterov;
+    EndSet E{};
+    E.a = o.ns.a; E.b = o.ns.b; E.c = o.ns.c; E.lr = o.muon.lr; E.decay = o.muon.weight_decay;
     for (int i = 0; i < n; ++i) {
-        B.g[i] = NsGroup{};
-        shape_ns(&B.g[i], g[i].count, g[i].rows, g[i].cols, 0);
-        B.g[i].in = arr(g[i].in);
-        B.g[i].out = arr(g[i].out);
+        const Group &G = mats[i];
+        PrepGroup &K = P.g[i];
+        K.in = G.in; K.mom = G.mom; K.part = G.part; K.ops = G.ops; K.ops_stride = G.ops_stride;
+        K.rows = G.rows; K.cols = G.cols; K.np = G.np; K.mp = G.mp; K.chunks = G.chunks;
+        K.flat = quads(G.in, sizeof(T), false, G.cols) && (!MUON || quads(G.mom, 4, false, G.cols));
+        E.g[i].ops = G.ops; E.g[i].ops_stride = G.ops_stride; E.g[i].np = G.np; E.g[i].mp = G.mp;
+        E.e[i].out = G.out; E.e[i].rows = G.rows; E.e[i].cols = G.cols; E.e[i].factor = G.factor;
+    }
+    grid = number_blocks(P.g, n, kSet, [&](int i) { return (int64_t)mats[i].count * (mats[i].np / 64) * (mats[i].mp / 64); });
+    ns_prepare<T, MUON, PARTS><<<grid, 256, 0, st>>>(P);
+    // tiles of 128 x 128 once they fill half of the chip, else of 64 x 64
+    auto product = [&](int mode) {
+        int64_t tiles = 0;
+        for (int i = 0; i < n; ++i) tiles += product_tiles(mats[i], 128, mode);
+        if (tiles >= 128) launch_product<128, PARTS, T>(mats, n, E, mode, st);
+        else launch_product<64, PARTS, T>(mats, n, E, mode, st);
+    };
+    for (int s = 0; s < o.ns.steps; ++s) {
+        E.cur = s & 1;
+        product(kGram);
+        product(kSquare);
+        product(s + 1 < o.ns.steps ? kApply : MUON ? kUpdate : kFinal);
     }
 }
 
-void fill_muon(NsBatch &B, const tag_muon_group *g, int32_t n) {
-    B.n_groups = n;
-    for (int i = 0; i < n; ++i) {
-        B.g[i] = NsGroup{};
-        shape_ns(&B.g[i], g[i].count, g[i].rows, g[i].cols, g[i].plain != 0);
-        B.g[i].in = arr(g[i].g);
-        B.g[i].out = arr(g[i].w);
-        B.g[i].mom = arr(g[i].m);
-        B.g[i].factor = (float)std::sqrt(std::max(1.0, (double)g[i].rows / g[i].cols));
+Arr arr(const tag_matrices &a, int32_t count) { return Arr{a.base, a.row_stride, count > 1 ? a.matrix_stride : 0}; }
+
+Group group_of(const tag_ortho_group &g) {
+    Group G = shape_ns(g.count, g.rows, g.cols, false);
+    G.in = arr(g.in, g.count);
+    G.out = arr(g.out, g.count);
+    return G;
+}
+
+Group group_of(const tag_muon_group &g) {
+    Group G = shape_ns(g.count, g.rows, g.cols, g.plain != 0);
+    G.in = arr(g.g, g.count);
+    G.out = arr(g.w, g.count);
+    G.mom = arr(g.m, g.count);
+    G.factor = (float)std::sqrt(std::max(1.0, (double)g.rows / g.cols));
+    return G;
+}
+
+// Goes over the groups by sets, which run one after the other in the same
+// workspace: each(matrix groups, plain groups).
+template <typename G, typename Each>
+void for_sets(const G *g, int32_t n, Each each) {
+    int32_t im = 0, ip = 0;   // next group to be looked at for either
+    while (im < n || ip < n) {
+        Group mats[kSet], plain[kSetPlain];
+        int32_t nm = 0, np = 0;
+        for (; im < n && nm < kSet; ++im) {
+            mats[nm] = group_of(g[im]);
+            nm += !mats[nm].plain;
+        }
+        for (; ip < n && np < kSetPlain; ++ip) {
+            plain[np] = group_of(g[ip]);
+            np += plain[np].plain;
+        }
+        if (nm || np) each(mats, nm, plain, np);
     }
 }
 
-// sets of at most kMaxGroups groups run one after the other in the same workspace
-template <typename Group, typename Fill>
-size_t workspace_of(const Group *g, int32_t n, Fill fill) {
+template <typename G>
+size_t workspace_of(const G *g, int32_t n) {
     size_t most = 0;
-    for (int32_t i = 0; i < n; i += kMaxGroups) {
-        NsBatch B{};
-        const int32_t k = std::min(kMaxGroups, n - i);
-        fill(B, g + i, k);
-        most = std::max(most, carve_ns(B.g, k, nullptr));
-    }
+    for_sets(g, n, [&](Group *mats, int32_t nm, const Group *, int32_t) { most = std::max(most, carve_ns(mats, nm, nullptr)); });
     return most;
+}
+
+template <typename T, bool MUON, int PARTS, typename G>
+void run_groups(const G *g, int32_t n, const Options &o, void *workspace, hipStream_t st) {
+    for_sets(g, n, [&](Group *mats, int32_t nm, const Group *plain, int32_t np) {
+        carve_ns(mats, nm, workspace);
+        run_set<T, MUON, PARTS>(mats, nm, plain, np, o, st);
+    });
 }
 
 tag_status check_ortho_groups(const tag_ortho_group *g, int32_t n, bool arrays, size_t el) {
@@ -730,7 +1152,7 @@ extern "C" tag_status tag_orthogonalise_workspace(const tag_ortho_group *groups,
     if (!bytes) TAG_FAIL(TAG_EINVAL, "bytes must be non-NULL");
     const tag_status st = check_ortho_groups(groups, n_groups, false, 4);
     if (st != TAG_OK) return st;
-    *bytes = workspace_of(groups, n_groups, fill_ortho);
+    *bytes = workspace_of(groups, n_groups);
     return TAG_OK;
 }
 
@@ -742,18 +1164,13 @@ extern "C" tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n
     tag_status st = check_ortho_groups(groups, n_groups, true, dtype == TAG_BF16 ? 2 : 4);
     if (st == TAG_OK) st = check_ns(ns);
     if (st != TAG_OK) return st;
-    if (workspace_of(groups, n_groups, fill_ortho) > ws_bytes)
+    if (workspace_of(groups, n_groups) > ws_bytes)
         TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_orthogonalise_workspace)");
     if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    for (int32_t i = 0; i < n_groups; i += kMaxGroups) {
-        NsBatch B{};
-        fill_ortho(B, groups + i, std::min(kMaxGroups, n_groups - i));
-        carve_ns(B.g, B.n_groups, workspace);
-        B.a = ns->a; B.b = ns->b; B.c = ns->c; B.eps = ns->eps;
-        if (dtype == TAG_BF16) run_ns<uint16_t, false, 1>(B, ns->steps, stream);
-        else run_ns<float, false, 2>(B, ns->steps, stream);
-    }
+    const Options o{*ns, {}};
+    if (dtype == TAG_BF16) run_groups<uint16_t, false, 1>(groups, n_groups, o, workspace, stream);
+    else run_groups<float, false, 2>(groups, n_groups, o, workspace, stream);
     return launch_status("tag_orthogonalise");
 }
 
@@ -762,7 +1179,7 @@ extern "C" tag_status tag_muon_workspace(const tag_muon_group *groups, int32_t n
     if (!bytes) TAG_FAIL(TAG_EINVAL, "bytes must be non-NULL");
     const tag_status st = check_muon_groups(groups, n_groups, false);
     if (st != TAG_OK) return st;
-    *bytes = workspace_of(groups, n_groups, fill_muon);
+    *bytes = workspace_of(groups, n_groups);
     return TAG_OK;
 }
 
@@ -778,19 +1195,10 @@ extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_grou
     if (!(options->momentum >= 0.f && options->momentum < 1.f)) TAG_FAIL(TAG_EINVAL, "momentum must be in [0, 1)");
     if (!(options->weight_decay >= 0.f) || !std::isfinite(options->weight_decay))
         TAG_FAIL(TAG_EINVAL, "weight_decay must be finite and >= 0");
-    const size_t need = workspace_of(groups, n_groups, fill_muon);
+    const size_t need = workspace_of(groups, n_groups);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_muon_workspace)");
     if (need && (!workspace || (uintptr_t)workspace % 16))
         TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    for (int32_t i = 0; i < n_groups; i += kMaxGroups) {
-        NsBatch B{};
-        fill_muon(B, groups + i, std::min(kMaxGroups, n_groups - i));
-        carve_ns(B.g, B.n_groups, workspace);
-        B.a = ns->a; B.b = ns->b; B.c = ns->c; B.eps = ns->eps;
-        B.lr = options->lr; B.momentum = options->momentum; B.decay = options->weight_decay;
-        B.nesterov = options->nesterov != 0;
-        run_ns<float, true, 2>(B, ns->steps, stream);
-    }
+    run_groups<float, true, 2>(groups, n_groups, Options{*ns, *options}, workspace, static_cast<hipStream_t>(hip_stream));
     return launch_status("tag_muon_step");
 }
