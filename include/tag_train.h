@@ -65,6 +65,28 @@ tag_status tag_train_step(const tag_graph *g, const tag_model_dims *dims, const 
                           const tag_grads *grad, float lr, float *loss, void *workspace, size_t ws_bytes,
                           void *hip_stream);
 
+/*
+ * The same step with the balance loss of tag_balance (tag_policy.h) over the
+ * queries' scores added to the cross entropy: the gradients (and the update)
+ * are those of their sum, *loss is the sum.  The graph must hold one topology
+ * (TAG_ESHAPE otherwise), whose devices are those that are balanced; queries
+ * out of range are not counted.  balance->workspace is scratch of
+ * tag_train_balance_workspace bytes beside the step's own.
+ */
+typedef struct tag_train_balance {
+    float coef;                      /* finite, >= 0                                    */
+    float *loss;                     /* DEVICE [1]  the balance part of the loss        */
+    int32_t *count;                  /* DEVICE [S]  queries whose best slice this is    */
+    float *load;                     /* DEVICE [n_dev] load of each device              */
+    void *workspace;
+    size_t ws_bytes;
+} tag_train_balance;
+tag_status tag_train_balance_workspace(int32_t n_slices, int32_t n_query, size_t *bytes);
+tag_status tag_train_step_balanced(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w,
+                                   const tag_features *x, const tag_slices *slices, const tag_train_batch *batch,
+                                   const tag_grads *grad, float lr, const tag_train_balance *balance, float *loss,
+                                   void *workspace, size_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,7 +37,7 @@ SEARCH_EXPORTS = ("tag_search_problem_create", "tag_search_problem_destroy", "ta
 EXPORTS += ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace", "tag_balance")
 
 # include/tag_train.h
-TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step",
+TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step", "tag_train_balance_workspace", "tag_train_step_balanced",
                  # include/tag_optim.h
                  "tag_orthogonalise_workspace", "tag_orthogonalise", "tag_muon_workspace", "tag_muon_step")
 
@@ -103,6 +103,11 @@ class tag_constraints(C.Structure):
     _fields_ = [("allow", _PF), ("allow_stride", C.c_int64), ("bias", _PF), ("bias_stride", C.c_int64),
                 ("history", _PF), ("history_stride", C.c_int64), ("n_history", C.c_int32), ("history_len", _PF),
                 ("repetition", _PF), ("presence", _PF), ("frequency", _PF)]
+
+
+class tag_train_balance(C.Structure):
+    _fields_ = [("coef", C.c_float), ("loss", _PF), ("count", _PF), ("load", _PF), ("workspace", _PF),
+                ("ws_bytes", C.c_size_t)]
 
 
 class tag_newton_schulz(C.Structure):
@@ -226,6 +231,9 @@ def load() -> C.CDLL:
     lib.tag_train_step.argtypes = [vp, C.POINTER(tag_model_dims), C.POINTER(tag_weights), C.POINTER(tag_features),
                                    C.POINTER(tag_slices), C.POINTER(tag_train_batch), C.POINTER(tag_grads),
                                    C.c_float, vp, vp, C.c_size_t, vp]
+    lib.tag_train_balance_workspace.argtypes = [S, S, szp]
+    lib.tag_train_step_balanced.argtypes = lib.tag_train_step.argtypes[:8] + [C.POINTER(tag_train_balance), vp, vp,
+                                                                             C.c_size_t, vp]
     # include/tag_optim.h
     lib.tag_orthogonalise_workspace.argtypes = [C.POINTER(tag_ortho_group), S, szp]
     lib.tag_orthogonalise.argtypes = [C.POINTER(tag_ortho_group), S, S, C.POINTER(tag_newton_schulz), vp, C.c_size_t,

@@ -38,6 +38,7 @@
 // thread per output), so the step is bitwise repeatable.
 #include <algorithm>
 
+#include "../../include/tag_policy.h"
 #include "../../include/tag_train.h"
 #include "agg_common.hpp"
 #include "fwd_internal.hpp"
@@ -1532,6 +1533,7 @@ struct DecTrain {
     float *dT;               // [R n_dev][H]
     float *dopt_part;        // [RG][4][H]
     float *dw2_part;         // [RG][H]
+    float *sc;               // [Q][S] raw scores, wanted for the balance loss (or nullptr)
 };
 
 __device__ __forceinline__ bool dec_query(const DecTrain &A, int32_t q, int32_t *r, int32_t *g, int32_t *op) {
@@ -1587,7 +1589,10 @@ __global__ void __launch_bounds__(256) dec_scores(DecTrain A) {
     const int32_t q = blockIdx.x;
     int32_t r, g, op;
     if (!dec_query(A, q, &r, &g, &op)) {
-        for (int32_t a = tid; a < A.S; a += 256) A.ds[(int64_t)q * A.S + a] = 0.f;
+        for (int32_t a = tid; a < A.S; a += 256) {
+            A.ds[(int64_t)q * A.S + a] = 0.f;
+            if (A.sc) A.sc[(int64_t)q * A.S + a] = -INFINITY;   // (a row that is not counted)
+        }
         if (tid == 0) { A.loss_q[q] = 0.f; A.db2q[q] = 0.f; }
         return;
     }
@@ -1610,6 +1615,7 @@ __global__ void __launch_bounds__(256) dec_scores(DecTrain A) {
         for (; h < H; ++h) s = fmaf(w2s[h], fmaxf(urg[(int64_t)h * A.S + a] + vq[h], 0.f), s);
         s += A.b2[0];
         sc[a] = s;
+        if (A.sc) A.sc[(int64_t)q * A.S + a] = s;
         mx = fmaxf(mx, s);
     }
     red[tid] = mx;
@@ -1819,6 +1825,8 @@ __global__ void __launch_bounds__(256) dec_totals(const float *loss_q, const flo
     }
     if (t == 0) { loss[0] = r1[0]; g_b2[0] = r2[0]; }
 }
+
+__global__ void add_loss(float *loss, const float *part) { loss[0] += part[0]; }
 
 __global__ void fill_zero(float *p, int64_t n) {
     for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) p[i] = 0.f;
@@ -2139,11 +2147,15 @@ extern "C" tag_status tag_train_workspace(const tag_graph *g, const tag_model_di
     return TAG_OK;
 }
 
-extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w,
-                                     const tag_features *x, const tag_slices *slices, const tag_train_batch *batch,
-                                     const tag_grads *gr, float lr, float *loss, void *workspace, size_t ws_bytes,
-                                     void *hip_stream) {
-    clear_error();
+namespace tag {
+namespace {
+
+size_t score_bytes(int32_t S, int32_t Q) { return align_up(sizeof(float) * (size_t)S * Q); }
+
+// balance: nullptr for the cross entropy alone
+tag_status train_run(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w, const tag_features *x,
+                     const tag_slices *slices, const tag_train_batch *batch, const tag_grads *gr, float lr,
+                     const tag_train_balance *balance, float *loss, void *workspace, size_t ws_bytes, void *hip_stream) {
     if (!w || !x || !slices || !batch || !gr || !loss || !workspace)
         TAG_FAIL(TAG_EINVAL, "weights, features, slices, batch, grads, loss and workspace must be non-NULL");
     const int32_t R = x->n_replicas, S = slices->n_slices, Q = batch->n_query;
@@ -2160,6 +2172,17 @@ extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *d
     for (const float *p : gp)
         if (!p) TAG_FAIL(TAG_EINVAL, "gradient arrays must be non-NULL");
     if (!(lr >= 0.f) || lr == INFINITY) TAG_FAIL(TAG_EINVAL, "lr must be finite and >= 0");
+    if (balance) {
+        if (g->G != 1) TAG_FAIL(TAG_ESHAPE, "the balance loss needs a graph of one topology");
+        if (!(balance->coef >= 0.f) || balance->coef == INFINITY) TAG_FAIL(TAG_EINVAL, "coef must be finite and >= 0");
+        if (!balance->loss || !balance->count || !balance->load || !balance->workspace)
+            TAG_FAIL(TAG_EINVAL, "balance loss, count, load and workspace must be non-NULL");
+        if ((uintptr_t)balance->workspace % 16) TAG_FAIL(TAG_EINVAL, "balance workspace must be 16-byte aligned");
+        size_t need = 0;
+        st = tag_train_balance_workspace(S, Q, &need);
+        if (st != TAG_OK) return st;
+        if (need > balance->ws_bytes) TAG_FAIL(TAG_ENOSPACE, "balance workspace too small (see tag_train_balance_workspace)");
+    }
     TrainLayout L;
     if (carve_train(g, dims, R, S, Q, nullptr, &L) > ws_bytes)
         TAG_FAIL(TAG_ENOSPACE, "training workspace too small (see tag_train_workspace)");
@@ -2193,6 +2216,7 @@ extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *d
     D.inv_q = 1.f / (float)Q;
     D.ds = L.ds; D.loss_q = L.loss_q; D.db2q = L.db2q; D.dvq = L.dvq; D.dT = L.dT;
     D.dopt_part = L.dopt_part; D.dw2_part = L.dw2_part;
+    D.sc = balance ? static_cast<float *>(balance->workspace) : nullptr;
     const int din = 2 * F + 4;
     const int64_t RG = (int64_t)R * g->G;
     prof_begin(TAG_STAGE_BWD_DECODER, stream);
@@ -2205,9 +2229,16 @@ extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *d
     dec_scan<<<1, 256, 0, stream>>>(D);
     dec_count<<<grid_for(RG), 256, 0, stream>>>(D, 1);
     dec_scores<<<Q, 256, sizeof(float) * (S + 2 * H), stream>>>(D);
+    if (balance) {   // adds its gradient to ds (that of the output bias stays: the rows of it sum to zero)
+        st = tag_balance(Q, S, TAG_F32, D.sc, S, slices->mask, g->max_dev, nullptr, balance->coef, L.ds, S, 1, balance->loss,
+                         balance->count, balance->load, static_cast<char *>(balance->workspace) + score_bytes(S, Q),
+                         balance->ws_bytes - score_bytes(S, Q), hip_stream);
+        if (st != TAG_OK) return st;
+    }
     fill_zero<<<grid_for((int64_t)Q * H), 256, 0, stream>>>(L.dvq, (int64_t)Q * H);
     dec_grad<<<(unsigned)(RG * ((H + kDecHC - 1) / kDecHC)), 256, 0, stream>>>(D);
     dec_totals<<<1, 256, 0, stream>>>(L.loss_q, L.db2q, Q, loss, gr->dec_b2);
+    if (balance) add_loss<<<1, 1, 0, stream>>>(loss, balance->loss);
     dec_params<<<grid_for(H), 256, 0, stream>>>(D, gr->dec_w1, gr->dec_b1, gr->dec_w2);
     // device side: dE_dev = dT W1_dev, dW1_dev = dT^T E_dev
     launch_gemm(L.dT, H, w->dec_w1, din, rd, F, H, -1, L.G_dev, F, 0, H, true, 1, stream);
@@ -2355,5 +2386,32 @@ extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *d
         sl.lr = lr;
         sgd_update<<<dim3(64, 18), 256, 0, stream>>>(sl);
     }
-    return launch_status("tag_train_step");
+    return launch_status(balance ? "tag_train_step_balanced" : "tag_train_step");
+}
+
+}  // namespace
+}  // namespace tag
+
+extern "C" tag_status tag_train_step(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w,
+                                     const tag_features *x, const tag_slices *slices, const tag_train_batch *batch,
+                                     const tag_grads *gr, float lr, float *loss, void *workspace, size_t ws_bytes,
+                                     void *hip_stream) {
+    clear_error();
+    return train_run(g, dims, w, x, slices, batch, gr, lr, nullptr, loss, workspace, ws_bytes, hip_stream);
+}
+
+extern "C" tag_status tag_train_balance_workspace(int32_t n_slices, int32_t n_query, size_t *bytes) {
+    const tag_status st = tag_balance_workspace(n_query, n_slices, bytes);
+    if (st == TAG_OK) *bytes += score_bytes(n_slices, n_query);
+    return st;
+}
+
+extern "C" tag_status tag_train_step_balanced(const tag_graph *g, const tag_model_dims *dims, const tag_weights *w,
+                                              const tag_features *x, const tag_slices *slices,
+                                              const tag_train_batch *batch, const tag_grads *gr, float lr,
+                                              const tag_train_balance *balance, float *loss, void *workspace,
+                                              size_t ws_bytes, void *hip_stream) {
+    clear_error();
+    if (!balance) TAG_FAIL(TAG_EINVAL, "balance must be non-NULL");
+    return train_run(g, dims, w, x, slices, batch, gr, lr, balance, loss, workspace, ws_bytes, hip_stream);
 }

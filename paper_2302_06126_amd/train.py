@@ -3,6 +3,10 @@ forward pass, the cross entropy between the decoder's priors and target
 distributions over the slice table (Section 4.2.2), every parameter's
 gradient and, when lr > 0, the SGD update of the model's device parameters.
 
+With ``balance`` the step adds the loss that spreads the decisions over the
+devices (include/tag_policy.h).  ``optim.Muon.of(trainer)`` updates the
+parameters from a step's gradients instead of the step's own SGD.
+
 Argument marshalling only; the step runs in libtag.so's HIP kernels.
 """
 from __future__ import annotations
@@ -13,7 +17,7 @@ import numpy as np
 
 from . import Graph, Model, _ptr, _stream, _torch
 from . import _abi
-from ._abi import check, tag_grads, tag_slices, tag_train_batch
+from ._abi import check, tag_grads, tag_slices, tag_train_balance, tag_train_batch
 
 PARAM_NAMES = ("enc_op_w", "enc_op_b", "enc_dev_w", "enc_dev_b", "enc_edge_w0", "enc_edge_b0",
                "enc_edge_w1", "enc_edge_b1", "enc_edge_w2", "enc_edge_b2", "layer_w", "layer_b",
@@ -25,9 +29,14 @@ class Trainer:
 
     Owns the workspace, the gradient tensors (flat fp32, one per parameter
     of ``model``) and the loss.  ``step`` updates ``model``'s parameters in
-    place when lr > 0."""
+    place when lr > 0.
 
-    def __init__(self, graph: Graph, model: Model, n_replicas: int, masks, options, q_rep, q_graph, q_op):
+    ``balance``: coefficient of the balance loss, added to the cross entropy (0:
+    none).  A step then also gives ``balance_loss`` [1] (its part of the loss),
+    ``count`` [S] (queries whose best slice this is) and ``load`` [n_dev]."""
+
+    def __init__(self, graph: Graph, model: Model, n_replicas: int, masks, options, q_rep, q_graph, q_op,
+                 balance: float = 0.0):
         torch = _torch()
         dev = graph.device
         self.graph, self.model, self.R = graph, model, int(n_replicas)
@@ -53,6 +62,16 @@ class Trainer:
         self.grad_struct = g
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.target = torch.zeros((max(self.Q, 1), self.S), dtype=torch.float32, device=dev)
+        self.balance = None
+        if balance != 0.0:
+            check(_abi.load().tag_train_balance_workspace(self.S, self.Q, _abi.C.byref(b)),
+                  "tag_train_balance_workspace")
+            self.balance_ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
+            self.balance_loss = torch.zeros(1, dtype=torch.float32, device=dev)
+            self.count = torch.zeros(self.S, dtype=torch.int32, device=dev)
+            self.load = torch.zeros(graph.info.max_dev, dtype=torch.float32, device=dev)
+            self.balance = tag_train_balance(float(balance), _ptr(self.balance_loss), _ptr(self.count),
+                                             _ptr(self.load), _ptr(self.balance_ws), b.value)
 
     def set_targets(self, target) -> None:
         """Target distributions [Q, S] (host array or device tensor)."""
@@ -64,10 +83,13 @@ class Trainer:
         """One step on the features ``feats`` (a tag_features); returns the
         loss tensor (device, [1]).  Gradients are in ``self.grads``."""
         batch = tag_train_batch(self.Q, _ptr(self.q[0]), _ptr(self.q[1]), _ptr(self.q[2]), _ptr(self.target))
-        st = _abi.load().tag_train_step(self.graph.handle, _abi.C.byref(self.model.dims),
-                                        _abi.C.byref(self.model.weights), _abi.C.byref(feats),
-                                        _abi.C.byref(self.slices), _abi.C.byref(batch),
-                                        _abi.C.byref(self.grad_struct), float(lr), _ptr(self.loss), _ptr(self.ws),
-                                        self.ws_bytes, _stream(stream))
-        check(st, "tag_train_step")
+        args = [self.graph.handle, _abi.C.byref(self.model.dims), _abi.C.byref(self.model.weights),
+                _abi.C.byref(feats), _abi.C.byref(self.slices), _abi.C.byref(batch),
+                _abi.C.byref(self.grad_struct), float(lr)]
+        tail = [_ptr(self.loss), _ptr(self.ws), self.ws_bytes, _stream(stream)]
+        if self.balance is None:
+            check(_abi.load().tag_train_step(*args, *tail), "tag_train_step")
+        else:
+            check(_abi.load().tag_train_step_balanced(*args, _abi.C.byref(self.balance), *tail),
+                  "tag_train_step_balanced")
         return self.loss
