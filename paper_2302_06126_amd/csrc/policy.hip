@@ -62,6 +62,17 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
     const T *xr = static_cast<const T *>(A.x) + q * A.xs;
     float y[VPT], b[VPT];
     uint32_t ok[NV];
+    // the first of the history, whatever its length: it is needed first
+    constexpr int NH = 4;
+    int32_t taken[NH], n_taken = 0;
+    const int32_t *hist = nullptr;
+    if (C.history) {
+        hist = C.history + q * C.history_stride;
+        n_taken = C.n_history;
+        if (C.history_len) n_taken = min(n_taken, max(C.history_len[q], 0));
+#pragma unroll
+        for (int k = 0; k < NH; ++k) taken[k] = tid + NT * k < C.n_history ? hist[tid + NT * k] : -1;
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
         load4<T, VEC>(xr, c0 + 4 * (tid + NT * k), A.S, -INFINITY, *reinterpret_cast<float(*)[4]>(y + 4 * k));
@@ -78,18 +89,20 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
         if (c + 4 > A.S && c < A.S) ok[k] &= (1u << (A.S - c)) - 1u;   // (columns past the end)
     }
     if (C.history) {
-        int32_t n = C.n_history;
-        if (C.history_len) n = min(n, max(C.history_len[q], 0));
         const float rep = C.repetition ? C.repetition[q] : 1.f, pre = C.presence ? C.presence[q] : 0.f,
                     frq = C.frequency ? C.frequency[q] : 0.f;
-        const int32_t *h = C.history + q * C.history_stride;
         const uint32_t span = (uint32_t)min((int64_t)W, A.S - c0);
 #pragma unroll
         for (int k = 0; k < NV; ++k) *reinterpret_cast<int4 *>(cnt + 4 * (tid + NT * k)) = int4{0, 0, 0, 0};
         Team::sync();
-        for (int32_t t = tid; t < n; t += NT) {
-            const int64_t a = (int64_t)h[t] - c0;
-            if (a >= 0 && a < span) atomicAdd(cnt + a, 1);
+        for (int32_t t = tid; t < n_taken; t += NH * NT) {
+#pragma unroll
+            for (int k = 0; k < NH; ++k) {
+                const int64_t a = (int64_t)taken[k] - c0;
+                if (t + NT * k < n_taken && a >= 0 && a < span) atomicAdd(cnt + a, 1);
+            }
+#pragma unroll
+            for (int k = 0; k < NH; ++k) taken[k] = t + NT * (NH + k) < n_taken ? hist[t + NT * (NH + k)] : -1;
         }
         Team::sync();
 #pragma unroll
