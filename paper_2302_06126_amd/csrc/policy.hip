@@ -303,6 +303,7 @@ constexpr int kBalMaxS = 16384;
 constexpr int kBalParts = 256;      // blocks that count decisions
 constexpr int kBalGrad = 4096;      // blocks that walk the rows for their gradients, at most
 constexpr int kBalSpan = 64;        // slices per merging block
+constexpr int kBalInline = 256;     // slices whose h every gradient block forms itself
 
 struct BalArgs {
     int32_t Q, S, M;
@@ -381,6 +382,7 @@ __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
     __shared__ int32_t sub[16][kBalSpan];
     __shared__ uint64_t mask[kBalSpan];
     __shared__ double each[kBalSpan], dev[16][64];   // what a slice gives each of its devices
+    __shared__ int32_t used;
     const int t = threadIdx.x, c = t & 63, g = t >> 6, s = blockIdx.x * kBalSpan + c;
     uint64_t m = 0;
     if (g == 0 && s < A.S) m = A.mask[s] & device_bits(A.M);
@@ -390,11 +392,14 @@ __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
         const int p = g + 16 * i;
         v[i] = s < A.S && p < A.parts ? A.hist[(int64_t)p * A.S + s] : 0;
     }
+    const int32_t mine = blockIdx.x == 0 && t < A.parts ? A.used[t] : 0;
+    if (t == 0) used = 0;
     int32_t n = 0;
 #pragma unroll
     for (int i = 0; i < kBalParts / 16; ++i) n += v[i];
     sub[g][c] = n;
     __syncthreads();
+    if (mine) atomicAdd(&used, mine);
     if (g == 0) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) n += sub[i][c];
@@ -413,17 +418,37 @@ __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
         for (int i = 1; i < 16; ++i) w += dev[i][c];
         A.part[(int64_t)blockIdx.x * 64 + c] = w;
     }
+    if (blockIdx.x == 0 && t == 0) A.total[1] = (double)used;
+}
+
+// Device t's load from the sum of its parts (threads t < 64, one wavefront), and
+// the centre of h: its mean over the decisions taken (the softmax's gradient does
+// not see a shift of h, and what is left of h rounds less).
+__device__ __forceinline__ double device_load(const BalArgs &A, double s, double n, bool write, double *centre) {
+    const int t = threadIdx.x;
+    s = n > 0.0 ? s / n : 0.0;
+    if (write && t < A.M) A.load[t] = (float)s;
+    double c = s * s;
+    for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+    *centre = c;
+    return s;
+}
+// h of a slice less the centre
+__device__ __forceinline__ float share_of(uint64_t mask, const double *load, double centre) {
+    const double pop = (double)__popcll(mask);
+    double w = 0.0;
+    for (; mask; mask &= mask - 1) w += load[__ffsll((unsigned long long)mask) - 1];
+    return (float)((pop > 0.0 ? w / pop : 0.0) - centre);
 }
 
 // Loads from the merging blocks' parts (in their order, by every block), then h of
 // 1,024 slices per block.
 __global__ void __launch_bounds__(1024) bal_shares(BalArgs A) {
     __shared__ double load[64], sub[16][64], centre;
-    __shared__ int32_t used;
     const int t = threadIdx.x, d = t & 63, g = t >> 6, nb = (A.S + kBalSpan - 1) / kBalSpan;
-    const int32_t mine = t < A.parts ? A.used[t] : 0;
     const int32_t slice = blockIdx.x * 1024 + t;
-    uint64_t m = slice < A.S ? A.mask[slice] & device_bits(A.M) : 0;
+    const uint64_t m = slice < A.S ? A.mask[slice] & device_bits(A.M) : 0;
+    const double n = A.total[1];
     double p[kBalMaxS / kBalSpan / 16];
 #pragma unroll
     for (int i = 0; i < kBalMaxS / kBalSpan / 16; ++i) {
@@ -433,29 +458,18 @@ __global__ void __launch_bounds__(1024) bal_shares(BalArgs A) {
     double s = 0.0;
 #pragma unroll
     for (int i = 0; i < kBalMaxS / kBalSpan / 16; ++i) s += p[i];
-    if (t == 0) used = 0;
     sub[g][d] = s;
-    __syncthreads();
-    if (mine) atomicAdd(&used, mine);
     __syncthreads();
     if (t < 64) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) s += sub[i][t];
-        s = used > 0 ? s / (double)used : 0.0;
-        load[t] = s;
-        if (blockIdx.x == 0 && t < A.M) A.load[t] = (float)s;
-        // centre of h: its mean over the decisions taken (the softmax's gradient does not see a shift of h, and
-        // what is left of h rounds less)
-        double c = s * s;
-        for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+        double c;
+        load[t] = device_load(A, s, n, blockIdx.x == 0, &c);
         if (t == 0) centre = c;
-        if (t == 0 && blockIdx.x == 0) { A.total[0] = c; A.total[1] = (double)used; }
+        if (t == 0 && blockIdx.x == 0) A.total[0] = c;
     }
     __syncthreads();
-    const double pop = (double)__popcll(m);
-    double w = 0.0;
-    for (; m; m &= m - 1) w += load[__ffsll((unsigned long long)m) - 1];
-    if (slice < A.S) A.h[slice] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
+    if (slice < A.S) A.h[slice] = share_of(m, load, centre);
 }
 
 // Gradient rows of the block's teams: each thread keeps h of its columns for
@@ -533,8 +547,28 @@ __device__ __forceinline__ float total_loss(const BalArgs &A, double sum, double
 template <typename T, int NT, int VPT, bool VEC>
 __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
     using Team = RowTeam<NT>;
-    __shared__ double lrow[Team::kRows];
-    const double lsum = rows_grad<T, NT, VPT, VEC, Team::kBlock>(A, A.h, row_scale(A, A.total[1]));
+    __shared__ double lrow[Team::kRows], load[64], centre;
+    __shared__ __attribute__((aligned(16))) float hs[kBalInline];
+    const float *h = A.h;
+    if (NT * VPT <= kBalInline) {   // few merging blocks: what bal_shares does, here, without its launch
+        const int t = threadIdx.x, nb = (A.S + kBalSpan - 1) / kBalSpan;
+        const uint64_t m = t < A.S ? A.mask[t] & device_bits(A.M) : 0;
+        if (t < 64) {
+            double p[kBalInline / kBalSpan], s = 0.0, c;
+#pragma unroll
+            for (int b = 0; b < kBalInline / kBalSpan; ++b) p[b] = b < nb ? A.part[(int64_t)b * 64 + t] : 0.0;
+#pragma unroll
+            for (int b = 0; b < kBalInline / kBalSpan; ++b) s += p[b];
+            load[t] = device_load(A, s, A.total[1], blockIdx.x == 0, &c);
+            if (t == 0) centre = c;
+            if (t == 0 && blockIdx.x == 0) A.total[0] = c;
+        }
+        __syncthreads();
+        hs[t] = share_of(m, load, centre);
+        __syncthreads();
+        h = hs;
+    }
+    const double lsum = rows_grad<T, NT, VPT, VEC, Team::kBlock>(A, h, row_scale(A, A.total[1]));
     if (Team::tid() == 0) lrow[Team::row()] = lsum;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -558,9 +592,8 @@ __global__ void __launch_bounds__(1024) bal_small(BalArgs A) {
     const uint64_t m = t < A.S ? A.mask[t] & device_bits(A.M) : 0;
     rows_argmax<T, NT, VPT, VEC>(A, hist);
     const int32_t used = hist[A.S];
-    const double pop = (double)__popcll(m);
     mask[t] = m;
-    each[t] = m ? (double)hist[t] / pop : 0.0;   // (m = 0 past the slices)
+    each[t] = m ? (double)hist[t] / (double)__popcll(m) : 0.0;   // (m = 0 past the slices)
     if (t < A.S) A.count[t] = hist[t];
     __syncthreads();
     double s = 0.0;
@@ -570,17 +603,12 @@ __global__ void __launch_bounds__(1024) bal_small(BalArgs A) {
     if (t < 64) {
 #pragma unroll
         for (int i = 1; i < 16; ++i) s += sub[i][t];
-        s = used > 0 ? s / (double)used : 0.0;
-        load[t] = s;
-        if (t < A.M) A.load[t] = (float)s;
-        double c = s * s;   // (as in bal_shares)
-        for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
+        double c;
+        load[t] = device_load(A, s, (double)used, true, &c);
         if (t == 0) centre = c;
     }
     __syncthreads();
-    double w = 0.0;
-    for (uint64_t r = m; r; r &= r - 1) w += load[__ffsll((unsigned long long)r) - 1];
-    h[t] = (float)((pop > 0.0 ? w / pop : 0.0) - centre);
+    h[t] = share_of(m, load, centre);
     __syncthreads();
     const double lsum = rows_grad<T, NT, VPT, VEC, 1024>(A, h, row_scale(A, (double)used));
     if (Team::tid() == 0) lrow[Team::row()] = lsum;
@@ -628,7 +656,7 @@ void launch_bal(const BalArgs &A, bool vec, hipStream_t st) {
     if (vec) bal_argmax<T, NT, VPT, true><<<A.parts, 1024, lds, st>>>(A);
     else bal_argmax<T, NT, VPT, false><<<A.parts, 1024, lds, st>>>(A);
     bal_count<<<(A.S + kBalSpan - 1) / kBalSpan, 1024, 0, st>>>(A);
-    bal_shares<<<(A.S + 1023) / 1024, 1024, 0, st>>>(A);
+    if (NT * VPT > kBalInline) bal_shares<<<(A.S + 1023) / 1024, 1024, 0, st>>>(A);
     if (vec) bal_grad<T, NT, VPT, true><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
     else bal_grad<T, NT, VPT, false><<<A.lparts, RowTeam<NT>::kBlock, 0, st>>>(A);
     bal_loss<<<1, 1024, 0, st>>>(A);

@@ -17,7 +17,7 @@ from typing import Optional, Sequence, Tuple
 
 from . import _abi, _ptr, _torch
 from ._abi import (C, check, tag_muon_group, tag_muon_options, tag_newton_schulz, tag_ortho_group)
-from .policy import _current, _device, _dtype, _raw_stream
+from .policy import _device, _dtype, _launch, _raw_stream
 
 __all__ = ["Orthogonalise", "orthogonalise", "Muon", "QUINTIC"]
 
@@ -80,10 +80,8 @@ class Orthogonalise:
         for g, s, x, y in zip(self._g, self.shapes, matrices, out):
             _set(getattr(g, "in"), x, "a matrix", s, self.dtype, self.device)
             _set(g.out, y, "an output", s, self.dtype, self.device)
-        with _current(self.device):
-            check(_abi.load().tag_orthogonalise(self._g, len(self.shapes), self._code, C.byref(self._ns),
-                                                _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device)),
-                  "tag_orthogonalise")
+        _launch(self.device, "tag_orthogonalise", self._g, len(self.shapes), self._code, C.byref(self._ns),
+                _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))
         return list(out)
 
 
@@ -145,7 +143,5 @@ class Muon:
         """One step with the gradients as they stand."""
         if lr is not None:
             self.options.lr = float(lr)
-        with _current(self.device):
-            check(_abi.load().tag_muon_step(self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
-                                            _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device)),
-                  "tag_muon_step")
+        _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
+                _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))

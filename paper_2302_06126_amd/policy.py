@@ -13,8 +13,6 @@ other), and each overwrites the outputs of the last.
 """
 from __future__ import annotations
 
-import contextlib
-
 import numpy as np
 
 from . import _abi, _ptr, _torch
@@ -31,10 +29,17 @@ def _device(device):
     return torch.device("cuda", torch.cuda.current_device()) if d.index is None else d
 
 
-def _current(device):
-    """Makes `device` the current one while its kernels are launched."""
+def _launch(device, name: str, *args) -> None:
+    """Calls the library's `name` with `device` as the current one."""
     torch = _torch()
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    f = getattr(_abi.load(), name)
+    if torch._C._cuda_getDevice() == device.index:
+        st = f(*args)
+    else:
+        with torch.cuda.device(device):
+            st = f(*args)
+    if st != _abi.TAG_OK:
+        check(st, name)
 
 
 def _raw_stream(stream, device) -> int:
@@ -52,24 +57,26 @@ def _dtype(dtype) -> int:
 def _rows(t, what, dtypes, device, n_rows, n_cols, shared=False):
     """Row stride of t, [n_rows, n_cols] with unit column stride; with `shared`
     also [n_cols] or [1, n_cols] for every row (stride 0)."""
+    shape = t.shape
     if t.dtype not in dtypes or t.device != device:
         raise ValueError(f"{what} must be {' or '.join(str(d) for d in dtypes)} on {device}")
-    one = shared and (t.dim() == 1 or t.shape[0] == 1)
-    if t.dim() not in ((1, 2) if shared else (2,)) or t.shape[-1] != n_cols or not (one or t.shape[0] == n_rows):
+    one = shared and (len(shape) == 1 or shape[0] == 1)
+    if len(shape) not in ((1, 2) if shared else (2,)) or shape[-1] != n_cols or not (one or shape[0] == n_rows):
         raise ValueError(f"{what} must have the shape [{n_rows}, {n_cols}]" + (" or one row" if shared else "")
-                         + f", not {list(t.shape)}")
-    if n_cols > 1 and t.stride(-1) != 1:
+                         + f", not {list(shape)}")
+    stride = t.stride()
+    if n_cols > 1 and stride[-1] != 1:
         raise ValueError(f"{what} must have unit stride along a row")
     if one:
         return 0
     # (the stride of a single row means nothing)
-    return t.stride(0) if n_rows > 1 else max(t.stride(0), n_cols)
+    return stride[0] if n_rows > 1 else max(stride[0], n_cols)
 
 
 def _vector(t, what, dtype, device, n):
     if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{what} must be {dtype} [{n}] on {device}, contiguous")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 class Constrain:
@@ -95,6 +102,10 @@ class Constrain:
         self.argmax = torch.empty(self.Q, dtype=torch.int32, device=dev)
         self.best = torch.empty(self.Q, dtype=torch.float32, device=dev)
         self._c = tag_constraints()
+        self._byref = C.byref(self._c)
+        self._tail = (_ptr(self.scores), self.S, _ptr(self.prior), self.S, _ptr(self.argmax), _ptr(self.best),
+                      _ptr(self.ws), self.ws_bytes)
+        self._out = (self.prior, self.argmax, self.best) + (() if self.scores is None else (self.scores,))
 
     def __call__(self, scores, allow=None, bias=None, history=None, history_len=None, repetition=None, presence=None,
                  frequency=None, stream=None):
@@ -109,15 +120,15 @@ class Constrain:
         c.n_history = 0
         if allow is not None:
             c.allow_stride = _rows(allow, "allow", (torch.int32, torch.uint32), dev, Q, (S + 31) // 32, True)
-            c.allow = _ptr(allow)
+            c.allow = allow.data_ptr()
         if bias is not None:
             c.bias_stride = _rows(bias, "bias", (f32,), dev, Q, S, True)
-            c.bias = _ptr(bias)
+            c.bias = bias.data_ptr()
         if history is not None:
             T = int(history.shape[-1]) if history.dim() else 0
             c.history_stride = _rows(history, "history", (torch.int32,), dev, Q, T, True)
             if T > 0:
-                c.history, c.n_history = _ptr(history), T
+                c.history, c.n_history = history.data_ptr(), T
             if history_len is not None:
                 c.history_len = _vector(history_len, "history_len", torch.int32, dev, Q)
         elif history_len is not None or repetition is not None or presence is not None or frequency is not None:
@@ -128,12 +139,9 @@ class Constrain:
             c.presence = _vector(presence, "presence", f32, dev, Q)
         if frequency is not None:
             c.frequency = _vector(frequency, "frequency", f32, dev, Q)
-        with _current(dev):
-            check(_abi.load().tag_constrain(Q, S, self._code, _ptr(scores), xs, C.byref(c), _ptr(self.scores), S,
-                                            _ptr(self.prior), S, _ptr(self.argmax), _ptr(self.best), _ptr(self.ws),
-                                            self.ws_bytes, _raw_stream(stream, dev)), "tag_constrain")
-        out = (self.prior, self.argmax, self.best)
-        return out if self.scores is None else out + (self.scores,)
+        _launch(dev, "tag_constrain", Q, S, self._code, scores.data_ptr(), xs, self._byref, *self._tail,
+                _raw_stream(stream, dev))
+        return self._out
 
 
 class Balance:
@@ -157,6 +165,8 @@ class Balance:
         self.loss = torch.empty(1, dtype=torch.float32, device=dev)
         self.count = torch.empty(self.S, dtype=torch.int32, device=dev)
         self.load = torch.empty(self.M, dtype=torch.float32, device=dev)
+        self._tail = (_ptr(self.grad), self.S, 0, _ptr(self.loss), _ptr(self.count), _ptr(self.load), _ptr(self.ws),
+                      self.ws_bytes)
 
     def __call__(self, scores, coef: float = 1e-2, use=None, stream=None):
         """scores [Q, S]; use [Q] (uint8 or bool): 0 leaves a row out."""
@@ -165,9 +175,6 @@ class Balance:
         u = None
         if use is not None:
             u = _vector(use, "use", torch.bool if use.dtype == torch.bool else torch.uint8, self.device, self.Q)
-        with _current(self.device):
-            check(_abi.load().tag_balance(self.Q, self.S, self._code, _ptr(scores), xs, _ptr(self.masks), self.M, u,
-                                          float(coef), _ptr(self.grad), self.S, 0, _ptr(self.loss), _ptr(self.count),
-                                          _ptr(self.load), _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device)),
-                  "tag_balance")
+        _launch(self.device, "tag_balance", self.Q, self.S, self._code, scores.data_ptr(), xs, _ptr(self.masks), self.M,
+                u, float(coef), *self._tail, _raw_stream(stream, self.device))
         return self.loss
