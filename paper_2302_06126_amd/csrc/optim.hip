@@ -369,10 +369,10 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
 #pragma unroll
     for (int i = 1; i < kSet; ++i)
         if (group == i) G = B.g[i];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 7;
     const int kg = wave >> 2, wi = (wave >> 1) & 1, wj = wave & 1;
     const int nt = (G.np + T - 1) / T, mt = (G.mp + T - 1) / T, tiles = SYM ? nt * (nt + 1) / 2 : nt * mt;
-    const int mat = bid / tiles, t = bid % tiles;
+    const int mat = bid / tiles, t = bid - mat * tiles;
     int I, J;
     if (SYM) {   // I <= J, in the order of J
         J = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
@@ -380,9 +380,9 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         while ((J + 1) * (J + 2) / 2 <= t) ++J;
         I = t - J * (J + 1) / 2;
     } else {     // strips of eight rows of tiles
-        const int strip = t / (8 * mt), h = min(8, nt - 8 * strip), r = t - strip * 8 * mt;
-        I = 8 * strip + r % h;
-        J = r / h;
+        const int strip = nt <= 8 ? 0 : t / (8 * mt), h = min(8, nt - 8 * strip), r = t - strip * 8 * mt;
+        J = h == 8 ? r >> 3 : r / h;
+        I = 8 * strip + r - J * h;
     }
     const int K = MODE == kGram ? G.mp : G.np, nk = K / 16;
     const int rfR = G.np / 32, rfS = (SYM ? G.np : G.mp) / 32;   // row fragments of R and S
@@ -390,7 +390,9 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
     const uint16_t *src[L];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-        const int f = wave + 8 * i, side = f / (F * PARTS * KF), plane = f / (F * KF) % PARTS, rf = f / KF % F, kf = f % KF;
+        // (plain shifts of wave, and constants where its eight fragments are of one kind)
+        const int side = i / (L / 2), f = wave + 8 * (i % (L / 2));
+        const int plane = F * KF == 8 ? i % (L / 2) : f / (F * KF), rf = f % (F * KF) / KF, kf = f % KF;
         const uint16_t *p;
         if (MODE == kGram) p = x_plane(G, mat, B.cur, 0, plane);
         else if (MODE == kSquare) p = s_plane(G, mat, 0, plane);
