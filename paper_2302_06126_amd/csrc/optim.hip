@@ -1051,11 +1051,14 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
     }
     grid = number_blocks(P.g, n, kSet, [&](int i) { return (int64_t)mats[i].count * (mats[i].np / 64) * (mats[i].mp / 64); });
     ns_prepare<T, MUON, PARTS><<<grid, 256, 0, st>>>(P);
-    // tiles of 128 x 128 once they fill half of the chip, else of 64 x 64
+    // Tiles of 128 x 128 once more than half of the CUs get one, else of 64 x 64.  Always the smaller | from 64 of the
+    // larger ones | above 128, us, fp32 (the larger take fewer bytes per product, the smaller spread further): 2 of
+    // 1024 x 1024 281 | 372 | 281, 8 of 512 x 512 195 | 255 | 195, 40 of 256 x 256 178 | 207 | 175, 1500 x 1500 416 |
+    // 488 | 412, 2048 x 2048 755 | 703 | 704.
     auto product = [&](int mode) {
         int64_t tiles = 0;
         for (int i = 0; i < n; ++i) tiles += product_tiles(mats[i], 128, mode);
-        if (tiles >= 128) launch_product<128, PARTS, T>(mats, n, E, mode, st);
+        if (tiles > 128) launch_product<128, PARTS, T>(mats, n, E, mode, st);
         else launch_product<64, PARTS, T>(mats, n, E, mode, st);
     };
     for (int s = 0; s < o.ns.steps; ++s) {
