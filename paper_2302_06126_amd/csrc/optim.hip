@@ -224,8 +224,8 @@ __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
 #pragma unroll 4
         for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
             int64_t r = 0, c = e;
-            if (G.rows > 1) {   // (up to 2^30 elements)
-                r = (uint32_t)e / (uint32_t)G.cols;
+            if (G.rows > 1) {
+                r = total < ((int64_t)1 << 32) ? (uint32_t)e / (uint32_t)G.cols : e / G.cols;
                 c = e - r * G.cols;
             }
             float u = get(in + r * G.in.row + c);
