@@ -182,7 +182,11 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) con_rows(ConArgs A) {
     }
 }
 
-constexpr int64_t kConWhole = 8192;   // longest row that one block keeps in registers
+// Longest row that one block keeps in registers; longer ones go by parts, in two
+// launches that both read the scores.  Whole | by parts, us: 1 x 8,000 7.4 | 11.5,
+// 2,000 x 8,000 27 | 46, 1 x 16,000 9.5 | 11.1, 500 x 16,000 19 | 28, 1,500 x 10,000
+// 41 | 46.
+constexpr int64_t kConWhole = 16384;
 constexpr int kConPart = 4096;        // columns of a part of a longer one
 
 template <typename T, int NT, int VPT, int PASS>
@@ -194,13 +198,18 @@ void launch_con_pass(const ConArgs &A, bool vec, int64_t items, hipStream_t st) 
     else con_rows<T, NT, VPT, false, PASS><<<grid, Team::kBlock, lds, st>>>(A);
 }
 
+// Threads per row: 16 columns each (a wavefront takes four rows of up to 256, whose
+// reductions cost it one), more threads only where those do not hold the row.
+// 2,000 x 4,000 by 256 threads 14.5 us, by 1,024 34; 10,000 x 1,000 by 64 19, by 256 23;
+// 42,496 x 256 by 16 36.9, by 64 36.2.
 template <typename T>
 void launch_constrain(const ConArgs &A, bool vec, hipStream_t st) {
     if (A.S <= 64) launch_con_pass<T, 16, 4, kWhole>(A, vec, A.Q, st);
     else if (A.S <= 256) launch_con_pass<T, 16, 16, kWhole>(A, vec, A.Q, st);
     else if (A.S <= 1024) launch_con_pass<T, 64, 16, kWhole>(A, vec, A.Q, st);
     else if (A.S <= 4096) launch_con_pass<T, 256, 16, kWhole>(A, vec, A.Q, st);
-    else if (A.S <= kConWhole) launch_con_pass<T, 512, 16, kWhole>(A, vec, A.Q, st);
+    else if (A.S <= 8192) launch_con_pass<T, 512, 16, kWhole>(A, vec, A.Q, st);
+    else if (A.S <= kConWhole) launch_con_pass<T, 1024, 16, kWhole>(A, vec, A.Q, st);
     else {
         launch_con_pass<T, 256, kConPart / 256, kPart>(A, vec, (int64_t)A.Q * A.chunks, st);
         launch_con_pass<T, 256, kConPart / 256, kFinish>(A, vec, (int64_t)A.Q * A.chunks, st);
@@ -579,8 +588,12 @@ __global__ void __launch_bounds__(RowTeam<NT>::kBlock) bal_grad(BalArgs A) {
 }
 
 // Few rows: everything in one block, the scores' second reading from its cache.
+// Its time grows with the turns that its teams take over the rows, that of the
+// other way is four launches or five; this | those, us: 64 x 60 (a turn) 6.5 | 16.0,
+// 256 x 60 (four) 10.8 | 16.5, 512 x 60 17.2 | 16.4; 64 x 256 (a turn) 10.1 | 17.0,
+// 256 x 256 (four) 21.0 | 18.0; 16 x 1,000 (a turn) 14.8 | 21.9, 64 x 1,000 26.9 | 22.2.
 constexpr int kBalSmallS = 1024;   // slices whose masks it keeps in LDS
-constexpr int kBalSmallTurns = 8;  // turns that its teams take over the rows, at most
+constexpr int bal_small_turns(int vpt) { return vpt == 4 ? 6 : 2; }
 template <typename T, int NT, int VPT, bool VEC>
 __global__ void __launch_bounds__(1024) bal_small(BalArgs A) {
     using Team = RowTeam<NT, 1024>;
@@ -646,7 +659,7 @@ __global__ void __launch_bounds__(1024) bal_loss(BalArgs A) {
 template <typename T, int NT, int VPT>
 void launch_bal(const BalArgs &A, bool vec, hipStream_t st) {
     if constexpr (NT <= 64) {
-        if (A.Q <= kBalSmallTurns * (1024 / NT)) {
+        if (A.Q <= bal_small_turns(VPT) * (1024 / NT)) {
             if (vec) bal_small<T, NT, VPT, true><<<1, 1024, 0, st>>>(A);
             else bal_small<T, NT, VPT, false><<<1, 1024, 0, st>>>(A);
             return;

@@ -21,7 +21,7 @@ from tests import _policy as R
 pytestmark = pytest.mark.gpu
 
 SIZES = [1, 2, 3, 31, 32, 33, 60, 64, 65, 101, 255, 256, 257, 1000, 1024, 1025, 4095, 4096, 4097, 8191, 8192, 8193,
-         12288, 20003, 70001]
+         12288, 16383, 16384, 16385, 20003, 70001]
 
 
 @pytest.fixture(scope="module")
@@ -112,7 +112,7 @@ def test_constrain_sizes(torch, S, dtype):
         _compare(torch, case, case.run())
 
 
-@pytest.mark.parametrize("S", [60, 300, 9001])
+@pytest.mark.parametrize("S", [60, 300, 9001, 20001])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_constrain_what_stands_in_masked_places(torch, S, dtype):
     _say(f"[constrain] masked places S={S} {dtype}")
@@ -138,7 +138,7 @@ def test_constrain_what_stands_in_masked_places(torch, S, dtype):
     assert np.isfinite(out[0][1]).all() and out[0][1].max() == 1.0
 
 
-@pytest.mark.parametrize("S", [50, 700, 5000, 10000])
+@pytest.mark.parametrize("S", [50, 700, 5000, 10000, 20000])
 def test_constrain_nan_and_infinity_where_allowed(torch, S):
     from paper_2302_06126_amd.policy import Constrain
     x = np.random.default_rng(S).normal(0, 1, (5, S)).astype(np.float32)
@@ -165,7 +165,7 @@ def test_constrain_ties_go_to_the_lowest_slice(torch):
         assert at.tolist() == [0, S // 2, S // 3], S
 
 
-@pytest.mark.parametrize("S", [60, 500, 4500, 9000])
+@pytest.mark.parametrize("S", [60, 500, 4500, 9000, 20000])
 def test_constrain_history_edges(torch, S):
     """Ids out of range, lengths of zero, below zero and above the rows, the same
     id throughout, a history longer than the row."""
@@ -192,7 +192,7 @@ def test_constrain_history_edges(torch, S):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("S", [37, 256, 1500, 8195])
+@pytest.mark.parametrize("S", [37, 256, 1500, 8195, 20001])
 def test_constrain_rows_anywhere(torch, S, dtype):
     """Rows of a wider tensor that start at odd elements: the same bits."""
     case = _Case(S + 7, 9, S, dtype)
@@ -209,7 +209,7 @@ def test_constrain_in_place_and_rows_behind_the_last(torch):
     from paper_2302_06126_amd._abi import check, tag_constraints
     lib = P._abi.load()
     for S, dtype in ((60, torch.float32), (256, torch.bfloat16), (3000, torch.float32), (8500, torch.bfloat16),
-                     (9000, torch.float32)):
+                     (9000, torch.float32), (20000, torch.float32), (20001, torch.bfloat16)):
         case = _Case(S, 5, S, "bf16" if dtype == torch.bfloat16 else "f32")
         x = torch.full((8, S + 4), 9.0, dtype=dtype, device="cuda")
         x[:5, :S] = case.t.cuda()
@@ -386,7 +386,7 @@ def test_side_streams_and_captured_graphs(torch):
     from paper_2302_06126_amd.policy import Balance, Constrain
     s = torch.cuda.Stream()
     objs = []
-    for S, Q in ((256, 300), (9000, 5)):
+    for S, Q in ((256, 300), (9000, 5), (20000, 7)):
         t, masks, _ = _bal_case(S, Q, S, 8, "f32", torch)
         S_b = min(S, 256)
         x = t.cuda()
