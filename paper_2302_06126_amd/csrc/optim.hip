@@ -178,7 +178,8 @@ __device__ __forceinline__ float4 get4(const uint16_t *p) {
 
 // Sums of squares of u per kSumChunk elements (in 64 bits: a gradient's squares
 // leave the range of fp32), with the momentum update on the way; plain groups
-// are finished here.
+// are finished here.  Memory bounds it: 2048 x 2048 fp32 5.7 us (2.9 TB/s, a launch
+// and its tail), 1.7 M parameters of the 256-wide model 11.7 us.
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
     __shared__ double red[4];
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
 
 // X and X^T of the first buffer: one block per 64 x 64 tile of the padded
 // matrix (as it is stored), through LDS.  PARTS = 1: X (for A alone) has no lo
-// plane.
+// plane.  Memory bounds it: 2048 x 2048 fp32 12.6 us (17 MB read, 34 MB written).
 template <typename T, bool MUON, int PARTS>
 __global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
     __shared__ float tile[64][65];
@@ -345,6 +346,16 @@ __device__ __forceinline__ void wait_arrival() {
 // products (a stage's products take less time than a load from beyond the L2),
 // and a stage's fragments are read from LDS while the last stage's are
 // multiplied.
+//
+// 2048^3, PARTS = 2: B X 54 us (256 tiles, 950 TFLOP/s of fp16 products; a library's
+// bf16 product of 2048^3 reaches 418, of 8192^3 1,164), of which 43 us of products
+// at the 1.6 GHz that the chip then holds, 70% of their peak at it; X X^T and A A
+// 43 us (136 tiles, half of the CUs, a higher clock).  Around the products a launch
+// takes 2 us to the first load, 1 until it lands, 2 to join the halves of k, 4 to write
+// 34 MB.  PARTS = 1, four of 1024 x 4096: B X 63 us, bound by memory (100 MB written,
+// 67 MB of X read again).  Tried without gain: two stages of twice the length instead
+// of four, stages' barriers by the compiler (which waits for every load), one
+// wavefront per SIMD (the products wait for LDS: 60 us).
 //
 // The matrix cores round their sums towards minus infinity, a bias that grows
 // with the number of steps where rounding errors grow with its root; the odd
