@@ -45,7 +45,7 @@ typedef struct tag_matrices {
 } tag_matrices;
 
 typedef struct tag_ortho_group {
-    int32_t count, rows, cols;
+    int32_t count, rows, cols;     /* sides up to 32768, at most 2^19 tiles of 64 x 64 in all */
     tag_matrices in, out;          /* out may be in; otherwise written arrays do not overlap */
 } tag_ortho_group;
 
@@ -69,10 +69,10 @@ tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n_groups, in
  *   w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) O(u)
  * with O the iteration above; for a group with plain != 0 (biases, vectors:
  * give them as one row) O(u) = u with factor 1.  w, g and m are three
- * different arrays.
+ * different arrays, and no w or m is part of another group.
  */
 typedef struct tag_muon_group {
-    int32_t count, rows, cols, plain;
+    int32_t count, rows, cols, plain;   /* as above; plain: up to 2^31 elements */
     tag_matrices w, g, m;          /* w and m written, g read */
 } tag_muon_group;
 

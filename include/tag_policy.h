@@ -37,7 +37,8 @@ tag_status tag_gnn_scores(const tag_graph *g, const tag_model_dims *dims, const 
  *   bias         added to the scores (NULL: none); -inf forbids too
  *   history      rows of n_history slice ids the query took before, of which
  *                the first history_len[q] count (NULL: all n_history; values
- *                are clamped to [0, n_history]); ids outside [0, S) are ignored
+ *                are clamped to [0, n_history], which is at most 2^30); ids
+ *                outside [0, S) are ignored
  *   repetition   [Q] divides a taken slice's positive score and multiplies a
  *                negative one (NULL: 1)
  *   presence     [Q] subtracted from a taken slice's score (NULL: 0)

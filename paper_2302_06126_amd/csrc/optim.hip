@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
         for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
             int64_t r = 0, c = e;
             if (G.rows > 1) {
-                r = total < ((int64_t)1 << 32) ? (uint32_t)e / (uint32_t)G.cols : e / G.cols;
+                r = (uint32_t)e / (uint32_t)G.cols;   // (at most 2^31 elements)
                 c = e - r * G.cols;
             }
             float u = get(in + r * G.in.row + c);
@@ -907,9 +907,9 @@ constexpr int kMaxSide = 32768;   // rows or columns
 tag_status check_shape(int32_t count, int32_t rows, int32_t cols, bool plain) {
     if (count < 1 || rows < 1 || cols < 1) TAG_FAIL(TAG_EINVAL, "need count, rows and cols >= 1");
     if (!plain && (rows > kMaxSide || cols > kMaxSide)) TAG_FAIL(TAG_ESHAPE, "at most 32768 rows or columns");
-    // (blocks are counted in 32 bits)
+    // (a launch has fewer than 2^32 threads, over all groups of its set)
     const int64_t blocks = std::max((up64(rows) / 64) * (up64(cols) / 64), ((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
-    if (blocks * count > (1 << 26)) TAG_FAIL(TAG_ESHAPE, "too many or too large matrices in a group");
+    if (blocks * count > (1 << 19)) TAG_FAIL(TAG_ESHAPE, "too many or too large matrices in a group");
     return TAG_OK;
 }
 

@@ -270,10 +270,12 @@ extern "C" tag_status tag_constrain(int32_t n_query, int32_t n_slices, int32_t d
     if ((c.allow && c.allow_stride != 0 && c.allow_stride < words) || (c.bias && c.bias_stride != 0 && c.bias_stride < S))
         TAG_FAIL(TAG_EINVAL, "allow_stride and bias_stride must be 0 or cover a row");
     if (c.n_history < 0 || (c.n_history > 0 && !c.history)) TAG_FAIL(TAG_EINVAL, "n_history needs a history");
+    if (c.n_history > (1 << 30)) TAG_FAIL(TAG_ESHAPE, "at most 2^30 history entries");
     if (c.history && c.history_stride != 0 && c.history_stride < c.n_history)
         TAG_FAIL(TAG_EINVAL, "history_stride must be 0 or cover a row");
     if (!aligned(scores, el) || !aligned(constrained, el) || !aligned(prior, 4) || !aligned(c.bias, 4) ||
-        !aligned(c.allow, 4) || !aligned(c.history, 4))
+        !aligned(c.allow, 4) || !aligned(c.history, 4) || !aligned(c.history_len, 4) || !aligned(c.repetition, 4) ||
+        !aligned(c.presence, 4) || !aligned(c.frequency, 4) || !aligned(argmax, 4) || !aligned(best, 4))
         TAG_FAIL(TAG_EINVAL, "an array is not aligned to its elements");
     if (constrained && constrained == scores ? constrained_stride != score_stride
                                              : Span(constrained, n_query, S, constrained_stride, el)
@@ -291,7 +293,9 @@ extern "C" tag_status tag_constrain(int32_t n_query, int32_t n_slices, int32_t d
     A.prior = prior; A.ps = prior_stride;
     A.argmax = argmax; A.best = best;
     A.chunks = (int32_t)std::max<int64_t>(1, con_chunks(n_slices));
-    if ((int64_t)n_query * A.chunks > INT32_MAX) TAG_FAIL(TAG_ESHAPE, "too many rows of this length");
+    // (a launch has fewer than 2^32 threads)
+    const int64_t team = S <= 256 ? 16 : S <= 1024 ? 64 : S <= 4096 || S > kConWhole ? 256 : S <= 8192 ? 512 : 1024;
+    if ((int64_t)n_query * A.chunks >= ((int64_t)1 << 32) / team) TAG_FAIL(TAG_ESHAPE, "too many rows of this length");
     size_t need = 0;
     tag_constrain_workspace(n_query, n_slices, &need);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_constrain_workspace)");
@@ -743,7 +747,8 @@ extern "C" tag_status tag_balance(int32_t n_query, int32_t n_slices, int32_t dty
         TAG_FAIL(TAG_EINVAL, "a row stride is below the number of slices");
     if (accumulate && dtype != TAG_F32) TAG_FAIL(TAG_EINVAL, "accumulate needs TAG_F32");
     const size_t el = dtype == TAG_BF16 ? 2 : 4;
-    if (!aligned(scores, el) || !aligned(grad, el) || !aligned(mask, 8))
+    if (!aligned(scores, el) || !aligned(grad, el) || !aligned(mask, 8) || !aligned(loss, 4) || !aligned(count, 4) ||
+        !aligned(load, 4))
         TAG_FAIL(TAG_EINVAL, "an array is not aligned to its elements");
     if (Span(scores, n_query, n_slices, score_stride, el).meets(Span(grad, n_query, n_slices, grad_stride, el)))
         TAG_FAIL(TAG_EINVAL, "grad must not overlap scores");

@@ -9,7 +9,9 @@
                   followed by ``muon.step()``.
 
 Argument checks and marshalling only; everything runs in libtag.so's HIP
-kernels.  An object owns its workspace: its calls must be ordered.
+kernels.  An object owns its workspace: its calls must be ordered.  It is memory
+of the stream that is current when the object is made (a Muon's momentum too):
+another stream that a call is given has to wait for it first.
 """
 from __future__ import annotations
 
@@ -77,6 +79,9 @@ class Orthogonalise:
                 if stream is not None:   # (memory of the current stream)
                     stream.wait_stream(torch.cuda.current_stream(self.device))
             out = self.out
+        elif len({y.data_ptr() for y in out}) != len(out) or any(
+                y.data_ptr() == x.data_ptr() for i, x in enumerate(matrices) for j, y in enumerate(out) if i != j):
+            raise ValueError("an output may be its own input, not another's, nor another output")
         for g, s, x, y in zip(self._g, self.shapes, matrices, out):
             _set(getattr(g, "in"), x, "a matrix", s, self.dtype, self.device)
             _set(g.out, y, "an output", s, self.dtype, self.device)
@@ -112,6 +117,9 @@ class Muon:
         self.m = [torch.zeros_like(w) for w, _ in self.params] if state is None else list(state)
         if len(self.m) != len(self.params):
             raise ValueError("one momentum tensor per parameter is wanted")
+        written = [t.data_ptr() for t in self.m] + [w.data_ptr() for w, _ in self.params]
+        if len(set(written)) != len(written):
+            raise ValueError("a weight or a momentum stands there twice")
         self.options = tag_muon_options(float(lr), float(momentum), float(weight_decay), 1 if nesterov else 0)
         self._ns = _iteration(steps, coef, eps)
         self._g = (tag_muon_group * len(self.params))()
@@ -140,7 +148,9 @@ class Muon:
         return cls([(t[k].view(shapes[k]), g[k].view(shapes[k])) if k in shapes else (t[k], g[k]) for k in g], **kw)
 
     def step(self, lr: Optional[float] = None, stream=None) -> None:
-        """One step with the gradients as they stand."""
+        """One step with the gradients as they stand.  ``lr`` holds for this
+        step and the following ones; a step captured into a graph keeps the one
+        that it was captured with."""
         if lr is not None:
             self.options.lr = float(lr)
         _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),

@@ -9,7 +9,9 @@
 Argument checks and marshalling only; the operators run in libtag.so's HIP
 kernels.  As with the other reusable calls, an object owns its workspace and
 its outputs: calls of one object must be ordered (one stream, or one after the
-other), and each overwrites the outputs of the last.
+other), and each overwrites the outputs of the last.  They are memory of the
+stream that is current when the object is made: another stream that a call is
+given has to wait for it first.
 """
 from __future__ import annotations
 
@@ -60,7 +62,7 @@ def _rows(t, what, dtypes, device, n_rows, n_cols, shared=False):
     shape = t.shape
     if t.dtype not in dtypes or t.device != device:
         raise ValueError(f"{what} must be {' or '.join(str(d) for d in dtypes)} on {device}")
-    one = shared and (len(shape) == 1 or shape[0] == 1)
+    one = shared and (len(shape) == 1 or (len(shape) == 2 and shape[0] == 1))
     if len(shape) not in ((1, 2) if shared else (2,)) or shape[-1] != n_cols or not (one or shape[0] == n_rows):
         raise ValueError(f"{what} must have the shape [{n_rows}, {n_cols}]" + (" or one row" if shared else "")
                          + f", not {list(shape)}")

@@ -164,6 +164,21 @@ def test_orthogonalise_refusals(torch):
         Muon([(x, x + 1)], momentum=1.0).step()
 
 
+def test_arrays_given_twice_are_refused(torch):
+    from paper_2302_06126_amd.optim import Muon, Orthogonalise
+    x, y, g = (torch.ones(1, 8, 8, device="cuda") for _ in range(3))
+    call = Orthogonalise([(1, 8, 8), (1, 8, 8)])
+    for matrices, out in (([x, y], [y, x]), ([x, y], [g, g]), ([x, x], [x, y])):
+        with pytest.raises(ValueError):
+            call(matrices, out=out)
+    call([x, y], out=[x, g])
+    with pytest.raises(ValueError):   # one weight twice, one momentum for two
+        Muon([(x, g), (x, g)])
+    with pytest.raises(ValueError):
+        Muon([(x, g), (y, g)], state=[torch.zeros_like(x)[:]] * 2)
+    Muon([(x, g), (y, g)]).step()     # (a shared gradient is only read)
+
+
 # ----------------------------------------------------------------------- muon
 def _muon_reference(w, g, m, lr, mu, nesterov, wd, steps):
     """steps of the update in 64 bits (w, m), gradients held."""

@@ -101,7 +101,7 @@ def test_refusals(torch):
     one = TrainCase(topos[:1], 1, 64, 4, 1, 8, 1, seed=3)
     graph, model, tr, feats = _trainer(torch, one, 0.1)
     for kw in (dict(coef=-1.0), dict(coef=float("nan")), dict(loss=None), dict(count=None), dict(load=None),
-               dict(workspace=None), dict(ws_bytes=16)):
+               dict(workspace=None), dict(ws_bytes=16), dict(loss=tr.balance.loss + 2), dict(load=tr.balance.load + 1)):
         keep, tr.balance = tr.balance, tag_train_balance.from_buffer_copy(tr.balance)
         for k, v in kw.items():
             setattr(tr.balance, k, v)

@@ -39,6 +39,9 @@ def _ortho(abi, count=2, rows=8, cols=6, x=(1 << 20, 6, 48), y=(1 << 24, 6, 48),
     (dict(n=0), EINVAL), (dict(count=0), EINVAL), (dict(rows=0), EINVAL), (dict(cols=0), EINVAL), (dict(dtype=2), EINVAL),
     (dict(rows=32769, x=(1 << 20, 6, 1 << 20), y=(1 << 24, 6, 1 << 20)), ESHAPE),
     (dict(count=1 << 20, rows=20000, cols=20000, x=(1 << 20, 20000, 1 << 30), y=(1 << 24, 20000, 1 << 30)), ESHAPE),
+    # (launches of 2^32 threads and more)
+    (dict(count=(1 << 19) + 1), ESHAPE),
+    (dict(count=3, rows=32768, cols=32768, x=(1 << 20, 32768, 1 << 30), y=(1 << 50, 32768, 1 << 30)), ESHAPE),
     (dict(x=(None, 6, 48)), EINVAL), (dict(y=(None, 6, 48)), EINVAL), (dict(x=((1 << 20) + 2, 6, 48)), EINVAL),
     (dict(x=(1 << 20, 5, 48)), EINVAL), (dict(y=(1 << 24, 5, 48)), EINVAL), (dict(x=(1 << 20, 6, -48)), EINVAL),
     # results that overlap: a matrix stride of nothing, within a matrix, across interleaved rows

@@ -49,6 +49,11 @@ def _constrain(lib, Q=4, S=100, dtype=0, x=1 << 20, xs=100, c=None, out=None, os
     (dict(S=70000, xs=70000, ps=70000), ENOSPACE),
     (dict(S=70000, xs=70000, ps=70000, nb=1 << 20, ws=None), EINVAL),
     (dict(S=70000, xs=70000, ps=70000, nb=1 << 20, ws=(1 << 28) + 4), EINVAL),
+    (dict(c=_constraints(history=1 << 22, n_history=(1 << 30) + 1)), ESHAPE),
+    (dict(c=_constraints(repetition=(1 << 22) + 2)), EINVAL), (dict(best=(1 << 27) + 1), EINVAL),
+    # (launches of 2^32 threads and more)
+    (dict(Q=1 << 28, S=2, xs=2, ps=2, x=1 << 40, prior=1 << 44), ESHAPE),
+    (dict(Q=1 << 24, S=3000, xs=3000, ps=3000, x=1 << 40, prior=1 << 44), ESHAPE),
     (dict(Q=1 << 22, S=1 << 28, xs=1 << 28, ps=1 << 28, x=0x1000, prior=1 << 61, nb=1 << 40), ESHAPE),
 ])
 def test_constrain_refuses(lib, kw, status):
