@@ -54,7 +54,9 @@ typedef struct tag_ortho_group {
  * TAG_F32: products of two-part splits that hold every operand to 2^-22, with
  * fp32 accumulation, about as near the exact iteration as fp32 products.
  * TAG_BF16: X is carried to 2^-22 as well, the operands of the products are
- * rounded to 2^-11; the result is rounded once, to bf16.  Both are relative to
+ * rounded to 2^-11 (not the diagonals of A and B, and not at all where every
+ * matrix of a call is at most 64 x 256); the result is rounded once, to bf16,
+ * by more than the operands cost.  Both are relative to
  * the largest values of X, which is at most of norm one at first: where
  * ||G||_F is far below eps, what is left of it is held to 2^-37 of one.
  */

@@ -15,8 +15,14 @@
 // 2^-22 of it (2^-24.7 root mean square; fp32's own rounding 2^-25.4).  A product
 // is hi hi' + hi lo' + lo hi' (what is left out, lo lo', is below 2^-22 of it,
 // 2^-24.8 root mean square): three fp16 matrix instructions instead of the six
-// that exact bf16 splits need, or of fp32 ones at a sixteenth of the rate.  bf16 matrices take hi hi' alone; X keeps both parts, since the
-// a X term carries its error through every step.
+// that exact bf16 splits need, or of fp32 ones at a sixteenth of the rate.
+//
+// bf16 matrices take hi hi' alone.  X keeps both parts, since the a X term
+// carries its error through every step.  The nearer X comes to orthogonal, the
+// more of A and B stands on their diagonals, so those are left out of the
+// operands and kept in fp32: with A = L + A', B = c (A' A' + L A' + A' L + L L)
+// + b A in the products' epilogue, and B X = (B's diagonal) X + B' X there (with
+// the hi part of X in both, or a rounding error that B would cancel stays).
 //
 // Layout.  The operands lie in the order in which a 32x32x16 instruction takes
 // them ("fragments": 32 rows x 16 k, lane l holds 8 consecutive k of row l % 32,
@@ -132,6 +138,13 @@ __device__ __forceinline__ uint16_t *x_plane(const G &g, int mat, int buf, int t
 template <typename G>
 __device__ __forceinline__ uint16_t *s_plane(const G &g, int mat, int which, int plane) {
     return g.ops + mat * g.ops_stride + (int64_t)8 * g.np * g.mp + (int64_t)(which * 2 + plane) * g.np * g.np;
+}
+
+// PARTS = 1: 2^12 times the diagonal of A (which: 0) and of B (1)
+template <typename G>
+__device__ __forceinline__ float *diagonal(const G &g, int mat, int which) {
+    return reinterpret_cast<float *>(g.ops + mat * g.ops_stride + (int64_t)8 * g.np * g.mp + (int64_t)4 * g.np * g.np) +
+           which * g.np;
 }
 
 // group of a block (uniform selects among a few, all read at once)
@@ -555,6 +568,27 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         kf = f % TK;
     };
     u4v old[NQ][2];
+    // PARTS = 1: diagonals of the tile's rows (of a thread's pieces: eight, the same for all of them) and columns
+    constexpr bool DIAG = PARTS == 1 && MODE != kGram;
+    static_assert(8 % TK == 0, "a thread's pieces are of the same rows");
+    float drow[8] = {}, dcol[NQ] = {};
+    if (DIAG) {
+        const float *d = diagonal(G, mat, MODE != kSquare);
+        int rf, kf;
+        piece(0, rf, kf);
+        if (I * TK + kf < G.np / 16) {
+            const float *p = d + I * T + kf * 16 + pk;
+            const float4 x = *reinterpret_cast<const float4 *>(p), y = *reinterpret_cast<const float4 *>(p + 4);
+            drow[0] = x.x; drow[1] = x.y; drow[2] = x.z; drow[3] = x.w;
+            drow[4] = y.x; drow[5] = y.y; drow[6] = y.z; drow[7] = y.w;
+        }
+        if (MODE == kSquare)
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                piece(q, rf, kf);
+                if (J * F + rf < rfS) dcol[q] = d[J * T + rf * 32 + prow];
+            }
+    }
     if (MODE != kGram) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
@@ -591,6 +625,14 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (PARTS == 1 && MODE == kGram && I == J) {   // A's diagonal out of the operand
+        const int r = threadIdx.x;
+        if (r < T && I * T + r < G.np) {
+            diagonal(G, mat, 0)[I * T + r] = tile[r * P + r];
+            tile[r * P + r] = 0.f;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
     constexpr bool LAST = MODE == kFinal || MODE == kUpdate;
     auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8], bool both) {
         u4v hi, lo;
@@ -616,7 +658,15 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             for (int e = 0; e < 8; ++e) {
                 v[e] = c[e * P];
                 if (MODE != kGram) {
-                    v[e] = fmaf(ct, join2(old[q][0][e / 2], old[q][1][e / 2], e % 2), cv * v[e]);
+                    float t = ct;
+                    v[e] *= cv;
+                    if (DIAG && MODE == kSquare) t += B.c * kInvScale * (drow[e] + dcol[q]);
+                    if (DIAG && MODE != kSquare) v[e] = fmaf(drow[e] * kInvScale, join2(old[q][0][e / 2], 0u, e % 2), v[e]);
+                    v[e] = fmaf(t, join2(old[q][0][e / 2], old[q][1][e / 2], e % 2), v[e]);
+                    if (DIAG && MODE == kSquare && I == J && kf * 16 + pk + e == rf * 32 + prow) {
+                        diagonal(G, mat, 1)[I * T + kf * 16 + pk + e] = fmaf(fmaf(B.c * kInvScale, drow[e], ct), drow[e], v[e]);
+                        v[e] = 0.f;
+                    }
                     c[e * P] = v[e];
                 }
             }
@@ -663,7 +713,8 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
 
 // ------------------------------------------------------------- small matrices
 // A matrix of at most 64 by 64 MB: everything in one block, the operands in LDS,
-// one launch instead of 17 (a 64 x 42 matrix: 68 -> 18 us).  Few products, many waits: 16x16x32 instructions
+// one launch instead of 17 (a 64 x 42 matrix: 68 -> 18 us), products of both parts for
+// bf16 matrices too (one part alone: 15.6 us, and twice the error).  Few products, many waits: 16x16x32 instructions
 // (fragments of 16 rows x 32 k, lane l holds 8 consecutive k of row l % 16, k / 8
 // % 4 = l / 16), so that eight wavefronts share the smallest matrix and a block
 // has four values a lane.  What is read is held in registers until every
@@ -671,20 +722,15 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
 struct Sums {   // of fragments of even and of odd k (one operand negated), of the main and the cross products
     f4 m[2], x[2];
     __device__ __forceinline__ Sums() { m[0] = m[1] = x[0] = x[1] = f4{0.f, 0.f, 0.f, 0.f}; }
-    template <int PARTS>
     __device__ __forceinline__ void add(const h8 (&a)[2], const h8 (&b)[2], int odd) {
-        if (PARTS == 2) {
-            x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1], b[0], x[odd], 0, 0, 0);
-            m[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], m[odd], 0, 0, 0);
-            x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[1], x[odd], 0, 0, 0);
-        } else {
-            m[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], m[odd], 0, 0, 0);
-        }
+        x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1], b[0], x[odd], 0, 0, 0);
+        m[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], m[odd], 0, 0, 0);
+        x[odd] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[1], x[odd], 0, 0, 0);
     }
     __device__ __forceinline__ f4 total() const { return ((m[0] - m[1]) + (x[0] - x[1])) * kInvScale; }
 };
 
-template <typename T, bool MUON, int PARTS, int MB>
+template <typename T, bool MUON, int MB>
 __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
     constexpr int kX = 64 * 64 * MB, kA = 64 * 64;   // elements of a plane
     __shared__ __attribute__((aligned(1024))) uint16_t X[2 * kX], XT[2 * kX], S[2 * kA];
@@ -783,11 +829,11 @@ __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
     };
     auto frag = [&](const uint16_t *d, int plane, int f, h8 (&v)[2]) {
         v[0] = *reinterpret_cast<const h8 *>(d + f * kFrag + lane * 8);
-        if (PARTS == 2) v[1] = *reinterpret_cast<const h8 *>(d + plane + f * kFrag + lane * 8);
+        v[1] = *reinterpret_cast<const h8 *>(d + plane + f * kFrag + lane * 8);
     };
     auto negated = [&](h8 (&v)[2]) {
         v[0] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, v[0]) ^ 0x80008000u);
-        if (PARTS == 2) v[1] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, v[1]) ^ 0x80008000u);
+        v[1] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, v[1]) ^ 0x80008000u);
     };
     const int bi = wave >> 1, bj = wave & 1;   // rows of blocks, and the wavefront's blocks in it: bj, bj + 2, ..
     // C = R R^T of 64 x 64, R of nk fragments a row
@@ -801,8 +847,8 @@ __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
                 frag(d, plane, bj * nk + k + odd, b[0]);
                 frag(d, plane, (bj + 2) * nk + k + odd, b[1]);
                 if (odd) negated(a);
-                c[0].add<PARTS>(a, b[0], odd);
-                c[1].add<PARTS>(a, b[1], odd);
+                c[0].add(a, b[0], odd);
+                c[1].add(a, b[1], odd);
             }
         }
         v[0] = c[0].total();
@@ -838,12 +884,12 @@ __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
             frag(XT, kX, j * 2, x[0]);
             frag(XT, kX, j * 2 + 1, x[1]);
             Sums t, o;
-            t.add<PARTS>(r[0], x[0], 0);
-            t.add<PARTS>(rn, x[1], 1);
+            t.add(r[0], x[0], 0);
+            t.add(rn, x[1], 1);
             vt[q] = t.total() + B.a * here(XT, kX, at(j, bi, 2));
             if (last) continue;
-            o.add<PARTS>(x[0], r[0], 0);
-            o.add<PARTS>(x[1], rn, 1);
+            o.add(x[0], r[0], 0);
+            o.add(x[1], rn, 1);
             vx[q] = o.total() + B.a * here(X, kX, at(bi, j, kx));
         }
         __syncthreads();
@@ -886,7 +932,7 @@ size_t carve_ns(Group *g, int32_t n, void *base) {
     for (int i = 0; i < n; ++i) {
         Group &G = g[i];
         G.part = c.take<double>((size_t)G.count * G.chunks);
-        G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np;
+        G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np + 4ll * G.np;
         G.ops = c.take<uint16_t>((size_t)G.count * G.ops_stride);
     }
     return c.used;
@@ -1037,8 +1083,8 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
             K.rows = G.rows; K.cols = G.cols; K.mp = G.mp; K.factor = G.factor;
         }
         const unsigned blocks = number_blocks(S.g, n, kSet, [&](int i) { return (int64_t)mats[i].count; });
-        if (wide <= 128) ns_small<T, MUON, PARTS, 2><<<blocks, 512, 0, st>>>(S);
-        else ns_small<T, MUON, PARTS, 4><<<blocks, 512, 0, st>>>(S);
+        if (wide <= 128) ns_small<T, MUON, 2><<<blocks, 512, 0, st>>>(S);
+        else ns_small<T, MUON, 4><<<blocks, 512, 0, st>>>(S);
         if (n_plain == 0) return;
     }
     unsigned grid = number_blocks(N.g, N.n_groups, kSet + kSetPlain, [&](int i) {

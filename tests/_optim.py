@@ -45,3 +45,29 @@ def tolerance(shape, norms, steps=5, bf16=False):
     if bf16:   # X's own error is raised all the same
         total += sum(4.0 ** (steps - 1 - k) * 9 * 2.0 ** -20 * norms[k + 1] for k in range(steps))
     return total, 10 * total / np.sqrt(min(shape) * max(shape))
+
+
+def rounded_bf16(g, steps=5, coef=QUINTIC, eps=1e-7):
+    """The iteration of products in 64 bits with the operands' roundings of the
+    bf16 form: 2^12 times X, A and B in fp16, the diagonals of A and B apart
+    from them and exact, X held in two parts."""
+    def held(x, parts):
+        x = 4096.0 * x
+        hi = x.astype(np.float16).astype(np.float64)
+        return (hi + (0.0 if parts == 1 else (x - hi).astype(np.float16).astype(np.float64))) / 4096.0
+
+    g = np.asarray(g, np.float64)
+    x = g if g.shape[0] <= g.shape[1] else g.T
+    x = held(x / (np.sqrt((x * x).sum()) + eps), 2)
+    a, b, c = coef
+    eye = np.eye(x.shape[0])
+    for _ in range(steps):
+        xh = held(x, 1)
+        A = xh @ xh.T
+        d = np.diag(A)
+        off = A - eye * d
+        offh = held(off, 1)
+        B = b * A + c * (offh @ offh + (d[:, None] + d[None]) * held(off, 2) + eye * (d * d))
+        e = np.diag(B)
+        x = held(a * x + e[:, None] * xh + held(B - eye * e, 1) @ xh, 2)
+    return x if g.shape[0] <= g.shape[1] else x.T

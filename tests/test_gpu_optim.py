@@ -69,6 +69,36 @@ def test_orthogonalise_large_tiles(torch, count, shape, dtype):
         _check(got[i], t[i].float().numpy(), bf16=dtype == "bf16")
 
 
+@pytest.mark.parametrize("shape", [(64, 1024), (8, 2000), (256, 256), (300, 900), (700, 500)])
+@pytest.mark.parametrize("kind", ["gradient", "normal"])
+def test_bf16_loses_little_beside_the_results_rounding(torch, shape, kind):
+    """The result is a rounding to bf16 of an iteration with the roundings of
+    rounded_bf16.  It strays from that by fp32 sums (2^-17 and less of ||X||, see
+    tests/_optim.py) that now and then turn an operand's rounding (2^-10 of the
+    operand; one in 2^6 of them at 2^-17 over a spacing of 2^-11, so 2^-3 of the
+    roundings' own effect, which is below 2^-8): 2^-11 in all.  Without the
+    diagonals apart the error is 1.5 to 2.3 times the rounding's."""
+    from paper_2302_06126_amd.optim import orthogonalise
+    t = torch.from_numpy(_matrix(8, *shape, kind=kind)).to(torch.bfloat16)
+    g = t.double().numpy()
+    exact, want = R.newton_schulz(g)[0], R.rounded_bf16(g)
+    rounding = np.linalg.norm(torch.from_numpy(want).to(torch.bfloat16).double().numpy() - want)
+    size = np.linalg.norm(exact)
+    got = orthogonalise(t.cuda()).double().cpu().numpy()
+    err = np.linalg.norm(got - exact)
+    _say(f"   {shape} {kind}: {err / size:.2e}, of it the result's rounding {rounding / size:.2e}, the operands' "
+         f"{np.linalg.norm(want - exact) / size:.2e}")
+    assert err <= rounding + np.linalg.norm(want - exact) + 2.0 ** -11 * size
+
+
+@pytest.mark.parametrize("shape", [(5, 9), (64, 256), (42, 64), (200, 30)])
+def test_small_bf16_matrices_are_the_rounded_fp32_ones(torch, shape):
+    """Up to 64 x 256 both types take products of both parts: the same sums, rounded once at the end."""
+    from paper_2302_06126_amd.optim import orthogonalise
+    t = torch.from_numpy(_matrix(9, 3, *shape)).to(torch.bfloat16).cuda()
+    assert torch.equal(orthogonalise(t), orthogonalise(t.float()).to(torch.bfloat16))
+
+
 @pytest.mark.parametrize("steps,coef", [(1, R.QUINTIC), (2, R.QUINTIC), (3, (2.0, -1.5, 0.5)), (12, (1.5, -0.5, 0.0)),
                                         (6, (3.0, -3.2, 1.2))])
 def test_orthogonalise_other_iterations(torch, steps, coef):

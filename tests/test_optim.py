@@ -116,6 +116,15 @@ def test_workspaces_hold_the_largest_set_of_groups(abi):
 
 
 # ------------------------------------------------------------ the restatement
+@pytest.mark.parametrize("shape", [(8, 8), (64, 300), (90, 40)])
+def test_restatement_with_the_bf16_forms_roundings(shape):
+    """Near the exact one (2^-11 of an operand's elements, five steps), and not equal to it."""
+    g = np.random.default_rng(shape).normal(0, 1, shape)
+    want = R.newton_schulz(g)[0]
+    err = np.linalg.norm(R.rounded_bf16(g) - want) / np.linalg.norm(want)
+    assert 1e-5 < err < 2.0 ** -8
+
+
 @pytest.mark.parametrize("shape", [(5, 9), (9, 5), (16, 16), (1, 7)])
 def test_restatement_is_the_iteration_of_products(shape):
     g = np.random.default_rng(shape).normal(0, 1, shape)
