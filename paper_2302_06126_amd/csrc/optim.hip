@@ -425,6 +425,25 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         const int row = min((side ? J : I) * F + rf, (side ? rfS : rfR) - 1);
         src[i] = p + ((int64_t)row * nk + kf) * kFrag + lane * 8;
     }
+    // (the tile as it leaves: below)
+    constexpr int P = T + 4, NQ = T * T / 8 / 512, TK = T / 16;
+    static_assert(T * P * 4 <= NB * kStage * 1024, "the ring holds the tile");
+    const int prow = (threadIdx.x & 31), pk = 8 * (lane >> 5);   // of a piece, within its fragment
+    // PARTS = 1: diagonals of the tile's rows (of a thread's pieces: eight, the same for all of them) and columns, asked
+    // for before the products (after them: 688 us for 4 of 1024 x 4096, so 681)
+    constexpr bool DIAG = PARTS == 1 && MODE != kGram;
+    static_assert(8 % TK == 0, "a thread's pieces are of the same rows");
+    float drow[8] = {}, dcol[NQ] = {};
+    if (DIAG) {   // (past the matrix: the last ones again, for pieces that are left out)
+        const float *d = diagonal(G, mat, MODE != kSquare);
+        const float *p = d + min(I * T + wave % TK * 16, G.np - 16) + pk;
+        const float4 x = *reinterpret_cast<const float4 *>(p), y = *reinterpret_cast<const float4 *>(p + 4);
+        drow[0] = x.x; drow[1] = x.y; drow[2] = x.z; drow[3] = x.w;
+        drow[4] = y.x; drow[5] = y.y; drow[6] = y.z; drow[7] = y.w;
+        if (MODE == kSquare)
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) dcol[q] = d[min(J * T + (wave + 8 * q) / TK * 32, G.np - 32) + prow];
+    }
     auto load = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
@@ -550,8 +569,6 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
     // What is left goes over the tile in LDS, by pieces of eight consecutive k of a row of the next operand: 64
     // threads to a fragment.  First in the order of S's rows (the transpose of the tile), with the term of the
     // iteration itself (c A A + b A, B X + a X), whose operand has that order too and is asked for now.
-    constexpr int P = T + 4, NQ = T * T / 8 / 512, TK = T / 16;
-    static_assert(T * P * 4 <= NB * kStage * 1024, "the ring holds the tile");
     float *tile = reinterpret_cast<float *>(sh);
     uint16_t *to[2][2];   // operand written in S's order, in R's; hi, lo
     const uint16_t *was[2] = {nullptr, nullptr};
@@ -561,34 +578,12 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         else { to[0][pl] = x_plane(G, mat, 1 - B.cur, 1, pl); to[1][pl] = x_plane(G, mat, 1 - B.cur, 0, pl); }
         if (MODE != kGram) was[pl] = MODE == kSquare ? s_plane(G, mat, 0, pl) : x_plane(G, mat, B.cur, 1, pl);
     }
-    const int prow = (threadIdx.x & 31), pk = 8 * (lane >> 5);   // of a piece, within its fragment
     auto piece = [&](int q, int &rf, int &kf) {                   // the fragment of a thread's piece
         const int f = wave + 8 * q;
         rf = f / TK;
         kf = f % TK;
     };
     u4v old[NQ][2];
-    // PARTS = 1: diagonals of the tile's rows (of a thread's pieces: eight, the same for all of them) and columns
-    constexpr bool DIAG = PARTS == 1 && MODE != kGram;
-    static_assert(8 % TK == 0, "a thread's pieces are of the same rows");
-    float drow[8] = {}, dcol[NQ] = {};
-    if (DIAG) {
-        const float *d = diagonal(G, mat, MODE != kSquare);
-        int rf, kf;
-        piece(0, rf, kf);
-        if (I * TK + kf < G.np / 16) {
-            const float *p = d + I * T + kf * 16 + pk;
-            const float4 x = *reinterpret_cast<const float4 *>(p), y = *reinterpret_cast<const float4 *>(p + 4);
-            drow[0] = x.x; drow[1] = x.y; drow[2] = x.z; drow[3] = x.w;
-            drow[4] = y.x; drow[5] = y.y; drow[6] = y.z; drow[7] = y.w;
-        }
-        if (MODE == kSquare)
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                piece(q, rf, kf);
-                if (J * F + rf < rfS) dcol[q] = d[J * T + rf * 32 + prow];
-            }
-    }
     if (MODE != kGram) {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
