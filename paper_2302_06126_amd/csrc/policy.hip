@@ -446,15 +446,17 @@ __global__ void __launch_bounds__(1024) bal_count(BalArgs A) {
 }
 
 // Device t's load from the sum of its parts (threads t < 64, one wavefront), and
-// the centre of h: its mean over the decisions taken (the softmax's gradient does
-// not see a shift of h, and what is left of h rounds less).
+// the centre of h: its mean over slices that use every device equally, the mean
+// load (the softmax's gradient does not see a shift of h, and what is left of h
+// rounds less; its mean over the decisions taken, which stand far from the others
+// where they are few, leaves gradients of 1 x 1,111 an error of 5.4e-7, this 1e-7).
 __device__ __forceinline__ double device_load(const BalArgs &A, double s, double n, bool write, double *centre) {
     const int t = threadIdx.x;
     s = n > 0.0 ? s / n : 0.0;
     if (write && t < A.M) A.load[t] = (float)s;
-    double c = s * s;
+    double c = s;
     for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, 64);
-    *centre = c;
+    *centre = c / A.M;
     return s;
 }
 // h of a slice less the centre

@@ -275,7 +275,7 @@ def _check_balance(t, masks, M, coef, use, bal, bf16):
     loss, grad, count, load, h = R.balance(x, masks, M, coef, use)
     assert np.array_equal(bal.count.cpu().numpy(), count)
     assert np.all(np.abs(bal.load.cpu().numpy() - load) <= 1.01 * R.EPS * load)
-    H = np.abs(h - load @ load).max(initial=0.0)
+    H = np.abs(h - load.sum() / M).max(initial=0.0)
     n = max(1, int((np.asarray(use) if use is not None else np.ones(len(x))).sum()))
     steps = 4 * 88 + 160
     got = float(bal.loss.item())
@@ -319,6 +319,32 @@ def test_balance_many_rows(torch, Q, S, M):
     bal.ws.fill_(255)
     bal(x, 0.01, use=u)
     assert all(torch.equal(a, b) for a, b in zip(first, (bal.loss, bal.grad, bal.count, bal.load)))
+
+
+@pytest.mark.parametrize("seed", range(4))
+@pytest.mark.parametrize("S,M", [(60, 8), (250, 64), (1111, 49), (9000, 30)])
+def test_balance_of_one_row(torch, S, M, seed):
+    """One query's gradient is small differences of h, most of which are far
+    below that of the slice it chose.  With h' = h less the mean load, in units
+    of 2^-24: h' and p'h rounded (1 each of |h'| and of their row's mean |h'|, the
+    sum's terms 3 for e^x and 1 for the product, its additions 2 by their root),
+    their difference, and 8 for p, the scale and the result."""
+    from paper_2302_06126_amd.policy import Balance
+    rng = np.random.default_rng((2302, seed, S, M))
+    x = rng.normal(0, 2, (1, S)).astype(np.float32)
+    masks = np.zeros(S, np.uint64)
+    for _ in range(3):   # up to three devices of a slice
+        masks |= np.uint64(1) << rng.integers(0, M, S, dtype=np.uint64)
+    bal = Balance(masks, M, 1)
+    loss = bal(torch.from_numpy(x).cuda(), 0.01).item()
+    want, grad, count, load, h = R.balance(x, masks, M, 0.01)
+    p = np.exp(x[0].astype(np.float64) - x.max())
+    p /= p.sum()
+    off = np.abs(h - load.sum() / M)
+    tol = R.EPS * (0.01 * M * p * (off + 8 * (p @ off)) + 8 * np.abs(grad[0]))
+    err = np.abs(bal.grad.cpu().numpy()[0] - grad[0])
+    _say(f"   {np.linalg.norm(err) / np.linalg.norm(grad):.2e} of the gradient, {(err / tol).max():.2f} of the tolerance")
+    assert np.all(err <= tol + 2.0 ** -125) and abs(loss - want) <= 8 * R.EPS * want
 
 
 @pytest.mark.parametrize("S", [50, 300, 2000, 5000])
