@@ -365,7 +365,7 @@ __device__ __forceinline__ void wait_arrival() {
 // at the 1.6 GHz that the chip then holds, 70% of their peak at it; X X^T and A A
 // 43 us (136 tiles, half of the CUs, a higher clock).  Around the products a launch
 // takes 2 us to the first load, 1 until it lands, 2 to join the halves of k, 4 to write
-// 34 MB.  PARTS = 1, four of 1024 x 4096: B X 63 us, bound by memory (100 MB written,
+// 34 MB.  PARTS = 1, four of 1024 x 4096: B X 65 to 73 us, bound by memory (100 MB written,
 // 67 MB of X read again).  Tried without gain: two stages of twice the length instead
 // of four, stages' barriers by the compiler (which waits for every load), one
 // wavefront per SIMD (the products wait for LDS: 60 us).
