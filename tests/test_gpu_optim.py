@@ -194,6 +194,18 @@ def test_orthogonalise_refusals(torch):
         Muon([(x, x + 1)], momentum=1.0).step()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 300), (5, 9), (300, 64), (70, 300)])
+def test_matrices_that_are_not_finite_stay_alone(torch, shape, dtype):
+    from paper_2302_06126_amd.optim import orthogonalise
+    x = torch.from_numpy(_matrix(10, 4, *shape)).to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+    clean = orthogonalise(x)
+    x[1, -1, 0], x[2, 0, -1], x[3] = float("nan"), float("-inf"), 0.0
+    y = orthogonalise(x)
+    assert torch.equal(y[0], clean[0]) and torch.isfinite(y[0]).all()
+    assert torch.isnan(y[1]).all() and torch.isnan(y[2]).all() and not y[3].any()
+
+
 def test_arrays_given_twice_are_refused(torch):
     from paper_2302_06126_amd.optim import Muon, Orthogonalise
     x, y, g = (torch.ones(1, 8, 8, device="cuda") for _ in range(3))
