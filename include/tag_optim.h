@@ -51,14 +51,12 @@ typedef struct tag_ortho_group {
 
 /*
  * Orthogonalises every matrix of every group.  dtype: of in and out.
- * TAG_F32: products of two-part splits that hold every operand to 2^-22, with
- * fp32 accumulation, about as near the exact iteration as fp32 products.
- * TAG_BF16: X is carried to 2^-22 as well, the operands of the products are
- * rounded to 2^-11 (not the diagonals of A and B, and not at all where every
- * matrix of a call is at most 64 x 256); the result is rounded once, to bf16,
- * by more than the operands cost.  Both are relative to
+ * Products of two-part splits that hold every operand to 2^-22, with fp32
+ * accumulation, about as near the exact iteration as fp32 products; TAG_BF16
+ * results are rounded once, from the same accuracy.  That is relative to
  * the largest values of X, which is at most of norm one at first: where
- * ||G||_F is far below eps, what is left of it is held to 2^-37 of one.
+ * ||G||_F is far below eps, what is left of it is held to 2^-37 of one.  Which
+ * order a matrix's sums take depends on the sizes of the call's other groups.
  */
 tag_status tag_orthogonalise_workspace(const tag_ortho_group *groups, int32_t n_groups, size_t *bytes);
 tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n_groups, int32_t dtype,

@@ -17,12 +17,10 @@
 // 2^-24.8 root mean square): three fp16 matrix instructions instead of the six
 // that exact bf16 splits need, or of fp32 ones at a sixteenth of the rate.
 //
-// bf16 matrices take hi hi' alone.  X keeps both parts, since the a X term
-// carries its error through every step.  The nearer X comes to orthogonal, the
-// more of A and B stands on their diagonals, so those are left out of the
-// operands and kept in fp32: with A = L + A', B = c (A' A' + L A' + A' L + L L)
-// + b A in the products' epilogue, and B X = (B's diagonal) X + B' X there (with
-// the hi part of X in both, or a rounding error that B would cancel stays).
+// bf16 matrices take the same products, and their result is rounded once.  With
+// one part of the operands (2^-11 of them) the products of 4 of 1024 x 4096 take
+// 670 us in place of 1,215, but the operands then cost as much as that rounding, and
+// where their roundings agree, as in a matrix of equal values, ten times as much.
 //
 // Layout.  The operands lie in the order in which a 32x32x16 instruction takes
 // them ("fragments": 32 rows x 16 k, lane l holds 8 consecutive k of row l % 32,
@@ -140,13 +138,6 @@ __device__ __forceinline__ uint16_t *s_plane(const G &g, int mat, int which, int
     return g.ops + mat * g.ops_stride + (int64_t)8 * g.np * g.mp + (int64_t)(which * 2 + plane) * g.np * g.np;
 }
 
-// PARTS = 1: 2^12 times the diagonal of A (which: 0) and of B (1)
-template <typename G>
-__device__ __forceinline__ float *diagonal(const G &g, int mat, int which) {
-    return reinterpret_cast<float *>(g.ops + mat * g.ops_stride + (int64_t)8 * g.np * g.mp + (int64_t)4 * g.np * g.np) +
-           which * g.np;
-}
-
 // group of a block (uniform selects among a few, all read at once)
 template <int N, typename G>
 __device__ __forceinline__ int find_group(const G (&g)[N], int n, int32_t &bid) {
@@ -260,9 +251,9 @@ __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
 }
 
 // X and X^T of the first buffer: one block per 64 x 64 tile of the padded
-// matrix (as it is stored), through LDS.  PARTS = 1: X (for A alone) has no lo
-// plane.  Memory bounds it: 2048 x 2048 fp32 12.6 us (17 MB read, 34 MB written).
-template <typename T, bool MUON, int PARTS>
+// matrix (as it is stored), through LDS.  Memory bounds it: 2048 x 2048 fp32 12.6
+// us (17 MB read, 34 MB written).
+template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
     __shared__ float tile[64][65];
     __shared__ double red[4];
@@ -335,7 +326,7 @@ __global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
         const int kf = (xt ? G.np : G.mp) / 16;
         const int64_t at = ((int64_t)(row / 32) * kf + k / 16) * kFrag + (row % 32 + 32 * (k / 8 % 2)) * 8;
         *reinterpret_cast<u4v *>(x_plane(G, mat, 0, xt, 0) + at) = hi;
-        if (PARTS == 2 || xt) *reinterpret_cast<u4v *>(x_plane(G, mat, 0, xt, 1) + at) = lo;
+        *reinterpret_cast<u4v *>(x_plane(G, mat, 0, xt, 1) + at) = lo;
     }
 }
 
@@ -352,23 +343,21 @@ __device__ __forceinline__ void wait_arrival() {
 }
 
 // C = R S^T over one tile of T x T outputs per block, R and S operand planes of
-// K/16 fragments per row.  PARTS = 2: three part products a step, PARTS = 1: the
-// hi planes alone.  Eight wavefronts: four cover the tile (T/2 x T/2 each) for
-// the even fragments of k, four for the odd ones.  Stages of KF fragments of k go
-// through a ring of NB LDS buffers by direct loads, up to NB stages ahead of the
-// products (a stage's products take less time than a load from beyond the L2),
-// and a stage's fragments are read from LDS while the last stage's are
-// multiplied.
+// K/16 fragments per row, three part products a step.  Eight wavefronts: four
+// cover the tile (T/2 x T/2 each) for the even fragments of k, four for the odd
+// ones.  Stages of KF fragments of k go through a ring of NB LDS buffers by direct
+// loads, up to NB stages ahead of the products (a stage's products take less time
+// than a load from beyond the L2), and a stage's fragments are read from LDS while
+// the last stage's are multiplied.
 //
-// 2048^3, PARTS = 2: B X 54 us (256 tiles, 950 TFLOP/s of fp16 products; a library's
+// 2048^3: B X 54 us (256 tiles, 950 TFLOP/s of fp16 products; a library's
 // bf16 product of 2048^3 reaches 418, of 8192^3 1,164), of which 43 us of products
 // at the 1.6 GHz that the chip then holds, 70% of their peak at it; X X^T and A A
 // 43 us (136 tiles, half of the CUs, a higher clock).  Around the products a launch
 // takes 2 us to the first load, 1 until it lands, 2 to join the halves of k, 4 to write
-// 34 MB.  PARTS = 1, four of 1024 x 4096: B X 65 to 73 us, bound by memory (100 MB written,
-// 67 MB of X read again).  Tried without gain: two stages of twice the length instead
-// of four, stages' barriers by the compiler (which waits for every load), one
-// wavefront per SIMD (the products wait for LDS: 60 us).
+// 34 MB.  Tried without gain: two stages of twice the length instead of four,
+// stages' barriers by the compiler (which waits for every load), one wavefront per
+// SIMD (the products wait for LDS: 60 us).
 //
 // The matrix cores round their sums towards minus infinity, a bias that grows
 // with the number of steps where rounding errors grow with its root; the odd
@@ -381,10 +370,10 @@ struct SetOf<kFinal> { typedef EndSet type; };
 template <>
 struct SetOf<kUpdate> { typedef EndSet type; };
 
-template <int T, int PARTS, int MODE, typename OUT>
+template <int T, int MODE, typename OUT>
 __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetOf<MODE>::type B) {
-    constexpr int F = T / 32, W = F / 2, KF = PARTS == 2 ? 2 : 4, NB = 4;   // (the last stages: cases up to 4)
-    constexpr int kStage = 2 * F * PARTS * KF, L = kStage / 8;   // fragments of a stage, and each wavefront's share
+    constexpr int F = T / 32, W = F / 2, KF = 2, NB = 4;   // (the last stages: cases up to 4)
+    constexpr int kStage = 4 * F * KF, L = kStage / 8;   // fragments of a stage, and each wavefront's share
     constexpr bool SYM = MODE == kGram || MODE == kSquare;
     __shared__ __attribute__((aligned(1024))) unsigned char sh[NB * kStage * 1024];
     int32_t bid = (int32_t)xcd_swizzle(blockIdx.x, gridDim.x);
@@ -429,21 +418,6 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
     constexpr int P = T + 4, NQ = T * T / 8 / 512, TK = T / 16;
     static_assert(T * P * 4 <= NB * kStage * 1024, "the ring holds the tile");
     const int prow = (threadIdx.x & 31), pk = 8 * (lane >> 5);   // of a piece, within its fragment
-    // PARTS = 1: diagonals of the tile's rows (of a thread's pieces: eight, the same for all of them) and columns, asked
-    // for before the products (after them: 688 us for 4 of 1024 x 4096, so 681)
-    constexpr bool DIAG = PARTS == 1 && MODE != kGram;
-    static_assert(8 % TK == 0, "a thread's pieces are of the same rows");
-    float drow[8] = {}, dcol[NQ] = {};
-    if (DIAG) {   // (past the matrix: the last ones again, for pieces that are left out)
-        const float *d = diagonal(G, mat, MODE != kSquare);
-        const float *p = d + min(I * T + wave % TK * 16, G.np - 16) + pk;
-        const float4 x = *reinterpret_cast<const float4 *>(p), y = *reinterpret_cast<const float4 *>(p + 4);
-        drow[0] = x.x; drow[1] = x.y; drow[2] = x.z; drow[3] = x.w;
-        drow[4] = y.x; drow[5] = y.y; drow[6] = y.z; drow[7] = y.w;
-        if (MODE == kSquare)
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) dcol[q] = d[min(J * T + (wave + 8 * q) / TK * 32, G.np - 32) + prow];
-    }
     auto load = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < L; ++i) {
@@ -451,9 +425,9 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             src[i] += KF * kFrag;
         }
     };
-    // (one block of accumulators per wavefront: a set for each part product, or for each fragment of a stage, since
-    // consecutive products into one set wait for one another)
-    constexpr int NA = W == 2 ? 1 : PARTS == 2 ? 3 : 2, NK = KF / 2;
+    // (one block of accumulators per wavefront: a set for each part product, since consecutive products into one set
+    // wait for one another)
+    constexpr int NA = W == 2 ? 1 : 3, NK = KF / 2;
     f16v acc[W][W], more[NA];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -465,7 +439,7 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
     const unsigned neg = kg ? 0x80008000u : 0u;
     const int stages = nk / KF;
     struct Frags {
-        h8 a[NK][W][PARTS], b[NK][W][PARTS];
+        h8 a[NK][W][2], b[NK][W][2];
     };
     auto fetch = [&](int s, Frags &f) {
         const u4v *fr = reinterpret_cast<const u4v *>(sh + (s % NB) * kStage * 1024);
@@ -474,36 +448,34 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
 #pragma unroll
             for (int i = 0; i < W; ++i)
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
+                for (int p = 0; p < 2; ++p) {
                     const int kf = 2 * k + kg;
                     f.a[k][i][p] = __builtin_bit_cast(h8, fr[((p * F + wi * W + i) * KF + kf) * 64 + lane]);
-                    f.b[k][i][p] = __builtin_bit_cast(h8, fr[(((PARTS + p) * F + wj * W + i) * KF + kf) * 64 + lane]);
+                    f.b[k][i][p] = __builtin_bit_cast(h8, fr[(((2 + p) * F + wj * W + i) * KF + kf) * 64 + lane]);
                 }
     };
     auto multiply = [&](const Frags &f) {
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-            h8 a[W][PARTS];
+            h8 a[W][2];
 #pragma unroll
             for (int i = 0; i < W; ++i)
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p)
+                for (int p = 0; p < 2; ++p)
                     a[i][p] = __builtin_bit_cast(h8, __builtin_bit_cast(u4v, f.a[k][i][p]) ^ neg);
             auto product = [&](f16v &d, int i, int j, int pa, int pb) {
                 d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][pa], f.b[k][j][pb], d, 0, 0, 0);
             };
             if constexpr (W == 1) {
-                if (PARTS == 2) {
-                    product(more[1], 0, 0, PARTS - 1, 0);
-                    product(more[NA - 1], 0, 0, 0, PARTS - 1);
-                }
-                product(PARTS == 2 ? more[0] : more[k % NA], 0, 0, 0, 0);
+                product(more[1], 0, 0, 1, 0);
+                product(more[2], 0, 0, 0, 1);
+                product(more[0], 0, 0, 0, 0);
             } else {
 #pragma unroll
-                for (int q = PARTS == 2 ? 0 : 2; q < 3; ++q)
+                for (int q = 0; q < 3; ++q)
 #pragma unroll
                     for (int ij = 0; ij < 4; ++ij)
-                        product(acc[ij / 2][ij % 2], ij / 2, ij % 2, q == 0 ? PARTS - 1 : 0, q == 1 ? PARTS - 1 : 0);
+                        product(acc[ij / 2][ij % 2], ij / 2, ij % 2, q == 0, q == 1);
             }
         }
     };
@@ -518,9 +490,9 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         load(s % NB);
         multiply(now);
         // the reads go out first, the direct loads between the products
-        constexpr int NM = (W == 2 ? 4 : 1) * NK * (PARTS == 2 ? 3 : 1), M1 = NM / (L + 1);
+        constexpr int NM = (W == 2 ? 4 : 1) * NK * 3, M1 = NM / (L + 1);
         static_assert(L == 2 || L == 4, "two or four direct loads");
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * NK * W * PARTS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4 * NK * W, 0);
         __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
         __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x8, M1, 0);
@@ -563,9 +535,8 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
     }
     if constexpr (W == 1) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[0][0][e] = PARTS == 2 ? more[0][e] + (more[1][e] + more[NA - 1][e]) : more[0][e] + more[NA - 1][e];
+        for (int e = 0; e < 16; ++e) acc[0][0][e] = more[0][e] + (more[1][e] + more[2][e]);
     }
-    // (PARTS = 1: the lo planes that are read are those of X^T and of A in S's order)
     // What is left goes over the tile in LDS, by pieces of eight consecutive k of a row of the next operand: 64
     // threads to a fragment.  First in the order of S's rows (the transpose of the tile), with the term of the
     // iteration itself (c A A + b A, B X + a X), whose operand has that order too and is asked for now.
@@ -620,16 +591,8 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             }
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (PARTS == 1 && MODE == kGram && I == J) {   // A's diagonal out of the operand
-        const int r = threadIdx.x;
-        if (r < T && I * T + r < G.np) {
-            diagonal(G, mat, 0)[I * T + r] = tile[r * P + r];
-            tile[r * P + r] = 0.f;
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    }
     constexpr bool LAST = MODE == kFinal || MODE == kUpdate;
-    auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8], bool both) {
+    auto store = [&](uint16_t *const (&d)[2], int64_t at, const float (&v)[8]) {
         u4v hi, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -639,7 +602,7 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             lo[e] = l;
         }
         *reinterpret_cast<u4v *>(d[0] + at) = hi;
-        if (both) *reinterpret_cast<u4v *>(d[1] + at) = lo;
+        *reinterpret_cast<u4v *>(d[1] + at) = lo;
     };
     {
         const float cv = MODE == kSquare ? B.c : 1.f, ct = MODE == kSquare ? B.b : B.a;
@@ -653,20 +616,11 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             for (int e = 0; e < 8; ++e) {
                 v[e] = c[e * P];
                 if (MODE != kGram) {
-                    float t = ct;
-                    v[e] *= cv;
-                    if (DIAG && MODE == kSquare) t += B.c * kInvScale * (drow[e] + dcol[q]);
-                    if (DIAG && MODE != kSquare) v[e] = fmaf(drow[e] * kInvScale, join2(old[q][0][e / 2], 0u, e % 2), v[e]);
-                    v[e] = fmaf(t, join2(old[q][0][e / 2], old[q][1][e / 2], e % 2), v[e]);
-                    if (DIAG && MODE == kSquare && I == J && kf * 16 + pk + e == rf * 32 + prow) {
-                        diagonal(G, mat, 1)[I * T + kf * 16 + pk + e] = fmaf(fmaf(B.c * kInvScale, drow[e], ct), drow[e], v[e]);
-                        v[e] = 0.f;
-                    }
+                    v[e] = fmaf(ct, join2(old[q][0][e / 2], old[q][1][e / 2], e % 2), cv * v[e]);
                     c[e * P] = v[e];
                 }
             }
-            if (!LAST) store(to[0], ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8, v,
-                             PARTS == 2 || MODE != kSquare);
+            if (!LAST) store(to[0], ((int64_t)(J * F + rf) * (G.np / 16) + I * TK + kf) * kFrag + lane * 8, v);
         }
         if (MODE != kGram) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
@@ -681,7 +635,7 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
             const float *c = tile + (rf * 32 + prow) * P + kf * 16 + pk;
             const float4 x = *reinterpret_cast<const float4 *>(c), y = *reinterpret_cast<const float4 *>(c + 4);
             const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-            store(to[1], ((int64_t)(I * F + rf) * nkR + J * TK + kf) * kFrag + lane * 8, v, PARTS == 2);
+            store(to[1], ((int64_t)(I * F + rf) * nkR + J * TK + kf) * kFrag + lane * 8, v);
         }
         return;
     }
@@ -708,8 +662,7 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
 
 // ------------------------------------------------------------- small matrices
 // A matrix of at most 64 by 64 MB: everything in one block, the operands in LDS,
-// one launch instead of 17 (a 64 x 42 matrix: 68 -> 18 us), products of both parts for
-// bf16 matrices too (one part alone: 15.6 us, and twice the error).  Few products, many waits: 16x16x32 instructions
+// one launch instead of 17 (a 64 x 42 matrix: 68 -> 18 us).  Few products, many waits: 16x16x32 instructions
 // (fragments of 16 rows x 32 k, lane l holds 8 consecutive k of row l % 16, k / 8
 // % 4 = l / 16), so that eight wavefronts share the smallest matrix and a block
 // has four values a lane.  What is read is held in registers until every
@@ -927,7 +880,7 @@ size_t carve_ns(Group *g, int32_t n, void *base) {
     for (int i = 0; i < n; ++i) {
         Group &G = g[i];
         G.part = c.take<double>((size_t)G.count * G.chunks);
-        G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np + 4ll * G.np;
+        G.ops_stride = 8ll * G.np * G.mp + 4ll * G.np * G.np;
         G.ops = c.take<uint16_t>((size_t)G.count * G.ops_stride);
     }
     return c.used;
@@ -1033,22 +986,22 @@ int64_t product_tiles(const Group &G, int T, int mode) {
     return G.count * (mode == kGram || mode == kSquare ? nt * (nt + 1) / 2 : nt * mt);
 }
 
-template <int T, int PARTS, typename OUT>
+template <int T, typename OUT>
 void launch_product(const Group *g, int32_t n, EndSet &B, int mode, hipStream_t st) {
     const unsigned grid = number_blocks(B.g, n, kSet, [&](int i) { return product_tiles(g[i], T, mode); });
     const ProductSet &P = B;
     switch (mode) {
-        case kGram: ns_product<T, PARTS, kGram, OUT><<<grid, 512, 0, st>>>(P); break;
-        case kSquare: ns_product<T, PARTS, kSquare, OUT><<<grid, 512, 0, st>>>(P); break;
-        case kApply: ns_product<T, PARTS, kApply, OUT><<<grid, 512, 0, st>>>(P); break;
-        case kFinal: ns_product<T, PARTS, kFinal, OUT><<<grid, 512, 0, st>>>(B); break;
+        case kGram: ns_product<T, kGram, float><<<grid, 512, 0, st>>>(P); break;
+        case kSquare: ns_product<T, kSquare, float><<<grid, 512, 0, st>>>(P); break;
+        case kApply: ns_product<T, kApply, float><<<grid, 512, 0, st>>>(P); break;
+        case kFinal: ns_product<T, kFinal, OUT><<<grid, 512, 0, st>>>(B); break;
         default:
-            if constexpr (sizeof(OUT) == 4) ns_product<T, PARTS, kUpdate, float><<<grid, 512, 0, st>>>(B);
+            if constexpr (sizeof(OUT) == 4) ns_product<T, kUpdate, float><<<grid, 512, 0, st>>>(B);
     }
 }
 
 // One set: at most kSet matrix groups (already carved) and kSetPlain plain ones.
-template <typename T, bool MUON, int PARTS>
+template <typename T, bool MUON>
 void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, const Options &o, hipStream_t st) {
     NormSet N{};
     N.lr = o.muon.lr; N.momentum = o.muon.momentum; N.decay = o.muon.weight_decay; N.nesterov = o.muon.nesterov != 0;
@@ -1102,7 +1055,7 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
         E.e[i].out = G.out; E.e[i].rows = G.rows; E.e[i].cols = G.cols; E.e[i].factor = G.factor;
     }
     grid = number_blocks(P.g, n, kSet, [&](int i) { return (int64_t)mats[i].count * (mats[i].np / 64) * (mats[i].mp / 64); });
-    ns_prepare<T, MUON, PARTS><<<grid, 256, 0, st>>>(P);
+    ns_prepare<T, MUON><<<grid, 256, 0, st>>>(P);
     // Tiles of 128 x 128 once more than half of the CUs get one, else of 64 x 64.  Always the smaller | from 64 of the
     // larger ones | above 128, us, fp32 (the larger take fewer bytes per product, the smaller spread further): 2 of
     // 1024 x 1024 281 | 372 | 281, 8 of 512 x 512 195 | 255 | 195, 40 of 256 x 256 178 | 207 | 175, 1500 x 1500 416 |
@@ -1110,8 +1063,8 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
     auto product = [&](int mode) {
         int64_t tiles = 0;
         for (int i = 0; i < n; ++i) tiles += product_tiles(mats[i], 128, mode);
-        if (tiles > 128) launch_product<128, PARTS, T>(mats, n, E, mode, st);
-        else launch_product<64, PARTS, T>(mats, n, E, mode, st);
+        if (tiles > 128) launch_product<128, T>(mats, n, E, mode, st);
+        else launch_product<64, T>(mats, n, E, mode, st);
     };
     for (int s = 0; s < o.ns.steps; ++s) {
         E.cur = s & 1;
@@ -1166,11 +1119,11 @@ size_t workspace_of(const G *g, int32_t n) {
     return most;
 }
 
-template <typename T, bool MUON, int PARTS, typename G>
+template <typename T, bool MUON, typename G>
 void run_groups(const G *g, int32_t n, const Options &o, void *workspace, hipStream_t st) {
     for_sets(g, n, [&](Group *mats, int32_t nm, const Group *plain, int32_t np) {
         carve_ns(mats, nm, workspace);
-        run_set<T, MUON, PARTS>(mats, nm, plain, np, o, st);
+        run_set<T, MUON>(mats, nm, plain, np, o, st);
     });
 }
 
@@ -1226,8 +1179,8 @@ extern "C" tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n
     if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const Options o{*ns, {}};
-    if (dtype == TAG_BF16) run_groups<uint16_t, false, 1>(groups, n_groups, o, workspace, stream);
-    else run_groups<float, false, 2>(groups, n_groups, o, workspace, stream);
+    if (dtype == TAG_BF16) run_groups<uint16_t, false>(groups, n_groups, o, workspace, stream);
+    else run_groups<float, false>(groups, n_groups, o, workspace, stream);
     return launch_status("tag_orthogonalise");
 }
 
@@ -1256,6 +1209,6 @@ extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_grou
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_muon_workspace)");
     if (need && (!workspace || (uintptr_t)workspace % 16))
         TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
-    run_groups<float, true, 2>(groups, n_groups, Options{*ns, *options}, workspace, static_cast<hipStream_t>(hip_stream));
+    run_groups<float, true>(groups, n_groups, Options{*ns, *options}, workspace, static_cast<hipStream_t>(hip_stream));
     return launch_status("tag_muon_step");
 }
