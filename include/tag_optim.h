@@ -72,7 +72,7 @@ tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n_groups, in
  * different arrays, and no w or m is part of another group.
  */
 typedef struct tag_muon_group {
-    int32_t count, rows, cols, plain;   /* as above; plain: up to 2^31 elements */
+    int32_t count, rows, cols, plain;   /* as above; plain: up to 2^31 elements, each matrix's rounded up to 4,096 */
     tag_matrices w, g, m;          /* w and m written, g read */
 } tag_muon_group;
 

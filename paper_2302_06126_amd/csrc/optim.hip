@@ -891,7 +891,7 @@ Group shape_ns(int32_t count, int32_t rows, int32_t cols, bool plain) {
     G.count = count; G.rows = rows; G.cols = cols; G.plain = plain;
     G.trans = rows > cols;
     G.n = std::min(rows, cols); G.m = std::max(rows, cols);
-    G.np = (int32_t)up64(G.n); G.mp = (int32_t)up64(G.m);
+    if (!plain) { G.np = (int32_t)up64(G.n); G.mp = (int32_t)up64(G.m); }
     G.chunks = (int32_t)(((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
     return G;
 }
@@ -901,9 +901,10 @@ constexpr int kMaxSide = 32768;   // rows or columns
 tag_status check_shape(int32_t count, int32_t rows, int32_t cols, bool plain) {
     if (count < 1 || rows < 1 || cols < 1) TAG_FAIL(TAG_EINVAL, "need count, rows and cols >= 1");
     if (!plain && (rows > kMaxSide || cols > kMaxSide)) TAG_FAIL(TAG_ESHAPE, "at most 32768 rows or columns");
-    // (a launch has fewer than 2^32 threads, over all groups of its set)
-    const int64_t blocks = std::max((up64(rows) / 64) * (up64(cols) / 64), ((int64_t)rows * cols + kSumChunk - 1) / kSumChunk);
-    if (blocks * count > (1 << 19)) TAG_FAIL(TAG_ESHAPE, "too many or too large matrices in a group");
+    // (a launch has fewer than 2^32 threads, over all groups of its set; plain groups have no tiles)
+    const int64_t chunks = ((int64_t)rows * cols + kSumChunk - 1) / kSumChunk;
+    const int64_t blocks = plain ? chunks : std::max((up64(rows) / 64) * (up64(cols) / 64), chunks);
+    if (blocks > (1 << 19) / count) TAG_FAIL(TAG_ESHAPE, "too many or too large matrices in a group");
     return TAG_OK;
 }
 
