@@ -293,9 +293,11 @@ extern "C" tag_status tag_constrain(int32_t n_query, int32_t n_slices, int32_t d
     A.prior = prior; A.ps = prior_stride;
     A.argmax = argmax; A.best = best;
     A.chunks = (int32_t)std::max<int64_t>(1, con_chunks(n_slices));
-    // (a launch has fewer than 2^32 threads)
+    // (a launch has fewer than 2^32 threads: whole blocks of 256, or of a longer row's team)
     const int64_t team = S <= 256 ? 16 : S <= 1024 ? 64 : S <= 4096 || S > kConWhole ? 256 : S <= 8192 ? 512 : 1024;
-    if ((int64_t)n_query * A.chunks >= ((int64_t)1 << 32) / team) TAG_FAIL(TAG_ESHAPE, "too many rows of this length");
+    const int64_t block = std::max<int64_t>(team, 256), rows = block / team;
+    if (((int64_t)n_query * A.chunks + rows - 1) / rows >= ((int64_t)1 << 32) / block)
+        TAG_FAIL(TAG_ESHAPE, "too many rows of this length");
     size_t need = 0;
     tag_constrain_workspace(n_query, n_slices, &need);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_constrain_workspace)");
