@@ -327,7 +327,7 @@ class Decide:
             torch = _torch()
             self.score = torch.empty((self.Q, self.S), dtype=torch.float32, device=self.graph.device)
             if stream is not None:   # (memory of the current stream)
-                stream.wait_stream(torch.cuda.current_stream())
+                stream.wait_stream(torch.cuda.current_stream(self.graph.device))
         st = tag_gnn_scores(self.graph.handle, self.model.dims, self.model.weights, self.R, _ptr(E_op), _ptr(E_dev),
                             self.slices, self.Q, _ptr(self.q[0]), _ptr(self.q[1]), _ptr(self.q[2]), _ptr(self.score),
                             _ptr(self.ws), self.ws_bytes, _stream(stream))
