@@ -46,7 +46,7 @@ typedef struct tag_matrices {
 
 typedef struct tag_ortho_group {
     int32_t count, rows, cols;     /* sides up to 32768, at most 2^19 tiles of 64 x 64 in all */
-    tag_matrices in, out;          /* out may be in; otherwise written arrays do not overlap */
+    tag_matrices in, out;          /* out may be in, with its strides; otherwise written arrays overlap nothing */
 } tag_ortho_group;
 
 /*

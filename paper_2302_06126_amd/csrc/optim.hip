@@ -922,6 +922,30 @@ tag_status check_array(const tag_matrices &a, int32_t count, int32_t rows, int32
     return TAG_OK;
 }
 
+// Whether two arrays of one shape share an element: exact where their strides are
+// the same (parts of wider rows, say, which interleave); others where their first
+// elements are the same one, and not beyond.
+bool same_place(const tag_matrices &a, const tag_matrices &b, int32_t count, int32_t rows) {
+    return a.base == b.base && (rows == 1 || a.row_stride == b.row_stride) &&
+           (count == 1 || a.matrix_stride == b.matrix_stride);
+}
+bool overlap(const tag_matrices &a, const tag_matrices &b, int32_t count, int32_t rows, int32_t cols, size_t el) {
+    if (a.base == b.base) return true;
+    if ((rows > 1 && a.row_stride != b.row_stride) || (count > 1 && a.matrix_stride != b.matrix_stride)) return false;
+    const int64_t bytes = (int64_t)((uintptr_t)b.base - (uintptr_t)a.base), row = rows > 1 ? a.row_stride : 0,
+                  mat = count > 1 ? a.matrix_stride : 0;
+    const int64_t d = bytes / (int64_t)el;   // (arrays are aligned to their elements)
+    if (std::abs(d) >= (count - 1) * mat + (rows - 1) * row + cols) return false;
+    // d = i mat + j row + k with |i| < count, |j| < rows, |k| < cols
+    for (int64_t i = 1 - count; i < count; ++i) {
+        const int64_t r = d - i * mat;
+        const int64_t j = row > 0 ? std::min<int64_t>(std::max<int64_t>(r / row, 1 - rows), rows - 1) : 0;
+        for (int64_t t = std::max<int64_t>(j - 1, 1 - rows); t <= std::min<int64_t>(j + 1, rows - 1); ++t)
+            if (std::abs(r - t * row) < cols) return true;
+    }
+    return false;
+}
+
 // the largest |p| over [0, hi] of p(s) = s (a + b s^2 + c s^4), or with `poly` of
 // b t + c t^2 over t in [0, hi^2]: at the ends and where the derivative is zero
 double peak(double a, double b, double c, double hi, bool poly) {
@@ -1135,6 +1159,9 @@ tag_status check_ortho_groups(const tag_ortho_group *g, int32_t n, bool arrays, 
         if (st == TAG_OK && arrays) st = check_array(g[i].in, g[i].count, g[i].rows, g[i].cols, el, false, "in");
         if (st == TAG_OK && arrays) st = check_array(g[i].out, g[i].count, g[i].rows, g[i].cols, el, true, "out");
         if (st != TAG_OK) return st;
+        if (arrays && !same_place(g[i].in, g[i].out, g[i].count, g[i].rows) &&
+            overlap(g[i].in, g[i].out, g[i].count, g[i].rows, g[i].cols, el))
+            TAG_FAIL(TAG_EINVAL, "out must be in, matrix by matrix and row by row, or not overlap it");
     }
     return TAG_OK;
 }
@@ -1147,7 +1174,10 @@ tag_status check_muon_groups(const tag_muon_group *g, int32_t n, bool arrays) {
         if (st == TAG_OK && arrays) st = check_array(g[i].w, g[i].count, g[i].rows, g[i].cols, 4, true, "w");
         if (st == TAG_OK && arrays) st = check_array(g[i].m, g[i].count, g[i].rows, g[i].cols, 4, true, "m");
         if (st != TAG_OK) return st;
-        if (arrays && (g[i].w.base == g[i].g.base || g[i].w.base == g[i].m.base || g[i].g.base == g[i].m.base))
+        auto meet = [&](const tag_matrices &a, const tag_matrices &b) {
+            return overlap(a, b, g[i].count, g[i].rows, g[i].cols, 4);
+        };
+        if (arrays && (meet(g[i].w, g[i].g) || meet(g[i].w, g[i].m) || meet(g[i].g, g[i].m)))
             TAG_FAIL(TAG_EINVAL, "w, g and m must be different arrays");
     }
     return TAG_OK;
