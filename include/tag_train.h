@@ -75,7 +75,7 @@ tag_status tag_train_step(const tag_graph *g, const tag_model_dims *dims, const 
  */
 typedef struct tag_train_balance {
     float coef;                      /* finite, >= 0                                    */
-    float *loss;                     /* DEVICE [1]  the balance part of the loss        */
+    float *loss;                     /* DEVICE [1]  the balance part of *loss, elsewhere */
     int32_t *count;                  /* DEVICE [S]  queries whose best slice this is    */
     float *load;                     /* DEVICE [n_dev] load of each device              */
     void *workspace;

@@ -2177,6 +2177,7 @@ tag_status train_run(const tag_graph *g, const tag_model_dims *dims, const tag_w
         if (!(balance->coef >= 0.f) || balance->coef == INFINITY) TAG_FAIL(TAG_EINVAL, "coef must be finite and >= 0");
         if (!balance->loss || !balance->count || !balance->load || !balance->workspace)
             TAG_FAIL(TAG_EINVAL, "balance loss, count, load and workspace must be non-NULL");
+        if (balance->loss == loss) TAG_FAIL(TAG_EINVAL, "the balance part of the loss and the loss must be two places");
         if ((uintptr_t)slices->mask % 8 || (uintptr_t)balance->loss % 4 || (uintptr_t)balance->count % 4 ||
             (uintptr_t)balance->load % 4)
             TAG_FAIL(TAG_EINVAL, "masks, balance loss, count and load must be aligned to their elements");
