@@ -17,7 +17,7 @@ from __future__ import annotations
 
 from typing import Optional, Sequence, Tuple
 
-from . import _abi, _ptr, _torch
+from . import TagError, _abi, _ptr, _torch
 from ._abi import (C, check, tag_muon_group, tag_muon_options, tag_newton_schulz, tag_ortho_group)
 from .policy import _device, _dtype, _launch, _raw_stream
 
@@ -151,7 +151,12 @@ class Muon:
         """One step with the gradients as they stand.  ``lr`` holds for this
         step and the following ones; a step captured into a graph keeps the one
         that it was captured with."""
+        was = self.options.lr
         if lr is not None:
             self.options.lr = float(lr)
-        _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
-                _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))
+        try:
+            _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
+                    _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))
+        except TagError:   # (a rate that was refused is not kept)
+            self.options.lr = was
+            raise
