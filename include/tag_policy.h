@@ -9,7 +9,8 @@
  * validated before anything is enqueued, no allocation.  Row strides are in
  * elements and at least S; rows may start at any element.  A workspace is
  * scratch for the duration of a call (calls that share one must be ordered);
- * nothing in it needs to start at zero.
+ * nothing in it needs to start at zero.  But where a call says so, no array that
+ * it writes overlaps another of its arrays.
  */
 #ifndef TAG_POLICY_H
 #define TAG_POLICY_H
@@ -95,7 +96,8 @@ tag_status tag_constrain(int32_t n_query, int32_t n_slices, int32_t dtype, const
  * Evenly spread decisions over M devices give the least, coef.  Rows that are
  * not used have a zero gradient (their scores are not read where use[q] = 0);
  * with no used row the loss is 0.  A used row with a NaN counts for no slice
- * and makes the loss and its own gradient NaN, as does one of +inf.
+ * and makes the loss and its own gradient NaN; so does one of +inf, which counts
+ * for its slice.
  *
  *   scores  [Q] rows of S <= 16384, TAG_F32 or TAG_BF16
  *   mask    [S] device masks (tag_slices.mask)

@@ -182,8 +182,10 @@ __device__ __forceinline__ float4 get4(const uint16_t *p) {
 
 // Sums of squares of u per kSumChunk elements (in 64 bits: a gradient's squares
 // leave the range of fp32), with the momentum update on the way; plain groups
-// are finished here.  Memory bounds it: 2048 x 2048 fp32 5.7 us (2.9 TB/s, a launch
-// and its tail), 1.7 M parameters of the 256-wide model 11.7 us.
+// are finished here.  Memory bounds whole chunks: 2048 x 2048 fp32 5.7 us (2.9 TB/s,
+// a launch and its tail).  The last chunk of a matrix or vector goes element by
+// element, up to 16 turns of a thread with a memory round trip each: 1.7 M parameters
+// of the 256-wide model, whose vectors and encoders end so, 12.2 us.
 template <typename T, bool MUON>
 __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
     __shared__ double red[4];
@@ -350,12 +352,13 @@ __device__ __forceinline__ void wait_arrival() {
 // than a load from beyond the L2), and a stage's fragments are read from LDS while
 // the last stage's are multiplied.
 //
-// 2048^3: B X 54 us (256 tiles, 950 TFLOP/s of fp16 products; a library's
+// 2048^3: B X 55 us (256 tiles, 940 TFLOP/s of fp16 products; a library's
 // bf16 product of 2048^3 reaches 418, of 8192^3 1,164), of which 43 us of products
 // at the 1.6 GHz that the chip then holds, 70% of their peak at it; X X^T and A A
-// 43 us (136 tiles, half of the CUs, a higher clock).  Around the products a launch
+// 44 to 45 us (136 tiles, half of the CUs, a higher clock).  Around the products a launch
 // takes 2 us to the first load, 1 until it lands, 2 to join the halves of k, 4 to write
-// 34 MB.  Tried without gain: two stages of twice the length instead of four,
+// 34 MB.  Four of 1024 x 4096: B X 124 us (830 TFLOP/s, blocks of 32 stages), X X^T 82
+// (144 tiles).  Tried without gain: two stages of twice the length instead of four,
 // stages' barriers by the compiler (which waits for every load), one wavefront per
 // SIMD (the products wait for LDS: 60 us).
 //

@@ -49,7 +49,8 @@ class Orthogonalise:
     """Orthogonalises matrices of fixed shapes: ``shapes`` is a list of
     (count, rows, cols).  A call takes a tensor [count, rows, cols] for each and
     returns the results, tensors of this object unless ``out`` gives others
-    (they may be the inputs)."""
+    (they may be the inputs, each its own; what is written shares no other
+    memory with anything)."""
 
     def __init__(self, shapes: Sequence[Tuple[int, int, int]], dtype=None, device="cuda", steps: int = 5,
                  coef=QUINTIC, eps: float = 1e-7):
@@ -102,7 +103,8 @@ class Muon:
     """Momentum with orthogonalised updates of ``params``: (weight, gradient)
     pairs of fp32 tensors, updated in place by ``step``.  [rows, cols] and
     [count, rows, cols] are matrices; one-dimensional tensors take plain
-    momentum SGD.  ``state`` gives the momentum tensors (default: zeros)."""
+    momentum SGD.  ``state`` gives the momentum tensors (default: zeros).  No
+    weight or momentum shares memory with another tensor of them."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
                  weight_decay: float = 0.0, steps: int = 5, coef=QUINTIC, eps: float = 1e-7,
