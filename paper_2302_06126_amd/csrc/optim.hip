@@ -19,8 +19,8 @@
 //
 // bf16 matrices take the same products, and their result is rounded once.  With
 // one part of the operands (2^-11 of them) the products of 4 of 1024 x 4096 take
-// 670 us in place of 1,215, but the operands then cost as much as that rounding, and
-// where their roundings agree, as in a matrix of equal values, ten times as much.
+// 670 us in place of 1,215, but the operands then cost about as much as that rounding,
+// and where their roundings agree, as in a matrix of equal values, ten times as much.
 //
 // Layout.  The operands lie in the order in which a 32x32x16 instruction takes
 // them ("fragments": 32 rows x 16 k, lane l holds 8 consecutive k of row l % 32,
@@ -925,13 +925,14 @@ tag_status check_array(const tag_matrices &a, int32_t count, int32_t rows, int32
     return TAG_OK;
 }
 
-// Whether two arrays of one shape share an element: exact where their strides are
-// the same (parts of wider rows, say, which interleave); others where their first
-// elements are the same one, and not beyond.
+// whether two arrays of one shape are the same one, element by element
 bool same_place(const tag_matrices &a, const tag_matrices &b, int32_t count, int32_t rows) {
     return a.base == b.base && (rows == 1 || a.row_stride == b.row_stride) &&
            (count == 1 || a.matrix_stride == b.matrix_stride);
 }
+
+// Whether they share an element: exact where their strides are the same (parts of
+// wider rows, say, which interleave); for others only whether both start at one.
 bool overlap(const tag_matrices &a, const tag_matrices &b, int32_t count, int32_t rows, int32_t cols, size_t el) {
     if (a.base == b.base) return true;
     if ((rows > 1 && a.row_stride != b.row_stride) || (count > 1 && a.matrix_stride != b.matrix_stride)) return false;

@@ -52,7 +52,8 @@ __device__ __forceinline__ void load4(const T *row, int64_t c, int64_t n, float 
 // Results leave by non-temporal stores: rows written through the caches push out
 // those that are still to be read (42,496 x 256 constrained bf16 scores 37 us
 // without, 27 with; 64 x 262,140 79 | 74, balance gradients 38.3 | 37.8).  Rows that
-// are not four columns apart are stored column by column (42,496 x 255: 45 us).
+// do not start at multiples of four columns are stored column by column (42,496 x
+// 255: 45 us).
 template <typename T, bool VEC>
 __device__ __forceinline__ void store4(T *row, int64_t c, int64_t n, const float (&v)[4]) {
     if (VEC && c + 4 <= n) {

@@ -41,9 +41,3 @@ def test_matrices_keep_their_own_limits(abi):
     for shape in [(1, 1, 32769), (3, 32768, 32768), (2 ** 19, 64, 65), (2 ** 19 + 1, 1, 1)]:
         assert _workspace(abi, *shape, plain=0)[0] == ESHAPE
     assert _workspace(abi, 0, 1, 5)[0] == EINVAL
-
-
-def test_no_launch_of_full_groups_reaches_2_32_threads():
-    """Eight groups of matrices and sixteen plain ones at the limit share launches
-    of 256 threads a block (sums, preparation), the matrices those of 512 (products)."""
-    assert (8 + 16) * 2 ** 19 * 256 < 2 ** 32 and 8 * 2 ** 19 * 512 < 2 ** 32
