@@ -36,6 +36,9 @@ SEARCH_EXPORTS = ("tag_search_problem_create", "tag_search_problem_destroy", "ta
 # include/tag_policy.h
 EXPORTS += ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace", "tag_balance")
 
+# include/tag_beam.h
+EXPORTS += ("tag_beam_workspace", "tag_beam_select", "tag_beam_reorder")
+
 # include/tag_train.h
 TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step", "tag_train_balance_workspace", "tag_train_step_balanced",
                  # include/tag_optim.h
@@ -158,6 +161,11 @@ class tag_sim_out(C.Structure):
                 ("link_idle", _PF)]
 
 
+class tag_beam_state(C.Structure):
+    _fields_ = [("in", C.c_void_p), ("out", C.c_void_p), ("row_bytes", C.c_int64), ("in_search", C.c_int64),
+                ("in_beam", C.c_int64), ("out_search", C.c_int64), ("out_beam", C.c_int64)]
+
+
 class tag_decision(C.Structure):
     _fields_ = [("mask", C.c_uint64), ("option", C.c_int32), ("replicas", C.c_int32),
                 ("sync", C.c_int32), ("sfb", C.c_int32)]
@@ -262,8 +270,12 @@ def load() -> C.CDLL:
     lib.tag_balance_workspace.argtypes = [S, S, szp]
     lib.tag_balance.argtypes = [S, S, S, vp, C.c_int64, vp, S, vp, C.c_float, vp, C.c_int64, S, vp, vp, vp, vp,
                                 C.c_size_t, vp]
+    # include/tag_beam.h
+    lib.tag_beam_workspace.argtypes = [S, S, S, S, szp]
+    lib.tag_beam_select.argtypes = [S, S, S, S, S, vp, C.c_int64, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.tag_beam_reorder.argtypes = [S, S, S, vp, C.POINTER(tag_beam_state), S, vp]
     for name in ("tag_gnn_scores", "tag_constrain_workspace", "tag_constrain", "tag_balance_workspace",
-                 "tag_balance"):
+                 "tag_balance", "tag_beam_workspace", "tag_beam_select", "tag_beam_reorder"):
         getattr(lib, name).restype = S
     for name in SEARCH_EXPORTS:
         if name not in ("tag_search_problem_destroy", "tag_mcts_destroy"):

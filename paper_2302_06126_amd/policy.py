@@ -1,10 +1,13 @@
-"""Binding of include/tag_policy.h: operators on the decision head's scores
-(``Decide.scores``).
+"""Binding of include/tag_policy.h and include/tag_beam.h: operators on the
+decision head's scores (``Decide.scores``).
 
   Constrain  priors, argmax and best score under slice masks, biases and
              penalties for slices that a query's history took already
   Balance    the loss that spreads the decisions over the devices, with the
              slices' counts, the devices' loads and the scores' gradient
+  Beam       one level of a beam search: the best continuations of all beams'
+             slices, their parents and slices
+  Reorder    the beams' states, brought into the order of their parents
 
 Argument checks and marshalling only; the operators run in libtag.so's HIP
 kernels.  As with the other reusable calls, an object owns its workspace and
@@ -18,9 +21,9 @@ from __future__ import annotations
 import numpy as np
 
 from . import _abi, _ptr, _torch
-from ._abi import C, TAG_BF16, TAG_F32, check, tag_constraints
+from ._abi import C, TAG_BF16, TAG_F32, check, tag_beam_state, tag_constraints
 
-__all__ = ["Constrain", "Balance"]
+__all__ = ["Constrain", "Balance", "Beam", "Reorder"]
 
 
 def _device(device):
@@ -180,3 +183,109 @@ class Balance:
         _launch(self.device, "tag_balance", self.Q, self.S, self._code, scores.data_ptr(), xs, _ptr(self.masks), self.M,
                 u, float(coef), *self._tail, _raw_stream(stream, self.device))
         return self.loss
+
+
+def _beams(t, what, dtypes, device, n, width):
+    if t.dtype not in dtypes or t.device != device or tuple(t.shape) != (n, width) or not t.is_contiguous():
+        raise ValueError(f"{what} must be {' or '.join(str(d) for d in dtypes)} [{n}, {width}] on {device}, contiguous")
+    return t.data_ptr()
+
+
+class Beam:
+    """One level of ``n_search`` beam searches: ``width`` beams after it,
+    ``width_in`` before it (default: as many).
+
+    A call returns (total [n, width] fp32, parent, slice [n, width] int32), best
+    first.  ``total`` may go into the next level's call as it is.  A finished
+    beam goes on with slice -1; what is left over of the width has parent -1."""
+
+    def __init__(self, n_search: int, width: int, n_slices: int, width_in=None, dtype=None, device="cuda"):
+        torch = _torch()
+        self.dtype = torch.float32 if dtype is None else dtype
+        self._code = _dtype(self.dtype)
+        self.device = dev = _device(device)
+        self.n, self.W, self.S = int(n_search), int(width), int(n_slices)
+        self.V = self.W if width_in is None else int(width_in)
+        b = C.c_size_t(0)
+        check(_abi.load().tag_beam_workspace(self.n, self.V, self.W, self.S, C.byref(b)), "tag_beam_workspace")
+        self.ws_bytes = b.value
+        self.ws = torch.empty(max(b.value, 16), dtype=torch.uint8, device=dev)
+        self.total = torch.empty((self.n, self.W), dtype=torch.float32, device=dev)
+        self.parent = torch.empty((self.n, self.W), dtype=torch.int32, device=dev)
+        self.slice = torch.empty((self.n, self.W), dtype=torch.int32, device=dev)
+        self._out = (self.total, self.parent, self.slice)
+        self._tail = tuple(_ptr(t) for t in self._out) + (_ptr(self.ws), self.ws_bytes)
+
+    def start(self):
+        """This object's ``total`` [n, width], set to what a search starts from:
+        one beam of probability one, the others not there."""
+        self.total.fill_(-float("inf"))
+        self.total[:, :1].zero_()
+        return self.total
+
+    def __call__(self, scores, total, done=None, stream=None):
+        """scores [n width_in, S], a search's beams one after the other; total
+        [n, width_in]; done [n, width_in] (uint8 or bool): finished beams."""
+        torch = _torch()
+        n, V, dev = self.n, self.V, self.device
+        xs = _rows(scores, "scores", (self.dtype,), dev, n * V, self.S)
+        t = _beams(total, "total", (torch.float32,), dev, n, V)
+        d = None if done is None else _beams(done, "done", (torch.uint8, torch.bool), dev, n, V)
+        _launch(dev, "tag_beam_select", n, V, self.W, self.S, self._code, scores.data_ptr(), xs, t, d, *self._tail,
+                _raw_stream(stream, dev))
+        return self._out
+
+
+class Reorder:
+    """Brings the beams' ``states`` into the order of their parents: tensors of
+    any type whose first axis, or first two, are the beams, [n width_in, ...] or
+    [n, width_in, ...], each beam's part contiguous.  ``out`` gives tensors
+    [n width, ...] or [n, width, ...] to write; without it they are reordered in
+    place.  A call takes ``parent`` [n, width] (int32); beams whose parent is not
+    in [0, width_in) keep what they have."""
+
+    def __init__(self, states, n_search: int, width: int, width_in=None, out=None):
+        self.n, self.W = int(n_search), int(width)
+        self.V = self.W if width_in is None else int(width_in)
+        self.states = list(states)
+        self.out = self.states if out is None else list(out)
+        if not self.states or len(self.out) != len(self.states):
+            raise ValueError("states are wanted, and as many outputs")
+        if out is None and self.V != self.W:
+            raise ValueError("states of another width cannot be reordered in place")
+        self.device = self.states[0].device
+        if self.device.type != "cuda":
+            raise ValueError("the operators run on a GPU")
+        self._s = (tag_beam_state * len(self.states))()
+        for s, x, y in zip(self._s, self.states, self.out):
+            row, s_in, b_in = self._layout(x, self.V)
+            row_out, s.out_search, s.out_beam = self._layout(y, self.W)
+            if x.dtype != y.dtype or row != row_out:
+                raise ValueError("an output has the type of its states, and rows of their size")
+            setattr(s, "in", x.data_ptr())
+            s.out, s.row_bytes, s.in_search, s.in_beam = y.data_ptr(), row, s_in, b_in
+
+    def _layout(self, t, width):
+        """Bytes of a row, strides of searches and of beams."""
+        if t.device != self.device:
+            raise ValueError(f"states must be on {self.device}")
+        shape, stride, el = tuple(t.shape), t.stride(), t.element_size()
+        if len(shape) >= 1 and shape[0] == self.n * width:
+            lead, search, beam = 1, width * stride[0], stride[0]
+        elif len(shape) >= 2 and shape[:2] == (self.n, width):
+            lead, (search, beam) = 2, stride[:2]
+        else:
+            raise ValueError(f"states must have the shape [{self.n * width}, ...] or [{self.n}, {width}, ...], not "
+                             f"{list(shape)}")
+        row = 1
+        for size, step in zip(shape[:lead - 1:-1], stride[:lead - 1:-1]):
+            if size != 1 and step != row:
+                raise ValueError("each beam's part of the states must be contiguous")
+            row *= size
+        return row * el, search * el, beam * el
+
+    def __call__(self, parent, stream=None):
+        p = _beams(parent, "parent", (_torch().int32,), self.device, self.n, self.W)
+        _launch(self.device, "tag_beam_reorder", self.n, self.V, self.W, p, self._s, len(self.states),
+                _raw_stream(stream, self.device))
+        return self.out
