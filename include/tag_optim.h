@@ -2,7 +2,8 @@
  * tag_optim.h -- C ABI of the orthogonalised optimiser step: Newton-Schulz
  * products that bring a matrix's singular values near one, and the update of
  * weight matrices by the orthogonalised momentum of their gradients, the
- * matrix counterpart of the SGD update of tag_train_step.
+ * matrix counterpart of the SGD update of tag_train_step; and the clipping of
+ * gradients by their global norm.
  *
  * Conventions follow tag.h: caller-owned DEVICE buffers, asynchronous on
  * hip_stream, arguments validated before anything is enqueued, no allocation.
@@ -79,11 +80,59 @@ typedef struct tag_muon_group {
 typedef struct tag_muon_options {
     float lr, momentum, weight_decay;   /* lr >= 0, momentum in [0, 1), weight_decay >= 0 */
     int32_t nesterov;
+    const float *clip;             /* NULL, or DEVICE {norm, scale} as tag_clip writes them for these gradients: the   */
+                                   /* step takes scale g for g (one more rounding of fp32); with a norm that is not    */
+                                   /* finite it leaves weights and momentum as they are                                */
 } tag_muon_options;
 
 tag_status tag_muon_workspace(const tag_muon_group *groups, int32_t n_groups, size_t *bytes);
 tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
                          const tag_muon_options *options, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Clipping by the global norm, over all elements of all arrays of a plan:
+ *   norm  = sqrt(sum g^2)                          (64 bits; result: fp32)
+ *   scale = norm > max_norm ? max_norm / norm : 1  (rounded to fp32)
+ *   out   = scale g                                (rounded to fp32, then to the array's type)
+ * A norm that is not finite as fp32 (an infinity or a NaN among the gradients, or
+ * values near the end of fp32's range) gives scale 0 and an out of zeros: the
+ * gradients of that step are dropped, as norm tells.
+ *
+ * Row r, column c of an array stand at g[r g_stride + c] and out[r out_stride + c]
+ * (strides in elements, at least cols; a vector is one row).  out may be g, with
+ * its stride (then nothing is written where scale is 1), or NULL: the array
+ * counts for the norm only.  Arrays of both types may stand in one plan; any
+ * alignment of their elements will do.  What is written overlaps nothing else.
+ */
+typedef struct tag_clip_array {
+    const void *g;
+    void *out;
+    int64_t rows, cols, g_stride, out_stride;   /* rows, cols >= 0 */
+    int32_t dtype;                 /* TAG_F32 or TAG_BF16 */
+} tag_clip_array;
+
+/* A plan of the arrays, on the HOST; filled by tag_clip_prepare, read by tag_clip. */
+typedef struct tag_clip_plan {
+    const void *table;             /* the DEVICE table */
+    int64_t chunks;                /* entries of it */
+    int32_t writes;                /* 1: some array has an out elsewhere than at g, 2: none has, but some at g */
+} tag_clip_plan;
+
+/*
+ * Lays the table out that tag_clip reads, tag_clip_table_bytes of DEVICE memory,
+ * which outlives the plan.  `arrays` (HOST) is read during the call; their
+ * addresses stay those of the plan.  Synchronises hip_stream once (so it cannot
+ * be captured; tag_clip can).
+ */
+tag_status tag_clip_table_bytes(const tag_clip_array *arrays, int32_t n_arrays, size_t *bytes);
+tag_status tag_clip_prepare(const tag_clip_array *arrays, int32_t n_arrays, void *table, size_t table_bytes,
+                            void *hip_stream, tag_clip_plan *plan);
+
+/* Clips.  max_norm >= 0 (infinity: the norm alone, scale 1).  result: DEVICE [2],
+ * norm and scale. */
+tag_status tag_clip_workspace(size_t *bytes);
+tag_status tag_clip(const tag_clip_plan *plan, float max_norm, float *result, void *workspace, size_t ws_bytes,
+                    void *hip_stream);
 
 #ifdef __cplusplus
 }

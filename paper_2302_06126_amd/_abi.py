@@ -42,7 +42,8 @@ EXPORTS += ("tag_beam_workspace", "tag_beam_select", "tag_beam_reorder")
 # include/tag_train.h
 TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step", "tag_train_balance_workspace", "tag_train_step_balanced",
                  # include/tag_optim.h
-                 "tag_orthogonalise_workspace", "tag_orthogonalise", "tag_muon_workspace", "tag_muon_step")
+                 "tag_orthogonalise_workspace", "tag_orthogonalise", "tag_muon_workspace", "tag_muon_step",
+                 "tag_clip_table_bytes", "tag_clip_prepare", "tag_clip_workspace", "tag_clip")
 
 # kernel stages (include/tag_profile.h)
 STAGE_NAMES = ("graph_build", "encode", "transform", "agg_op_op", "agg_op_dev", "agg_dev_op", "agg_dev_merge",
@@ -132,7 +133,17 @@ class tag_muon_group(C.Structure):
 
 
 class tag_muon_options(C.Structure):
-    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32)]
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32),
+                ("clip", C.c_void_p)]
+
+
+class tag_clip_array(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("g_stride", C.c_int64), ("out_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class tag_clip_plan(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("chunks", C.c_int64), ("writes", C.c_int32)]
 
 
 class tag_search_problem_desc(C.Structure):
@@ -249,6 +260,10 @@ def load() -> C.CDLL:
     lib.tag_muon_workspace.argtypes = [C.POINTER(tag_muon_group), S, szp]
     lib.tag_muon_step.argtypes = [C.POINTER(tag_muon_group), S, C.POINTER(tag_newton_schulz),
                                   C.POINTER(tag_muon_options), vp, C.c_size_t, vp]
+    lib.tag_clip_table_bytes.argtypes = [C.POINTER(tag_clip_array), S, szp]
+    lib.tag_clip_prepare.argtypes = [C.POINTER(tag_clip_array), S, vp, C.c_size_t, vp, C.POINTER(tag_clip_plan)]
+    lib.tag_clip_workspace.argtypes = [szp]
+    lib.tag_clip.argtypes = [C.POINTER(tag_clip_plan), C.c_float, vp, vp, C.c_size_t, vp]
     for name in TRAIN_EXPORTS:
         getattr(lib, name).restype = S
     lib.tag_gnn_decide_full_workspace.argtypes = [vp, C.POINTER(tag_model_dims), S, S, szp]

@@ -5,6 +5,7 @@
 #include <string>
 
 #include "../../include/tag_beam.h"
+#include "areas.hpp"
 #include "policy_rows.hpp"
 
 namespace tag {
@@ -332,19 +333,7 @@ tag_status check_select(int32_t n, int32_t V, int32_t W, int32_t S) {
     return TAG_OK;
 }
 
-// bytes from b up to e, of rows that repeat every `step` (0: one run)
-struct Area {
-    uintptr_t b, e;
-    int64_t step, run;
-    bool meets(const Area &o) const {
-        if (!(b < e && o.b < o.e && b < o.e && o.b < e)) return false;
-        if (step == 0 || step != o.step) return true;
-        const int64_t d = (int64_t)((o.b - b) % (uintptr_t)step);   // columns of wider rows, side by side
-        const int64_t back = o.b >= b ? d : (step - (int64_t)((b - o.b) % (uintptr_t)step)) % step;
-        return back < run || back + o.run > step;
-    }
-};
-Area flat(const void *p, size_t bytes) { return Area{(uintptr_t)p, (uintptr_t)p + (p ? bytes : 0), 0, 0}; }
+// rows of states
 Area area(const void *p, int64_t n, int64_t rows, int64_t search, int64_t beam, int64_t row) {
     const int64_t span = (n - 1) * search + (rows - 1) * beam + row;
     const bool even = rows == 1 || n == 1 || (beam > 0 && search % beam == 0);   // (steps of 0 are no columns)
@@ -384,8 +373,8 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
         TAG_FAIL(TAG_EINVAL, "an array is not aligned to its elements");
     const int64_t rows = (int64_t)n_search * width_in;
     const size_t wide = (size_t)n_search * width * 4;
-    const Area in[3] = {flat(scores, ((rows - 1) * score_stride + n_slices) * el), flat(done, rows), flat(total_in, rows * 4)};
-    const Area out[3] = {flat(parent, wide), flat(slice, wide), flat(total, wide)};
+    const Area in[3] = {flat_area(scores, ((rows - 1) * score_stride + n_slices) * el), flat_area(done, rows), flat_area(total_in, rows * 4)};
+    const Area out[3] = {flat_area(parent, wide), flat_area(slice, wide), flat_area(total, wide)};
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 3; ++i)
             if (out[o].meets(in[i]) && !(o == 2 && i == 2 && total == total_in && width == width_in))
@@ -427,8 +416,8 @@ extern "C" tag_status tag_beam_reorder(int32_t n_search, int32_t width_in, int32
         if ((width > 1 && s.out_beam < s.row_bytes) || (n > 1 && s.out_search < span &&
             !(s.out_search >= s.row_bytes && (width == 1 || s.out_beam >= (n - 1) * s.out_search + s.row_bytes))))
             TAG_FAIL(TAG_EINVAL, "rows of out overlap");
-        in[i] = s.row_bytes ? area(s.in, n, width_in, s.in_search, s.in_beam, s.row_bytes) : flat(nullptr, 0);
-        out[i] = s.row_bytes ? area(s.out, n, width, s.out_search, s.out_beam, s.row_bytes) : flat(nullptr, 0);
+        in[i] = s.row_bytes ? area(s.in, n, width_in, s.in_search, s.in_beam, s.row_bytes) : flat_area(nullptr, 0);
+        out[i] = s.row_bytes ? area(s.out, n, width, s.out_search, s.out_beam, s.row_bytes) : flat_area(nullptr, 0);
         if (s.in == s.out && s.row_bytes > 0) {
             const int32_t rows = std::max(width, width_in);
             const bool strides = (rows == 1 || s.in_beam == s.out_beam) && (n == 1 || s.in_search == s.out_search);
@@ -438,7 +427,7 @@ extern "C" tag_status tag_beam_reorder(int32_t n_search, int32_t width_in, int32
             TAG_FAIL(TAG_EINVAL, "out must be in, row by row, or not overlap it");
         }
     }
-    const Area par = flat(parent, (size_t)n * width * 4);
+    const Area par = flat_area(parent, (size_t)n * width * 4);
     for (int32_t i = 0; i < n_states; ++i) {
         if (out[i].meets(par)) TAG_FAIL(TAG_EINVAL, "out overlaps parent");
         for (int32_t j = 0; j < n_states; ++j)

@@ -83,6 +83,7 @@ struct NormSet {
     int32_t n_groups;
     float lr, momentum, decay;
     int32_t nesterov;
+    const float *clip;
 };
 struct PrepGroup {
     Arr in, mom;
@@ -95,6 +96,7 @@ struct PrepSet {
     PrepGroup g[kSet];
     float eps, momentum;
     int32_t nesterov;
+    const float *clip;
 };
 struct ProductGroup {
     uint16_t *ops;
@@ -122,10 +124,12 @@ struct SmallSet {
     int32_t steps;
     float lr, momentum, decay;
     int32_t nesterov;
+    const float *clip;
 };
 struct EndSet : ProductSet {     // of the last product
     EndGroup e[kSet];
     float lr, decay;
+    const float *clip;
 };
 
 // operands of a matrix: X and X^T of both buffers (hi, lo planes), A, B
@@ -151,6 +155,11 @@ __device__ __forceinline__ int find_group(const G (&g)[N], int n, int32_t &bid) 
     bid -= first;
     return at;
 }
+
+// norm and scale of clipped gradients: what the step takes of them (1 without), and
+// whether it is left out, which every launch of it decides alike
+__device__ __forceinline__ float clip_scale(const float *clip) { return clip ? clip[1] : 1.f; }
+__device__ __forceinline__ bool clip_drops(const float *clip) { return clip && !(clip[0] < INFINITY); }
 
 // two parts of 2^12 x
 __device__ __forceinline__ void split2(float x0, float x1, unsigned &hi, unsigned &lo) {
@@ -195,9 +204,11 @@ __global__ void __launch_bounds__(256) ns_norm(NormSet B) {
     const T *in = static_cast<const T *>(G.in.p) + mat * G.in.mat;
     float *mom = MUON ? static_cast<float *>(G.mom.p) + mat * G.mom.mat : nullptr;
     float *w = MUON && G.plain ? static_cast<float *>(G.out.p) + mat * G.out.mat : nullptr;
-    const float keep = 1.f - B.lr * B.decay;
+    if (MUON && clip_drops(B.clip)) return;
+    const float keep = 1.f - B.lr * B.decay, gs = MUON ? clip_scale(B.clip) : 1.f;
     // the momentum and u of one element, or the whole step of a plain one
     auto step = [&](float g, float &m, float &wt) {
+        g *= gs;
         m = fmaf(B.momentum, m, g);
         const float u = B.nesterov ? fmaf(B.momentum, m, g) : m;
         wt = keep * wt - B.lr * u;
@@ -268,6 +279,7 @@ __global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
     const float *mom = MUON ? static_cast<const float *>(G.mom.p) + mat * G.mom.mat : nullptr;
     // 16 threads to a row of the tile, four columns each
     const int a = threadIdx.x >> 4, b = (threadIdx.x & 15) * 4;
+    const float gs = MUON ? clip_scale(B.clip) : 1.f;
     float u[4][4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -292,7 +304,7 @@ __global__ void __launch_bounds__(256) ns_prepare(PrepSet B) {
         }
         if (MUON)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[k][i] = B.nesterov ? fmaf(B.momentum, m[i], u[k][i]) : m[i];
+            for (int i = 0; i < 4; ++i) u[k][i] = B.nesterov ? fmaf(B.momentum, m[i], u[k][i] * gs) : m[i];
     }
     double s = 0.0;
     for (int c = threadIdx.x; c < G.chunks; c += 256) s += G.part[(int64_t)mat * G.chunks + c];
@@ -650,6 +662,7 @@ __global__ void __launch_bounds__(512, T == 64 ? 4 : 2) ns_product(typename SetO
         const int64_t r0 = (int64_t)(trans ? J : I) * T, c0 = (int64_t)(trans ? I : J) * T;
         const int sr = trans ? 1 : P, sc = trans ? P : 1;
         const float keep = 1.f - B.lr * B.decay, rate = B.lr * E.factor;
+        if (MODE == kUpdate && clip_drops(B.clip)) return;
 #pragma unroll 4
         for (int e = threadIdx.x; e < T * T; e += 512) {
             const int r = e / T, c = e % T;
@@ -693,6 +706,8 @@ __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
     const int n = trans ? G.cols : G.rows, m = trans ? G.rows : G.cols, kx = G.mp / 32;   // fragments along a row of X
     const T *in = static_cast<const T *>(G.in.p) + bid * G.in.mat;
     float *mom = MUON ? static_cast<float *>(G.mom.p) + bid * G.mom.mat : nullptr;
+    if (MUON && clip_drops(B.clip)) return;
+    const float gs = MUON ? clip_scale(B.clip) : 1.f;
     // pieces of eight consecutive j of a row i, 64 threads to a fragment
     float u[MB][8];
     double s = 0.0;
@@ -707,6 +722,7 @@ __global__ void __launch_bounds__(512) ns_small(SmallSet B) {
                 const int64_t r = trans ? j : i, c = trans ? i : j;
                 float g = get(in + r * G.in.row + c);
                 if (MUON) {
+                    g *= gs;
                     float *mp = mom + r * G.mom.row + c;
                     const float v = fmaf(B.momentum, *mp, g);
                     *mp = v;
@@ -1034,6 +1050,7 @@ template <typename T, bool MUON>
 void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, const Options &o, hipStream_t st) {
     NormSet N{};
     N.lr = o.muon.lr; N.momentum = o.muon.momentum; N.decay = o.muon.weight_decay; N.nesterov = o.muon.nesterov != 0;
+    N.clip = o.muon.clip;
     // matrices of at most 64 x 256 alone: one launch for all of them
     int32_t wide = 0;
     for (int i = 0; i < n; ++i) wide = std::max(wide, mats[i].np > 64 ? INT32_MAX : mats[i].mp);
@@ -1052,7 +1069,7 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
     if (small) {
         SmallSet S{};
         S.a = o.ns.a; S.b = o.ns.b; S.c = o.ns.c; S.eps = o.ns.eps; S.steps = o.ns.steps;
-        S.lr = N.lr; S.momentum = N.momentum; S.decay = N.decay; S.nesterov = N.nesterov;
+        S.lr = N.lr; S.momentum = N.momentum; S.decay = N.decay; S.nesterov = N.nesterov; S.clip = N.clip;
         for (int i = 0; i < n; ++i) {
             const Group &G = mats[i];
             SmallGroup &K = S.g[i];
@@ -1071,9 +1088,9 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
     ns_norm<T, MUON><<<grid, 256, 0, st>>>(N);
     if (norms == 0) return;
     PrepSet P{};
-    P.eps = o.ns.eps; P.momentum = N.momentum; P.nesterov = N.nesterov;
+    P.eps = o.ns.eps; P.momentum = N.momentum; P.nesterov = N.nesterov; P.clip = N.clip;
     EndSet E{};
-    E.a = o.ns.a; E.b = o.ns.b; E.c = o.ns.c; E.lr = o.muon.lr; E.decay = o.muon.weight_decay;
+    E.a = o.ns.a; E.b = o.ns.b; E.c = o.ns.c; E.lr = o.muon.lr; E.decay = o.muon.weight_decay; E.clip = o.muon.clip;
     for (int i = 0; i < n; ++i) {
         const Group &G = mats[i];
         PrepGroup &K = P.g[i];
@@ -1240,6 +1257,7 @@ extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_grou
     if (!(options->momentum >= 0.f && options->momentum < 1.f)) TAG_FAIL(TAG_EINVAL, "momentum must be in [0, 1)");
     if (!(options->weight_decay >= 0.f) || !std::isfinite(options->weight_decay))
         TAG_FAIL(TAG_EINVAL, "weight_decay must be finite and >= 0");
+    if ((uintptr_t)options->clip % 4) TAG_FAIL(TAG_EINVAL, "clip must be aligned to its elements");
     const size_t need = workspace_of(groups, n_groups);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_muon_workspace)");
     if (need && (!workspace || (uintptr_t)workspace % 16))

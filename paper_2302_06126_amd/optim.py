@@ -1,12 +1,16 @@
-"""Binding of include/tag_optim.h: orthogonalised updates.
+"""Binding of include/tag_optim.h: orthogonalised updates, clipped gradients.
 
   Orthogonalise   Newton-Schulz products that bring the singular values of
                   matrices near one
+  Clip            the norm over all gradients and, where it is above a limit,
+                  the gradients scaled down to it.  ``Clip.of(trainer, limit)``
+                  takes a Trainer's
   Muon            the optimiser step around them: momentum, the orthogonalised
                   update of weight matrices, momentum SGD for everything else.
                   ``Muon.of(trainer)`` takes a Trainer's parameters and
                   gradients; a training step is then ``trainer.step(feats)``
-                  followed by ``muon.step()``.
+                  followed by ``muon.step()``; with ``max_norm`` the step is
+                  that of the clipped gradients.
 
 Argument checks and marshalling only; everything runs in libtag.so's HIP
 kernels.  An object owns its workspace: its calls must be ordered.  It is memory
@@ -18,10 +22,11 @@ from __future__ import annotations
 from typing import Optional, Sequence, Tuple
 
 from . import TagError, _abi, _ptr, _torch
-from ._abi import (C, check, tag_muon_group, tag_muon_options, tag_newton_schulz, tag_ortho_group)
+from ._abi import (C, check, tag_clip_array, tag_clip_plan, tag_muon_group, tag_muon_options, tag_newton_schulz,
+                   tag_ortho_group)
 from .policy import _device, _dtype, _launch, _raw_stream
 
-__all__ = ["Orthogonalise", "orthogonalise", "Muon", "QUINTIC"]
+__all__ = ["Orthogonalise", "orthogonalise", "Clip", "Muon", "QUINTIC"]
 
 # coefficients of the quintic whose steps bring singular values from 0.01 and more to about [0.7, 1.2]
 QUINTIC = (3.4445, -4.7750, 2.0315)
@@ -99,16 +104,97 @@ def orthogonalise(x, steps: int = 5, coef=QUINTIC, eps: float = 1e-7):
     return call([x])[0].reshape(x.shape)
 
 
+def _pieces(g, out):
+    """Runs of (g, out, rows, cols, row strides) that make up a tensor and its
+    output (or None): axes that follow one another in memory are one."""
+    axes = [[n, s, t] for n, s, t in zip(g.shape, g.stride(), g.stride() if out is None else out.stride()) if n != 1]
+    merged = []
+    for n, s, t in axes:
+        if merged and merged[-1][1] == n * s and merged[-1][2] == n * t:
+            merged[-1] = [merged[-1][0] * n, s, t]
+        else:
+            merged.append([n, s, t])
+    if merged and (merged[-1][1] != 1 or merged[-1][2] != 1):
+        if len(merged) > 1 and g.shape[-1] != 1:
+            raise ValueError("gradients must have unit stride along a row")
+        merged.append([1, 1, 1])   # (single elements)
+    cols = merged.pop()[0] if merged else 1
+    rows, gs, os = merged.pop() if merged else (1, cols, cols)
+    starts = [(0, 0)]
+    for n, s, t in merged:
+        starts = [(a + i * s, b + i * t) for a, b in starts for i in range(n)]
+    el = g.element_size()
+    return [(_ptr(g) + a * el, None if out is None else _ptr(out) + b * el, rows, cols, gs, os) for a, b in starts]
+
+
+class Clip:
+    """Clips ``grads``, fp32 and bf16 tensors, by their global norm: in place, or
+    into the tensors ``out`` (``out=False``: the norm and the scale alone).
+
+    A call returns the norm [1] (fp32); ``scale`` [1] is what the gradients were
+    multiplied with.  A norm that is not finite drops them: scale 0, and zeros.
+    The tensors stay where they are for the object's life."""
+
+    def __init__(self, grads, max_norm: float, out=None):
+        torch = _torch()
+        self.grads = list(grads)
+        if not self.grads:
+            raise ValueError("no gradients")
+        self.device = self.grads[0].device
+        if self.device.type != "cuda":
+            raise ValueError("the operators run on a GPU")
+        self.out = self.grads if out is None else [None] * len(self.grads) if out is False else list(out)
+        if len(self.out) != len(self.grads):
+            raise ValueError("one output per gradient is wanted")
+        self.max_norm = float(max_norm)
+        arrays = []
+        for g, y in zip(self.grads, self.out):
+            if g.device != self.device or (y is not None and (y.device != self.device or y.shape != g.shape
+                                                              or y.dtype != g.dtype)):
+                raise ValueError(f"gradients must be on {self.device}, an output of its gradient's shape and type")
+            code = _dtype(g.dtype)
+            arrays += [tag_clip_array(*p, code) for p in (_pieces(g, y) if g.numel() else [])]
+        n = len(arrays)
+        arrays = (tag_clip_array * max(n, 1))(*arrays)
+        lib, b = _abi.load(), C.c_size_t(0)
+        check(lib.tag_clip_table_bytes(arrays, n, C.byref(b)), "tag_clip_table_bytes")
+        self.table = torch.empty(max(b.value, 16), dtype=torch.uint8, device=self.device)
+        self._plan = tag_clip_plan()
+        _launch(self.device, "tag_clip_prepare", arrays, n, _ptr(self.table), b.value, _raw_stream(None, self.device),
+                C.byref(self._plan))
+        check(lib.tag_clip_workspace(C.byref(b)), "tag_clip_workspace")
+        self.ws_bytes = b.value
+        self.ws = torch.empty(b.value, dtype=torch.uint8, device=self.device)
+        self.result = torch.zeros(2, dtype=torch.float32, device=self.device)
+        self.norm, self.scale = self.result[:1], self.result[1:]
+        self._args = (_ptr(self.result), _ptr(self.ws), self.ws_bytes)
+
+    @classmethod
+    def of(cls, trainer, max_norm: float, **kw):
+        """Every gradient of ``trainer``."""
+        return cls(list(trainer.grads.values()), max_norm, **kw)
+
+    def __call__(self, max_norm: Optional[float] = None, stream=None):
+        """``max_norm`` in place of the object's, for this call."""
+        _launch(self.device, "tag_clip", C.byref(self._plan), self.max_norm if max_norm is None else float(max_norm),
+                *self._args, _raw_stream(stream, self.device))
+        return self.norm
+
+
 class Muon:
     """Momentum with orthogonalised updates of ``params``: (weight, gradient)
     pairs of fp32 tensors, updated in place by ``step``.  [rows, cols] and
     [count, rows, cols] are matrices; one-dimensional tensors take plain
     momentum SGD.  ``state`` gives the momentum tensors (default: zeros).  No
-    weight or momentum shares memory with another tensor of them."""
+    weight or momentum shares memory with another tensor of them.
+
+    With ``max_norm`` a step takes the gradients as ``Clip`` would scale them
+    (the tensors themselves stay); ``norm`` [1] is their norm.  Where it is not
+    finite, the step leaves weights and momentum as they are."""
 
     def __init__(self, params, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True,
                  weight_decay: float = 0.0, steps: int = 5, coef=QUINTIC, eps: float = 1e-7,
-                 state: Optional[Sequence] = None):
+                 state: Optional[Sequence] = None, max_norm: Optional[float] = None):
         torch = _torch()
         self.params = [(w, g) for w, g in params]
         if not self.params:
@@ -138,6 +224,11 @@ class Muon:
         check(_abi.load().tag_muon_workspace(self._g, len(self.params), C.byref(b)), "tag_muon_workspace")
         self.ws_bytes = b.value
         self.ws = torch.empty(max(b.value, 16), dtype=torch.uint8, device=self.device)
+        self.clip = self.norm = None
+        if max_norm is not None:
+            self.clip = Clip([g for _, g in self.params], max_norm, out=False)
+            self.norm = self.clip.norm
+            self.options.clip = _ptr(self.clip.result)
 
     @classmethod
     def of(cls, trainer, **kw):
@@ -157,6 +248,8 @@ class Muon:
         if lr is not None:
             self.options.lr = float(lr)
         try:
+            if self.clip is not None:
+                self.clip(stream=stream)
             _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
                     _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))
         except TagError:   # (a rate that was refused is not kept)

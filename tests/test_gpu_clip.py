@@ -1,0 +1,273 @@
+"""Clipping by the global norm on the GPU.
+
+Tolerances: the sum of squares is formed in 64 bits, N positive terms, so the norm
+is off by at most N 2^-53 of it before it is rounded to fp32, by half a step
+(2^-24); so is the scale.  What the gradients become follows from the scale that
+the call gives by one product in fp32 and, for bf16, one more rounding: exact.
+"""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    assert torch.cuda.is_available()
+    return torch
+
+
+def _norm(tensors):
+    return float(np.sqrt(sum((t.double() ** 2).sum().item() for t in tensors)))
+
+
+def _near(got, want, n):
+    assert abs(got - want) <= (2.0 ** -24 + n * 2.0 ** -53) * want + 2.0 ** -149, (got, want)
+
+
+def _scaled(torch, t, scale):
+    return (t.float() * torch.tensor(scale, dtype=torch.float32)).to(t.dtype)
+
+
+def _check(torch, call, before, outs, limit, untouched=()):
+    """One call of a Clip made of `before`'s copies."""
+    norm, scale = call().item(), call.scale.item()
+    n = sum(t.numel() for t in before)
+    want = _norm(before)
+    _near(norm, want, n)
+    limit = float(np.float32(limit))
+    if want > limit:
+        _near(scale, limit / want, n)
+    else:
+        assert scale == 1.0
+    for t, y in zip(before, outs):
+        assert torch.equal(y.cpu(), _scaled(torch, t, scale))
+
+
+SHAPES = [[(1,)], [(1,), (2,), (3,)], [(4095,), (4096,), (4097,), (8191,), (8192,), (8193,)], [(64, 42), (128, 8), (7, 3, 5)],
+          [(0,), (5,), (3, 0)], [(1000, 1000), (33,), (2, 2, 2, 2)], [()]]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("place", [True, False])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+@pytest.mark.parametrize("limit", [0.3, 2.0])
+def test_shapes(torch, case, place, dtype, limit):
+    from paper_2302_06126_amd.optim import Clip
+    gen = torch.Generator().manual_seed(case)
+    kinds = {"f32": [torch.float32], "bf16": [torch.bfloat16], "mixed": [torch.bfloat16, torch.float32]}[dtype]
+    before = [torch.randn(s, generator=gen).to(kinds[i % len(kinds)]) for i, s in enumerate(SHAPES[case])]
+    g = [t.cuda() for t in before]
+    out = None if place else [torch.full_like(t, 7.0) for t in g]
+    bound = limit * _norm(before)
+    call = Clip(g, bound, out=out)
+    _check(torch, call, before, g if place else out, bound)
+    if not place:
+        assert all(torch.equal(a.cpu(), b) for a, b in zip(g, before))
+
+
+@pytest.mark.parametrize("place", [True, False])
+def test_strides_and_starts(torch, place):
+    """Rows of wider tensors, starts at any element, single elements apart, parts
+    side by side; what stands between them stays."""
+    from paper_2302_06126_amd.optim import Clip
+    for dtype in (torch.float32, torch.bfloat16):
+        gen = torch.Generator(device="cuda").manual_seed(5)
+        rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(dtype)
+        wide, flat, deep, far = rnd(37, 1500), rnd(40000), rnd(4, 9, 30), rnd(90, 7)
+        views = [wide[:, 3:45], wide[:, 45:46], wide[:, 47:1300], flat[1:1000], flat[1001:20001], flat[20003:], deep[:, 1:, 2:29],
+                 far[:, 3]]
+        spare = lambda t: torch.full([s + 3 for s in t.shape], 7.0, device="cuda", dtype=dtype)[tuple(slice(1, 1 + s) for s in t.shape)]
+        outs = None if place else [spare(v) for v in views]
+        before = [v.clone().cpu() for v in views]
+        kept = [t.clone() for t in (wide, flat, deep, far)]
+        bound = 0.4 * _norm(before)
+        _check(torch, Clip(views, bound, out=outs), before, views if place else outs, bound)
+        if place:
+            for v, b in zip(views, before):
+                v.copy_(b.cuda())
+        assert all(torch.equal(a, b) for a, b in zip((wide, flat, deep, far), kept))
+        if not place:
+            for o in outs:
+                base = o._base
+                base[tuple(slice(1, 1 + s) for s in o.shape)] = 7.0
+                assert (base == 7.0).all()
+
+
+def test_thousands_of_tensors(torch):
+    from paper_2302_06126_amd.optim import Clip
+    rng = np.random.default_rng(3)
+    before = [torch.randn(int(n)).to(torch.bfloat16 if i % 3 else torch.float32)
+              for i, n in enumerate(np.exp(rng.uniform(0, np.log(30000), 3000)))]
+    g = [t.cuda() for t in before]
+    bound = 0.1 * _norm(before)
+    _check(torch, Clip(g, bound), before, g, bound)
+
+
+def test_values_at_the_ends_of_the_range(torch):
+    from paper_2302_06126_amd.optim import Clip
+    for values, limit in (([1e-45, 3e-45], 1e-45), ([1e-30] * 5, 1e-30), ([1e30, -2e30, 1e25], 1.0), ([3e38], 1e38),
+                          ([1e-20, 1e20], 5.0), ([0.0, -0.0], 0.0), ([0.0, 2.0], 0.0)):
+        before = [torch.tensor(values, dtype=torch.float32)]
+        g = [before[0].cuda()]
+        _check(torch, Clip(g, limit), before, g, limit)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_norms_that_are_not_finite_drop_the_gradients(torch, bad):
+    from paper_2302_06126_amd.optim import Clip
+    for dtype in (torch.float32, torch.bfloat16):
+        before = [torch.randn(5000).to(dtype), torch.randn(7, 9).to(dtype)]
+        before[1][6, 8] = bad
+        g = [t.cuda() for t in before]
+        norm = Clip(g, 1.0, out=False)()
+        assert not np.isfinite(norm.item()) and np.isnan(norm.item()) == np.isnan(bad)
+        assert all(torch.equal(a.cpu().nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(g, before))
+        outs = [torch.full_like(t, 7.0) for t in g]
+        call = Clip(g, 1.0, out=outs)
+        call()
+        assert call.scale.item() == 0.0 and all((o == 0).all() for o in outs)
+        call = Clip(g, 1.0)
+        call()
+        assert all((t == 0).all() for t in g)
+    big = [torch.full((100,), 3e38, device="cuda")]   # a norm past fp32's range
+    call = Clip(big, 1.0)
+    assert call().item() == float("inf") and call.scale.item() == 0.0 and (big[0] == 0).all()
+
+
+def test_limits_of_zero_and_infinity_and_of_a_call(torch):
+    from paper_2302_06126_amd.optim import Clip
+    t = torch.randn(300, device="cuda")
+    was = t.clone()
+    call = Clip([t], float("inf"))
+    _near(call().item(), _norm([was]), 300)
+    assert call.scale.item() == 1.0 and torch.equal(t, was)
+    call(0.5)
+    assert torch.equal(t.cpu(), _scaled(torch, was.cpu(), call.scale.item())) and abs(_norm([t]) - 0.5) < 1e-6
+    call(0.0)
+    assert (t == 0).all() and call.scale.item() == 0.0
+
+
+def test_more_elements_than_32_bits_count(torch):
+    from paper_2302_06126_amd.optim import Clip
+    n = (1 << 32) + 77
+    t = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = [0, 1 << 31, (1 << 32) - 1, 1 << 32, n - 1]
+    for i, a in enumerate(at):
+        t[a] = 1.0 + i
+    call = Clip([t], 1.0)
+    _near(call().item(), float(np.sqrt(55.0)), 1)
+    s = call.scale.item()
+    assert [t[a].item() for a in at] == [_scaled(torch, torch.tensor(1.0 + i).to(torch.bfloat16), s).item() for i in range(5)]
+    assert torch.count_nonzero(t[:1 << 31]).item() + torch.count_nonzero(t[1 << 31:]).item() == 5
+
+
+def test_streams_and_graphs(torch):
+    from paper_2302_06126_amd.optim import Clip
+    sets = [[torch.randn(s, device="cuda") * (i + 1) for s in (5, 70000, 8192, 333)] for i in range(3)]
+    g = [t.clone() for t in sets[0]]
+    out = [torch.empty_like(t) for t in g]
+    call = Clip(g, 20.0, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    other = [t.clone() for t in g]
+    eager = Clip(other, 20.0)
+    side = torch.cuda.Stream()
+    for i in (0, 1, 2, 1, 0):
+        for a, b, c in zip(g, other, sets[i]):
+            a.copy_(c)
+            b.copy_(c)
+        graph.replay()
+        side.wait_stream(torch.cuda.current_stream())
+        eager(stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(call.norm, eager.norm) and all(torch.equal(a, b) for a, b in zip(out, other))
+        assert all(torch.equal(a.cpu(), _scaled(torch, c.cpu(), call.scale.item())) for a, c in zip(out, sets[i]))
+
+
+def test_refusals_of_tensors(torch):
+    from paper_2302_06126_amd import TagError
+    from paper_2302_06126_amd.optim import Clip, Muon
+    t = torch.zeros(8, 9, device="cuda")
+    for bad in (dict(grads=[t.double()]), dict(grads=[t.t()]), dict(grads=[t], out=[t.to(torch.bfloat16)]),
+                dict(grads=[t], out=[]), dict(grads=[t], out=[torch.zeros(9, 8, device="cuda")])):
+        with pytest.raises(ValueError):
+            Clip(max_norm=1.0, **bad)
+    for grads, kw in (([t, t], {}), ([t, t[2:4]], {}), ([t[:4]], dict(out=[t[1:5]]))):
+        with pytest.raises(TagError):
+            Clip(grads, 1.0, **kw)
+    for limit in (-1.0, float("nan")):
+        with pytest.raises(TagError):
+            Clip([t], limit)()
+    Clip([t, t], 1.0, out=False)()   # (counted twice)
+    w = torch.zeros(8, 9, device="cuda")
+    with pytest.raises(TagError):
+        Muon([(w, t)], max_norm=-1.0).step()
+
+
+# ------------------------------------------------- the optimiser step around it
+def _params(torch, seed, shapes):
+    gen = torch.Generator().manual_seed(seed)
+    return [(torch.randn(s, generator=gen).cuda(), 0.01 * torch.randn(s, generator=gen).cuda()) for s in shapes]
+
+
+SETS = [[(64, 42)], [(64, 200), (40, 9), (77,)], [(128, 42), (9, 64, 130), (300, 200), (5001,), (3,)], [(50,), (4097,)]]
+
+
+@pytest.mark.parametrize("shapes", SETS)
+@pytest.mark.parametrize("limit", [0.1, 3.0])
+def test_step_is_that_of_the_clipped_gradients(torch, shapes, limit):
+    """Bit for bit what Clip and a step without it give, one after the other."""
+    from paper_2302_06126_amd.optim import Clip, Muon
+    a, b = _params(torch, 1, shapes), _params(torch, 1, shapes)
+    bound = limit * _norm([g for _, g in a])
+    one = Muon(a, max_norm=bound, weight_decay=0.01)
+    clip, two = Clip([g for _, g in b], bound), Muon(b, weight_decay=0.01)
+    for i in range(3):
+        one.step()
+        norm = clip().clone()
+        two.step()
+        assert torch.equal(one.norm, norm)
+        assert all(torch.equal(w, v) for (w, _), (v, _) in zip(a, b)) and all(torch.equal(m, n) for m, n in zip(one.m, two.m))
+        for (_, g), (_, h) in zip(a, b):   # (the step leaves its gradients, Clip does not)
+            g.normal_()
+            h.copy_(g)
+    assert all(torch.isfinite(w).all() for w, _ in a)
+
+
+@pytest.mark.parametrize("shapes", SETS)
+def test_step_of_gradients_that_are_not_finite_is_left_out(torch, shapes):
+    from paper_2302_06126_amd.optim import Muon
+    p = _params(torch, 2, shapes)
+    opt = Muon(p, max_norm=0.5, weight_decay=0.1)
+    opt.step()
+    was = [t.clone() for t in [w for w, _ in p] + opt.m]
+    p[-1][1].view(-1)[-1] = float("nan")
+    opt.step()
+    assert all(torch.equal(a, b) for a, b in zip(was, [w for w, _ in p] + opt.m)) and torch.isnan(opt.norm).all()
+    p[-1][1].fill_(0.25)
+    opt.step()
+    assert not torch.equal(was[0], p[0][0]) and all(torch.isfinite(w).all() for w, _ in p)
+
+
+def test_captured_clipped_step(torch):
+    from paper_2302_06126_amd.optim import Muon
+    a, b = _params(torch, 3, SETS[2]), _params(torch, 3, SETS[2])
+    one, two = Muon(a, max_norm=0.3), Muon(b, max_norm=0.3)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one.step()
+    for i in range(4):
+        graph.replay()
+        two.step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(w, v) for (w, _), (v, _) in zip(a, b)) and torch.equal(one.norm, two.norm)
+        for (_, g), (_, h) in zip(a, b):
+            g.mul_(1.0 + i)
+            h.copy_(g)
+            if i == 1:
+                g.view(-1)[0] = h.view(-1)[0] = float("inf")   # (this step is left out)
+            elif i == 2:
+                g.fill_(0.1), h.fill_(0.1)
