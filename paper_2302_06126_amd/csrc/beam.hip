@@ -21,6 +21,11 @@ struct BeamArgs {
     const uint8_t *done;
     float *total;
     int32_t *parent, *slice;
+    int32_t lanes;                // threads of a row, a power of two: 16 columns each
+    // rows in parts
+    int32_t segs, group, groups;  // parts of a row; columns of a group, and groups of a row
+    float *seg_max, *group_max;   // [rows][segs], [rows][groups]
+    double *seg_sum;              // [rows][segs]
 };
 
 // doubles (no NaN) as unsigned integers in the same order; both zeros are one
@@ -32,8 +37,54 @@ __device__ __forceinline__ double unordered(uint64_t u) {
     return __longlong_as_double((long long)(u >> 63 ? u ^ 1ull << 63 : ~u));
 }
 
+// The value of the lane that step STEP of a reduction over 2, 4, 8, .. 64 lanes pairs
+// this one with (as in lanes_reduce: lanes that agree already stand in for one another).
+template <int STEP>
+__device__ __forceinline__ unsigned partner(unsigned v) {
+    if constexpr (STEP < 4) {
+        return (unsigned)other_lane<STEP>((int)v);
+    } else if constexpr (STEP == 4) {
+        const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? a[0] : a[1];
+    } else {
+        const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? a[0] : a[1];
+    }
+}
+template <int STEP>
+__device__ __forceinline__ float partner(float v) { return __uint_as_float(partner<STEP>(__float_as_uint(v))); }
+template <int STEP>
+__device__ __forceinline__ double partner(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    const unsigned lo = partner<STEP>((unsigned)u), hi = partner<STEP>((unsigned)(u >> 32));
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+// over `n` lanes (a power of two, the same for the wavefront), into each of them
+template <typename V, typename Op>
+__device__ __forceinline__ V reduce_lanes(V v, int n, Op op) {
+    if (n > 1) v = op(v, partner<0>(v));
+    if (n > 2) v = op(v, partner<1>(v));
+    if (n > 4) v = op(v, partner<2>(v));
+    if (n > 8) v = op(v, partner<3>(v));
+    if (n > 16) v = op(v, partner<4>(v));
+    if (n > 32) v = op(v, partner<5>(v));
+    return v;
+}
+struct Larger {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
+struct Smaller {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a < b ? a : b; }
+};
+struct Plus {
+    template <typename V>
+    __device__ V operator()(V a, V b) const { return a + b; }
+};
+
 // The best W of a search's candidates (key, index), collected by a block of NT
-// threads that call everything here together.  Candidates that beat the bar are
+// threads that call everything here together.  Candidates that pass the bar are
 // appended to a list in LDS in any order; when it is full, its best W stay and the
 // W-th becomes the bar.  The order is total (larger key, then lower index), so the
 // result does not depend on the order in which they came.
@@ -45,6 +96,7 @@ struct Best {
         double key[CAP];
         int32_t idx[CAP];
         int32_t count[2][kWaves];
+        unsigned ends[2][kWaves];
         int32_t tail;
     };
     Shared &s;
@@ -53,13 +105,15 @@ struct Best {
     int32_t bar_idx = -1;
     int n = 0, flip = 0;         // entries of the list
 
+    // (a barrier follows before the first candidate: raise's)
     __device__ Best(Shared &s_, int w) : s(s_), W(w) {
         if (threadIdx.x == 0) s.tail = 0;
-        __syncthreads();
     }
     __device__ bool passes(double key, int32_t idx) const { return key > bar || (key == bar && idx <= bar_idx); }
+    static __device__ int lanes(bool b) { return __popcll(__ballot(b)); }
     // sum over the wavefronts of a number that each wavefront's lanes share
     __device__ int sum(int v) {
+        if constexpr (kWaves == 1) return v;
         if ((threadIdx.x & 63) == 0) s.count[flip][threadIdx.x >> 6] = v;
         __syncthreads();
         int r = 0;
@@ -68,7 +122,75 @@ struct Best {
         flip ^= 1;   // (written again only after the next barrier, which follows these reads)
         return r;
     }
-    static __device__ int lanes(bool b) { return __popcll(__ballot(b)); }
+    // Sets the bar from one candidate of each thread, the best that it has: as high
+    // as W threads, or a few more, still pass.  Bisection of the upper halves of the
+    // ordered keys between the block's ends.
+    __device__ void raise(double key) {
+        const unsigned u = key > -INFINITY ? (unsigned)(ordered(key) >> 32) : 0u;
+        unsigned hi = reduce_lanes(u, 64, Larger()), lo = reduce_lanes(u ? u : ~0u, 64, Smaller());
+        int live = lanes(u != 0);
+        if constexpr (kWaves > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                s.ends[0][threadIdx.x >> 6] = hi;
+                s.ends[1][threadIdx.x >> 6] = lo;
+            }
+        }
+        live = sum(live);   // (and its barrier)
+        if constexpr (kWaves > 1) {
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                hi = max(hi, s.ends[0][i]);
+                lo = min(lo, s.ends[1][i]);
+            }
+        } else {
+            __syncthreads();
+        }
+        if (live < W) return;
+        const int most = W + W / 4;
+        while (lo < hi) {
+            const unsigned mid = hi - (hi - lo) / 2;
+            const int c = sum(lanes(u >= mid));
+            if (c >= W) lo = mid;
+            else hi = mid - 1;
+            if (c >= W && c <= most) break;
+        }
+        bar = unordered((uint64_t)lo << 32);
+        bar_idx = INT32_MAX;
+    }
+    // A thread's candidates that are likely to fit: `each(put)` calls put(key, index) for
+    // `count` of them that pass.  Then all of them, whether they did.
+    template <typename Each>
+    __device__ void offer(int count, Each each) {
+        if (count == 0) return;
+        int at = atomicAdd(&s.tail, count);
+        each([&](double key, int32_t idx) {
+            if (at < CAP) {
+                s.key[at] = key;
+                s.idx[at] = idx;
+            }
+            ++at;
+        });
+    }
+    __device__ bool offered() {
+        __syncthreads();
+        n = s.tail;
+        if (n <= CAP) return true;
+        __syncthreads();
+        if (threadIdx.x == 0) s.tail = 0;
+        n = 0;
+        __syncthreads();
+        return false;
+    }
+    // one candidate of each thread (key -inf: none), however many pass
+    __device__ void take(double key, int32_t idx) {
+        int c = sum(lanes(passes(key, idx)));
+        if (n + c > CAP) {
+            keep_best();
+            c = sum(lanes(passes(key, idx)));
+        }
+        append(passes(key, idx), key, idx);
+        n += c;
+    }
     __device__ void append(bool is, double key, int32_t idx) {
         const uint64_t m = __ballot(is);
         if (m == 0) return;
@@ -79,39 +201,6 @@ struct Best {
         if (is) {
             s.key[at] = key;
             s.idx[at] = idx;
-        }
-    }
-    // N candidates of each thread (key -inf: none)
-    template <int N>
-    __device__ void take(const double (&key)[N], const int32_t (&idx)[N]) {
-        int c = 0;
-#pragma unroll
-        for (int k = 0; k < N; ++k) c += lanes(passes(key[k], idx[k]));
-        c = sum(c);
-        if (n + c <= CAP) {
-            if (c > 0) {
-#pragma unroll
-                for (int k = 0; k < N; ++k) append(passes(key[k], idx[k]), key[k], idx[k]);
-            }
-            n += c;
-            return;
-        }
-#pragma unroll 1
-        for (int k = 0; k < N; ++k) {
-            double kk = key[0];
-            int32_t ii = idx[0];
-#pragma unroll
-            for (int q = 1; q < N; ++q) {
-                kk = k == q ? key[q] : kk;
-                ii = k == q ? idx[q] : ii;
-            }
-            c = sum(lanes(passes(kk, ii)));
-            if (n + c > CAP) {
-                keep_best();
-                c = sum(lanes(passes(kk, ii)));
-            }
-            append(passes(kk, ii), kk, ii);
-            n += c;
         }
     }
     // leaves the best W of a list of more
@@ -154,6 +243,7 @@ struct Best {
                 if (sum(c) < need) last += 1 << b;
             }
         }
+        __syncthreads();   // (of one wavefront, sum has none)
         if (threadIdx.x == 0) s.tail = 0;
         __syncthreads();
 #pragma unroll
@@ -166,16 +256,22 @@ struct Best {
     // each(rank, key, index) of the best, at most W; returns how many
     template <typename Each>
     __device__ int ranked(Each each) {
-        if (n > W) keep_best();
+        if (n > kMaxWidth && n > W) keep_best();
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += NT) {
-            const double k = s.key[i];
-            const int32_t x = s.idx[i];
+        // several threads to an entry, which share the comparisons
+        int parts = 1;
+        while (parts < 16 && parts * 2 * n <= NT) parts *= 2;
+        const int p = threadIdx.x & (parts - 1);
+        for (int i0 = 0; i0 < n; i0 += NT / parts) {
+            const int i = i0 + threadIdx.x / parts;
+            const double k = i < n ? s.key[i] : 0.0;
+            const int32_t x = i < n ? s.idx[i] : 0;
             int r = 0;
-            for (int j = 0; j < n; ++j) r += s.key[j] > k || (s.key[j] == k && s.idx[j] < x);
-            each(r, k, x);
+            for (int j = p; j < n; j += parts) r += s.key[j] > k || (s.key[j] == k && s.idx[j] < x);
+            r = (int)reduce_lanes((unsigned)r, parts, Plus());
+            if (i < n && p == 0 && r < W) each(r, k, x);
         }
-        return n;
+        return min(n, W);
     }
 };
 
@@ -198,54 +294,307 @@ __device__ __forceinline__ void write_beams(const BeamArgs &A, int64_t b, B &bes
     }
 }
 
-// One block per search: what each beam adds to its scores, a wavefront to a row,
-// then all candidates.
+// four columns from c of a row of n (past its end: -inf), at any element
 template <typename T>
-__global__ void __launch_bounds__(1024) beam_search(BeamArgs A) {
+__device__ __forceinline__ void load_four(const T *row, int64_t c, int64_t n, float (&v)[4]) {
+    typedef typename Quad<T>::raw raw;
+    if (c + 4 <= n) {
+        raw r;
+        __builtin_memcpy(&r, row + c, sizeof(raw));
+        Quad<T>::get(r, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = c + i < n ? Quad<T>::get1(row[c + i]) : -INFINITY;
+    }
+}
+
+// Column of a row's thread j of `lanes`, and its k-th four columns: the lanes of a
+// wavefront take 256 (or 4 lanes) consecutive ones at a time, a wavefront 1,024.
+__device__ __forceinline__ int64_t column(int j, int lanes, int k) {
+    return lanes < 64 ? 4 * (j + lanes * k) : (int64_t)(j >> 6) * 1024 + k * 256 + (j & 63) * 4;
+}
+
+// maximum of a thread's 16 scores; whether a NaN or +inf is among them
+__device__ __forceinline__ float own_max(const float (&x)[16], bool &bad) {
+    float m = x[0];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        bad = bad || !(x[i] < INFINITY);
+        m = fmaxf(m, x[i]);
+    }
+    return m;
+}
+// sum of e^(x - m), m finite, in 64 bits
+__device__ __forceinline__ double own_sum(const float (&x)[16], float m) {
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += exp((double)x[i] - (double)m);
+    return s;
+}
+
+// Searches whose scores fit one block's registers, 16 to a thread.
+template <typename T, int NT, int CAP>
+__global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
+    using B = Best<NT, CAP>;
+    __shared__ typename B::Shared shared;
+    __shared__ float wave_max[NT / 64];
+    __shared__ double wave_sum[NT / 64];
+    const int64_t b = blockIdx.x;
+    const int v = threadIdx.x / A.lanes, j = threadIdx.x % A.lanes;
+    B best(shared, A.W);
+    float total = -INFINITY;
+    bool done = false;
+    if (v < A.V) {
+        total = A.total_in[b * A.V + v];
+        done = A.done && A.done[b * A.V + v];
+    }
+    const bool live = total - total == 0.f;
+    float x[16];
+    if (live && !done) {
+        const T *row = static_cast<const T *>(A.x) + (b * A.V + v) * A.xs;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load_four(row, column(j, A.lanes, k), A.S, *reinterpret_cast<float(*)[4]>(x + 4 * k));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = -INFINITY;
+    }
+    bool bad = false;
+    const float own = own_max(x, bad);
+    // the row's maximum and sum; several wavefronts of a row each relative to their own, then joined
+    const int in_wave = min(A.lanes, 64);
+    float m = reduce_lanes(bad ? INFINITY : own, in_wave, Larger());
+    double sum = m > -INFINITY && m < INFINITY ? own_sum(x, m) : 0.0;
+    sum = reduce_lanes(sum, in_wave, Plus());
+    if constexpr (NT > 64) {
+        if (A.lanes > 64) {
+            if ((threadIdx.x & 63) == 0) {
+                wave_max[threadIdx.x >> 6] = m;
+                wave_sum[threadIdx.x >> 6] = sum;
+            }
+            __syncthreads();
+            const int w0 = v * (A.lanes / 64), w1 = w0 + A.lanes / 64;
+            m = -INFINITY;
+            for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
+            sum = 0.0;
+            if (m > -INFINITY && m < INFINITY)
+                for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp((double)wave_max[w] - (double)m);
+        }
+    }
+    // what is added to the scores; a finished beam is its first slice alone
+    double off = 0.0;
+    float top = own;
+    if (done && live) {
+        off = total;
+        if (j == 0) x[0] = top = 0.f;
+    } else if (m > -INFINITY && m < INFINITY) {
+        off = (double)total - ((double)m + log(sum));
+    } else {
+        top = -INFINITY;
+    }
+    best.raise((double)top + off);
+    auto candidates = [&](auto put) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
+    };
+    int count = 0;
+    if (top > -INFINITY && best.passes((double)top + off, -1)) candidates([&](double k, int32_t i) { count += best.passes(k, i); });
+    best.offer(count, [&](auto put) {
+        candidates([&](double k, int32_t i) {
+            if (best.passes(k, i)) put(k, i);
+        });
+    });
+    if (!best.offered()) {
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            float xi = x[0];
+#pragma unroll
+            for (int q = 1; q < 16; ++q) xi = q == i ? x[q] : xi;
+            best.take(top > -INFINITY ? (double)xi + off : -INFINITY, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
+        }
+    }
+    write_beams(A, b, best);
+}
+
+// Rows in parts: a part's maximum and sum, and the maximum of every group of its
+// columns, from one reading of the scores.
+template <typename T>
+__global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
+    __shared__ float wave_max[4];
+    __shared__ double wave_sum[4];
+    const int per = 256 / A.lanes;   // rows of a block, or one of its parts
+    const uint32_t item = blockIdx.x * per + threadIdx.x / A.lanes, at = item / (uint32_t)A.segs;
+    const int64_t row = at;
+    const int32_t seg = (int32_t)(item - at * A.segs);
+    const int j = threadIdx.x % A.lanes;
+    const int64_t c0 = (int64_t)seg * 4096;
+    bool live = row < rows;
+    if (live) {
+        const float t = A.total_in[row];
+        live = t - t == 0.f && !(A.done && A.done[row]);
+    }
+    float x[16];
+    if (live) {
+        const T *p = static_cast<const T *>(A.x) + row * A.xs;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load_four(p, c0 + column(j, A.lanes, k), A.S, *reinterpret_cast<float(*)[4]>(x + 4 * k));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = -INFINITY;
+    }
+    bool bad = false;
+    const float own = own_max(x, bad);
+    const int in_wave = min(A.lanes, 64);
+    float m = reduce_lanes(bad ? INFINITY : own, in_wave, Larger());
+    double sum = m > -INFINITY && m < INFINITY ? own_sum(x, m) : 0.0;
+    sum = reduce_lanes(sum, in_wave, Plus());
+    if (live) {   // groups' maxima (not used where the row turns out to have no candidates)
+        float *g = A.group_max + row * A.groups;
+        if (A.group == 1024) {
+            const float w = reduce_lanes(own, 64, Larger());
+            const int64_t c = c0 + column(j, A.lanes, 0);
+            if ((j & 63) == 0 && c < A.S) g[c / 1024] = w;
+        } else {
+            const int wide = A.group / 4;   // lanes to a group
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float w = reduce_lanes(fmaxf(fmaxf(x[4 * k], x[4 * k + 1]), fmaxf(x[4 * k + 2], x[4 * k + 3])), wide, Larger());
+                const int64_t c = c0 + column(j, A.lanes, k);
+                if ((j & (wide - 1)) == 0 && c < A.S) g[c / A.group] = w;
+            }
+        }
+    }
+    if (A.lanes > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            wave_max[threadIdx.x >> 6] = m;
+            wave_sum[threadIdx.x >> 6] = sum;
+        }
+        __syncthreads();
+        const int w0 = threadIdx.x / A.lanes * (A.lanes / 64), w1 = w0 + A.lanes / 64;
+        m = -INFINITY;
+        for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
+        sum = 0.0;
+        if (m > -INFINITY && m < INFINITY)
+            for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp((double)wave_max[w] - (double)m);
+    }
+    if (live && j == 0) {
+        A.seg_max[item] = m;
+        A.seg_sum[item] = sum;
+    }
+}
+
+// One block per search: what each beam adds to its scores, from its parts; the bar
+// from the groups' maxima; then the candidates of the groups that reach it.
+constexpr int kListed = 2048;   // groups
+template <typename T>
+__global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
     using B = Best<1024, 2048>;
     __shared__ B::Shared shared;
-    __shared__ double off[kMaxWidth];
+    __shared__ double off[kMaxWidth];   // -inf: no candidates
+    __shared__ uint8_t done[kMaxWidth];
+    __shared__ int32_t listed[kListed], n_listed;
     const int64_t b = blockIdx.x;
     const int lane = threadIdx.x & 63;
+    B best(shared, A.W);
+    if (threadIdx.x == 0) n_listed = 0;
     for (int v = threadIdx.x >> 6; v < A.V; v += 16) {
-        const float t = A.total_in[b * A.V + v];
+        const int64_t row = b * A.V + v;
+        const float t = A.total_in[row];
+        const bool fin = A.done && A.done[row];
         double o = -INFINITY;
         if (t - t == 0.f) {
-            if (A.done && A.done[b * A.V + v]) {
+            if (fin) {
                 o = t;
             } else {
                 float m = -INFINITY;
-                bool bad = false;
-                for (int64_t c = lane; c < A.S; c += 64) {
-                    const float x = score<T>(A, b * A.V + v, c);
-                    bad = bad || !(x < INFINITY);
-                    m = fmaxf(m, x);
-                }
-                for (int i = 32; i > 0; i >>= 1) m = fmaxf(m, __shfl_xor(m, i, 64));
-                if (__ballot(bad) == 0 && m > -INFINITY) {
-                    double sum = 0.0;
-                    for (int64_t c = lane; c < A.S; c += 64) sum += exp((double)score<T>(A, b * A.V + v, c) - (double)m);
-                    for (int i = 32; i > 0; i >>= 1) sum += __shfl_xor(sum, i, 64);
-                    o = (double)t - ((double)m + log(sum));
+                for (int64_t i = lane; i < A.segs; i += 64) m = fmaxf(m, A.seg_max[row * A.segs + i]);
+                m = reduce_lanes(m, 64, Larger());
+                if (m > -INFINITY && m < INFINITY) {
+                    double s = 0.0;
+                    for (int64_t i = lane; i < A.segs; i += 64) {
+                        const float p = A.seg_max[row * A.segs + i];
+                        if (p > -INFINITY) s += A.seg_sum[row * A.segs + i] * exp((double)p - (double)m);
+                    }
+                    s = reduce_lanes(s, 64, Plus());
+                    o = (double)t - ((double)m + log(s));
                 }
             }
         }
-        if (lane == 0) off[v] = o;
+        if (lane == 0) {
+            off[v] = o;
+            done[v] = fin;
+        }
     }
-    B best(shared, A.W);   // (a barrier)
-    const int32_t total = A.V * A.S;
-    for (int32_t base = 0; base < total; base += 1024) {
-        double key[1] = {-INFINITY};
-        const int32_t idx[1] = {base + (int32_t)threadIdx.x};
-        if (idx[0] < total) {
-            const int32_t v = idx[0] / A.S, a = idx[0] - v * A.S;
+    __syncthreads();
+    // every group's best candidate: each(group, key)
+    const int32_t total = A.V * A.groups, up = 1024 / A.groups, rest = 1024 % A.groups;
+    auto groups = [&](auto each) {
+        int32_t v = threadIdx.x / A.groups, g = threadIdx.x % A.groups;
+        for (int32_t i = threadIdx.x; i < total; i += 1024) {
             const double o = off[v];
-            if (o > -INFINITY) {
-                if (A.done && A.done[b * A.V + v]) key[0] = a == 0 ? o : -INFINITY;
-                else key[0] = (double)score<T>(A, b * A.V + v, a) + o;
+            double key = -INFINITY;
+            if (o > -INFINITY) key = done[v] ? (g == 0 ? o : -INFINITY) : (double)A.group_max[(b * A.V + v) * A.groups + g] + o;
+            each(i, key);
+            v += up;
+            g += rest;
+            if (g >= A.groups) {
+                g -= A.groups;
+                ++v;
             }
         }
-        best.take(key, idx);
+    };
+    double top = -INFINITY;
+    groups([&](int32_t, double key) { top = key > top ? key : top; });
+    best.raise(top);
+    const int shift = 31 - __clz(A.group), within = A.group - 1;
+    // the candidate at place e of the group `id`
+    auto candidate = [&](int32_t id, int32_t e, double &key, int32_t &idx) {
+        const int32_t v = id / A.groups;
+        const int32_t c = ((id - v * A.groups) << shift) + e;
+        key = -INFINITY;
+        idx = v * A.S + c;
+        if (c >= A.S || !(off[v] > -INFINITY)) return;
+        if (done[v]) key = c == 0 ? off[v] : -INFINITY;
+        else key = (double)score<T>(A, b * A.V + v, c) + off[v];
+    };
+    bool fits = true;
+    if (best.passes(top, -1)) {
+        groups([&](int32_t i, double key) {
+            if (key > -INFINITY && best.passes(key, -1)) {
+                const int at = atomicAdd(&n_listed, 1);
+                if (at < kListed) listed[at] = i;
+            }
+        });
+    }
+    __syncthreads();
+    const int n = n_listed;
+    if (n <= kListed) {
+        for (int32_t e = threadIdx.x; e < n << shift; e += 1024) {
+            double key;
+            int32_t idx;
+            candidate(listed[e >> shift], e & within, key, idx);
+            if (key > -INFINITY && best.passes(key, idx)) best.offer(1, [&](auto put) { put(key, idx); });
+        }
+        fits = best.offered();
+    }
+    if (n > kListed || !fits) {   // too many at the bar: everything in turn, eight of each thread at a time
+        const int64_t places = (int64_t)total << shift;
+        for (int64_t e0 = threadIdx.x; e0 - threadIdx.x < places; e0 += 8192) {
+            double key[8];
+            int32_t idx[8];
+            int c = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int64_t e = e0 + 1024 * k;
+                key[k] = -INFINITY;
+                idx[k] = 0;
+                if (e < places) candidate((int32_t)(e >> shift), (int32_t)e & within, key[k], idx[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c += B::lanes(best.passes(key[k], idx[k]));
+            if (best.sum(c) == 0) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) best.take(key[k], idx[k]);
+        }
     }
     write_beams(A, b, best);
 }
@@ -319,6 +668,51 @@ __global__ void __launch_bounds__(256) beam_reorder(ReorderArgs A) {
 // ---------------------------------------------------------------------- host
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// The way that a level goes: one launch where each search's scores fit the registers
+// of a block, else rows in parts and a launch that joins them.
+struct Way {
+    int32_t lanes, segs, group, groups;
+    bool whole;
+    int64_t blocks;   // of the parts
+};
+Way way(int32_t n, int32_t V, int32_t W, int32_t S) {
+    Way w{};
+    for (w.lanes = 1; w.lanes < 1024 && 16 * w.lanes < S; w.lanes *= 2) {}
+    w.whole = 16 * w.lanes >= S && V * w.lanes <= 1024;
+    if (w.whole) return w;
+    w.lanes = std::min(w.lanes, 256);
+    w.segs = (int32_t)((S + 4095ll) / 4096);
+    // groups: few enough to be looked at twice by one block, and so many that a row's own best set a bar
+    const int32_t most = w.lanes >= 64 ? 1024 : 4 * w.lanes;
+    for (w.group = 16; 4 * w.group <= most && (int64_t)4 * w.group * W <= S && (int64_t)V * (S / w.group) > 16384;) w.group *= 4;
+    w.groups = (S + w.group - 1) / w.group;
+    const int64_t per = 256 / w.lanes, items = (int64_t)n * V * w.segs;
+    w.blocks = (items + per - 1) / per;
+    return w;
+}
+size_t carve(int32_t n, int32_t V, const Way &w, void *base, BeamArgs *A) {
+    if (w.whole) return 0;
+    Carver c(base);
+    const size_t rows = (size_t)n * V;
+    A->seg_max = c.take<float>(rows * w.segs);
+    A->seg_sum = c.take<double>(rows * w.segs);
+    A->group_max = c.take<float>(rows * w.groups);
+    return c.used;
+}
+
+template <typename T>
+void launch_select(const BeamArgs &A, const Way &w, int32_t n, hipStream_t st) {
+    if (w.whole) {
+        const int threads = A.V * A.lanes;
+        if (threads <= 64) beam_whole<T, 64, 320><<<n, 64, 0, st>>>(A);
+        else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A);
+        else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A);
+        return;
+    }
+    beam_parts<T><<<(unsigned)w.blocks, 256, 0, st>>>(A, (int64_t)n * A.V);
+    beam_join<T><<<n, 1024, 0, st>>>(A);
+}
+
 tag_status check_beams(int32_t n, int32_t V, int32_t W) {
     if (n < 0 || V < 1 || W < 1) TAG_FAIL(TAG_EINVAL, "need n_search >= 0, width_in >= 1 and width >= 1");
     if (V > kMaxWidth || W > kMaxWidth) TAG_FAIL(TAG_ESHAPE, "at most 256 beams");
@@ -329,7 +723,8 @@ tag_status check_select(int32_t n, int32_t V, int32_t W, int32_t S) {
     if (st != TAG_OK) return st;
     if (S < 1) TAG_FAIL(TAG_EINVAL, "need n_slices >= 1");
     if ((int64_t)V * S > (1 << 30)) TAG_FAIL(TAG_ESHAPE, "at most 2^30 continuations of a search");
-    if (n >= 1 << 22) TAG_FAIL(TAG_ESHAPE, "fewer than 2^22 searches");   // (a launch has fewer than 2^32 threads)
+    // (a launch has fewer than 2^32 threads)
+    if (n >= 1 << 22 || (n > 0 && way(n, V, W, S).blocks >= 1 << 24)) TAG_FAIL(TAG_ESHAPE, "too many scores for a launch");
     return TAG_OK;
 }
 
@@ -352,7 +747,8 @@ extern "C" tag_status tag_beam_workspace(int32_t n_search, int32_t width_in, int
     if (!bytes) TAG_FAIL(TAG_EINVAL, "bytes must be non-NULL");
     const tag_status st = check_select(n_search, width_in, width, n_slices);
     if (st != TAG_OK) return st;
-    *bytes = 0;
+    BeamArgs A{};
+    *bytes = carve(n_search, width_in, way(n_search, width_in, width, n_slices), nullptr, &A);
     return TAG_OK;
 }
 
@@ -382,12 +778,20 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
         for (int p = 0; p < o; ++p)
             if (out[o].meets(out[p])) TAG_FAIL(TAG_EINVAL, "outputs overlap one another");
     }
-    (void)workspace;
-    (void)ws_bytes;
-    const BeamArgs A{width_in, width, n_slices, scores, score_stride, total_in, done, total, parent, slice};
+    BeamArgs A{};
+    const Way w = way(n_search, width_in, width, n_slices);
+    const size_t need = carve(n_search, width_in, w, nullptr, &A);
+    if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_beam_workspace)");
+    if (need && (!workspace || !aligned(workspace, 16))) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
+    carve(n_search, width_in, w, workspace, &A);
+    A.V = width_in; A.W = width; A.S = n_slices;
+    A.x = scores; A.xs = score_stride;
+    A.total_in = total_in; A.done = done;
+    A.total = total; A.parent = parent; A.slice = slice;
+    A.lanes = w.lanes; A.segs = w.segs; A.group = w.group; A.groups = w.groups;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (dtype == TAG_BF16) beam_search<uint16_t><<<n_search, 1024, 0, stream>>>(A);
-    else beam_search<float><<<n_search, 1024, 0, stream>>>(A);
+    if (dtype == TAG_BF16) launch_select<uint16_t>(A, w, n_search, stream);
+    else launch_select<float>(A, w, n_search, stream);
     return launch_status("tag_beam_select");
 }
 
