@@ -157,6 +157,13 @@ struct Best {
         bar = unordered((uint64_t)lo << 32);
         bar_idx = INT32_MAX;
     }
+    // A score below which no score + off passes: the bar less off, by more than the roundings of either may be.
+    __device__ float least_score(double off) const {
+        if (!(bar > -INFINITY)) return -INFINITY;
+        const double d = bar - off - 0x1p-50 * (fabs(bar) + fabs(off));
+        const float f = (float)d;
+        return f - fabsf(f) * 0x1p-22f - 0x1p-140f;
+    }
     // A thread's candidates that are likely to fit: `each(put)` calls put(key, index) for
     // `count` of them that pass.  Then all of them, whether they did.
     template <typename Each>
@@ -324,11 +331,29 @@ __device__ __forceinline__ float own_max(const float (&x)[16], bool &bad) {
     }
     return m;
 }
+// e^x for x <= 0, within a few roundings of 64 bits; below -700 that of -700 (a
+// sum with a term of 1 in it does not see either).  2^(n + f) with |f| <= 1/2: n by
+// adding 1.5 2^52, whose last bits it then is, 2^f = 1 + f q(f) by interpolation of q
+// at eleven Chebyshev points (2e-17 off).  18 instructions, of the fp32 rate: 42,496 x
+// 256 scores 30 -> TIME us against the library's exp.
+__device__ __forceinline__ double exp_below(double x) {
+    constexpr double q[11] = {0.6931471805599453,    0.24022650695910097,   0.0555041086648216,    0.009618129107606888,
+                              0.0013333558146416936, 0.0001540353044173605, 1.525273382983612e-05, 1.321544258792169e-06,
+                              1.0178062445845774e-07, 7.072585949269223e-09, 4.4549605981865186e-10};
+    constexpr double log2e = 1.4426950408889634, shift = 6755399441055744.0;
+    x = x > -700.0 ? x : -700.0;
+    const double t = fma(x, log2e, shift), f = fma(x, log2e, shift - t);
+    double p = q[10];
+#pragma unroll
+    for (int i = 9; i >= 0; --i) p = fma(p, f, q[i]);
+    const uint64_t u = (uint64_t)__double_as_longlong(fma(p, f, 1.0));
+    return __longlong_as_double((long long)(u + ((uint64_t)__double_as_longlong(t) << 52)));
+}
 // sum of e^(x - m), m finite, in 64 bits
 __device__ __forceinline__ double own_sum(const float (&x)[16], float m) {
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += exp((double)x[i] - (double)m);
+    for (int i = 0; i < 16; ++i) s += exp_below((double)x[i] - (double)m);
     return s;
 }
 
@@ -377,7 +402,7 @@ __global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
             for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
             sum = 0.0;
             if (m > -INFINITY && m < INFINITY)
-                for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp((double)wave_max[w] - (double)m);
+                for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp_below((double)wave_max[w] - (double)m);
         }
     }
     // what is added to the scores; a finished beam is its first slice alone
@@ -392,16 +417,15 @@ __global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
         top = -INFINITY;
     }
     best.raise((double)top + off);
-    auto candidates = [&](auto put) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
-    };
+    // what may pass, by a bound on the scores that is a little lower (a superset will do)
+    const float least = top > -INFINITY ? best.least_score(off) : __builtin_nanf("");   // (nothing is at or above that)
     int count = 0;
-    if (top > -INFINITY && best.passes((double)top + off, -1)) candidates([&](double k, int32_t i) { count += best.passes(k, i); });
+#pragma unroll
+    for (int i = 0; i < 16; ++i) count += x[i] >= least && x[i] > -INFINITY;
     best.offer(count, [&](auto put) {
-        candidates([&](double k, int32_t i) {
-            if (best.passes(k, i)) put(k, i);
-        });
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (x[i] >= least && x[i] > -INFINITY) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
     });
     if (!best.offered()) {
 #pragma unroll 1
@@ -474,7 +498,7 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
         for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
         sum = 0.0;
         if (m > -INFINITY && m < INFINITY)
-            for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp((double)wave_max[w] - (double)m);
+            for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp_below((double)wave_max[w] - (double)m);
     }
     if (live && j == 0) {
         A.seg_max[item] = m;
@@ -493,52 +517,71 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
     __shared__ uint8_t done[kMaxWidth];
     __shared__ int32_t listed[kListed], n_listed;
     const int64_t b = blockIdx.x;
-    const int lane = threadIdx.x & 63;
     B best(shared, A.W);
     if (threadIdx.x == 0) n_listed = 0;
-    for (int v = threadIdx.x >> 6; v < A.V; v += 16) {
+    // a row by as many threads as it has parts, at most a wavefront
+    int wide = 1;
+    while (wide < 64 && wide < A.segs) wide *= 2;
+    for (int v0 = 0; v0 < A.V; v0 += 1024 / wide) {
+        const int v = v0 + threadIdx.x / wide, i0 = threadIdx.x & (wide - 1);
         const int64_t row = b * A.V + v;
-        const float t = A.total_in[row];
-        const bool fin = A.done && A.done[row];
-        double o = -INFINITY;
-        if (t - t == 0.f) {
-            if (fin) {
-                o = t;
-            } else {
-                float m = -INFINITY;
-                for (int64_t i = lane; i < A.segs; i += 64) m = fmaxf(m, A.seg_max[row * A.segs + i]);
-                m = reduce_lanes(m, 64, Larger());
-                if (m > -INFINITY && m < INFINITY) {
-                    double s = 0.0;
-                    for (int64_t i = lane; i < A.segs; i += 64) {
-                        const float p = A.seg_max[row * A.segs + i];
-                        if (p > -INFINITY) s += A.seg_sum[row * A.segs + i] * exp((double)p - (double)m);
-                    }
-                    s = reduce_lanes(s, 64, Plus());
-                    o = (double)t - ((double)m + log(s));
-                }
-            }
+        float t = -INFINITY;
+        bool fin = false;
+        if (v < A.V) {
+            t = A.total_in[row];
+            fin = A.done && A.done[row];
         }
-        if (lane == 0) {
-            off[v] = o;
+        const bool read = t - t == 0.f && !fin;
+        const float *pm = A.seg_max + row * A.segs;
+        const double *ps = A.seg_sum + row * A.segs;
+        // (the first part of each thread's at once)
+        const float m0 = read && i0 < A.segs ? pm[i0] : -INFINITY;
+        const double s0 = read && i0 < A.segs ? ps[i0] : 0.0;
+        float m = m0;
+        if (read)
+            for (int i = i0 + wide; i < A.segs; i += wide) m = fmaxf(m, pm[i]);
+        m = reduce_lanes(m, wide, Larger());
+        const bool some = m > -INFINITY && m < INFINITY;
+        double s = some && m0 > -INFINITY ? s0 * exp_below((double)m0 - (double)m) : 0.0;
+        if (some)
+            for (int i = i0 + wide; i < A.segs; i += wide)
+                if (pm[i] > -INFINITY) s += ps[i] * exp_below((double)pm[i] - (double)m);
+        s = reduce_lanes(s, wide, Plus());
+        if (v < A.V && i0 == 0) {
+            off[v] = some ? (double)t - ((double)m + log(s)) : fin && t - t == 0.f ? (double)t : -INFINITY;
             done[v] = fin;
         }
     }
     __syncthreads();
     // every group's best candidate: each(group, key)
     const int32_t total = A.V * A.groups, up = 1024 / A.groups, rest = 1024 % A.groups;
+    const float *maxima = A.group_max + b * total;
     auto groups = [&](auto each) {
+        constexpr int U = 8;
         int32_t v = threadIdx.x / A.groups, g = threadIdx.x % A.groups;
-        for (int32_t i = threadIdx.x; i < total; i += 1024) {
-            const double o = off[v];
-            double key = -INFINITY;
-            if (o > -INFINITY) key = done[v] ? (g == 0 ? o : -INFINITY) : (double)A.group_max[(b * A.V + v) * A.groups + g] + o;
-            each(i, key);
-            v += up;
-            g += rest;
-            if (g >= A.groups) {
-                g -= A.groups;
-                ++v;
+        for (int32_t i = threadIdx.x; i < total; i += U * 1024) {
+            float m[U];
+            int32_t row[U];
+            bool first[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                m[k] = i + 1024 * k < total ? maxima[i + 1024 * k] : -INFINITY;
+                row[k] = v;
+                first[k] = g == 0;
+                v += up;
+                g += rest;
+                if (g >= A.groups) {
+                    g -= A.groups;
+                    ++v;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                if (i + 1024 * k >= total) continue;
+                const double o = off[row[k]];
+                double key = -INFINITY;   // (what stands there for rows without candidates is not looked at)
+                if (o > -INFINITY) key = done[row[k]] ? (first[k] ? o : -INFINITY) : (double)m[k] + o;
+                each(i + 1024 * k, key);
             }
         }
     };

@@ -36,7 +36,7 @@ static_assert(sizeof(Chunk) == 64, "an entry to a cache line's half");
 struct ClipArgs {
     const Chunk *table;
     int64_t chunks;
-    int32_t sums, in_place;
+    int32_t sums, writes;
     double *part;
     float max_norm;
     float *result;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(256) clip_apply(ClipArgs A) {
         A.result[0] = rounded;
         A.result[1] = scale;
     }
-    if (A.in_place && scale == 1.f) return;
+    if (A.writes == 0 || (A.writes == 2 && scale == 1.f)) return;
     for (int64_t c = A.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const Chunk C = A.table[c];
         if (!C.out || (scale == 1.f && C.out == C.g)) continue;
@@ -342,7 +342,7 @@ extern "C" tag_status tag_clip(const tag_clip_plan *plan, float max_norm, float 
     if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
     ClipArgs A{};
     A.table = static_cast<const Chunk *>(plan->table); A.chunks = plan->chunks;
-    A.sums = (int32_t)std::min<int64_t>(plan->chunks, kBlocks); A.in_place = plan->writes != 1;
+    A.sums = (int32_t)std::min<int64_t>(plan->chunks, kBlocks); A.writes = plan->writes;
     A.part = static_cast<double *>(workspace);
     A.max_norm = max_norm; A.result = result;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
