@@ -24,14 +24,14 @@ extern "C" {
  * One level.  Beam v of a search has the row x_v of S scores and the log
  * probability total_v so far.  Its continuations, in 64 bits, are
  *   c_va = x_va + (total_v - log sum_b exp x_vb)       for every x_va > -inf
- * and those of a finished beam (done[v] != 0; its scores are not read) the one
+ * and those of a finished beam (done[v] != 0; its scores do not matter) the one
  * candidate c = total_v, which counts as slice 0 where ties are broken.  The
  * `width` best candidates of all beams of a search, best first, equal ones in
  * the order of (beam, slice), become its new beams:
  *   total   c, rounded to fp32          parent  v
  *   slice   a, or -1 of a finished beam
  * A beam has no candidates if its total is not finite, or if a NaN or +inf
- * stands among its scores (not looked at for a finished beam); what is left
+ * stands among its scores (which a finished beam may have); what is left
  * over of the width has total -inf, parent -1 and slice -1.  A search starts
  * from width_in = 1, or from totals of -inf but for one beam.
  *

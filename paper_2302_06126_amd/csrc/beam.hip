@@ -21,9 +21,9 @@ struct BeamArgs {
     const uint8_t *done;
     float *total;
     int32_t *parent, *slice;
-    int32_t lanes;                // threads of a row, a power of two: 16 columns each
+    int32_t shift;                // 2^shift threads of a row, 16 columns each
     // rows in parts
-    int32_t segs, group, groups;  // parts of a row; columns of a group, and groups of a row
+    int32_t segs, group, groups;  // parts of a row; 2^group columns of a group, and groups of a row
     float *seg_max, *group_max;   // [rows][segs], [rows][groups]
     double *seg_sum;              // [rows][segs]
 };
@@ -37,50 +37,75 @@ __device__ __forceinline__ double unordered(uint64_t u) {
     return __longlong_as_double((long long)(u >> 63 ? u ^ 1ull << 63 : ~u));
 }
 
-// The value of the lane that step STEP of a reduction over 2, 4, 8, .. 64 lanes pairs
-// this one with (as in lanes_reduce: lanes that agree already stand in for one another).
+// Step STEP of a reduction over 2, 4, 8, .. 64 lanes that ends in each of them: this
+// lane's value and that of its partner, in the same order or the other (as in
+// lanes_reduce, for commutative operations).
 template <int STEP>
-__device__ __forceinline__ unsigned partner(unsigned v) {
-    if constexpr (STEP < 4) {
-        return (unsigned)other_lane<STEP>((int)v);
-    } else if constexpr (STEP == 4) {
-        const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-        return threadIdx.x & 16 ? a[0] : a[1];
-    } else {
-        const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        return threadIdx.x & 32 ? a[0] : a[1];
+struct Pair {
+    unsigned a, b;
+    __device__ __forceinline__ explicit Pair(unsigned v) {
+        if constexpr (STEP < 4) {
+            a = v;
+            b = (unsigned)other_lane<STEP>((int)v);
+        } else if constexpr (STEP == 4) {
+            const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+            a = p[0];
+            b = p[1];
+        } else {
+            const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+            a = p[0];
+            b = p[1];
+        }
     }
+};
+template <int STEP, typename Op>
+__device__ __forceinline__ unsigned join(unsigned v, Op op) {
+    const Pair<STEP> p(v);
+    return op(p.a, p.b);
 }
-template <int STEP>
-__device__ __forceinline__ float partner(float v) { return __uint_as_float(partner<STEP>(__float_as_uint(v))); }
-template <int STEP>
-__device__ __forceinline__ double partner(double v) {
+template <int STEP, typename Op>
+__device__ __forceinline__ float join(float v, Op op) {
+    const Pair<STEP> p(__float_as_uint(v));
+    return op(__uint_as_float(p.a), __uint_as_float(p.b));
+}
+template <int STEP, typename Op>
+__device__ __forceinline__ double join(double v, Op op) {
     const uint64_t u = (uint64_t)__double_as_longlong(v);
-    const unsigned lo = partner<STEP>((unsigned)u), hi = partner<STEP>((unsigned)(u >> 32));
-    return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+    const Pair<STEP> lo((unsigned)u), hi((unsigned)(u >> 32));
+    return op(__hiloint2double((int)hi.a, (int)lo.a), __hiloint2double((int)hi.b, (int)lo.b));
 }
-// over `n` lanes (a power of two, the same for the wavefront), into each of them
+// over 2^n lanes, n the same for the wavefront
 template <typename V, typename Op>
 __device__ __forceinline__ V reduce_lanes(V v, int n, Op op) {
-    if (n > 1) v = op(v, partner<0>(v));
-    if (n > 2) v = op(v, partner<1>(v));
-    if (n > 4) v = op(v, partner<2>(v));
-    if (n > 8) v = op(v, partner<3>(v));
-    if (n > 16) v = op(v, partner<4>(v));
-    if (n > 32) v = op(v, partner<5>(v));
+    if (n > 0) v = join<0>(v, op);
+    if (n > 1) v = join<1>(v, op);
+    if (n > 2) v = join<2>(v, op);
+    if (n > 3) v = join<3>(v, op);
+    if (n > 4) v = join<4>(v, op);
+    if (n > 5) v = join<5>(v, op);
     return v;
 }
+// (no operand is a NaN; fmaxf would first quiet each)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 struct Larger {
-    template <typename V>
-    __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+    __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); }
+    __device__ __forceinline__ float operator()(float a, float b) const { return max2(a, b); }
 };
 struct Smaller {
-    template <typename V>
-    __device__ V operator()(V a, V b) const { return a < b ? a : b; }
+    __device__ __forceinline__ unsigned operator()(unsigned a, unsigned b) const { return min(a, b); }
 };
 struct Plus {
     template <typename V>
-    __device__ V operator()(V a, V b) const { return a + b; }
+    __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
 
 // The best W of a search's candidates (key, index), collected by a block of NT
@@ -96,6 +121,7 @@ struct Best {
         double key[CAP];
         int32_t idx[CAP];
         int32_t count[2][kWaves];
+        uint64_t count3[2][kWaves];
         unsigned ends[2][kWaves];
         int32_t tail;
     };
@@ -122,12 +148,25 @@ struct Best {
         flip ^= 1;   // (written again only after the next barrier, which follows these reads)
         return r;
     }
+    // the same of three numbers up to NT
+    __device__ void sum3(int &a, int &b, int &c) {
+        if constexpr (kWaves == 1) return;
+        if ((threadIdx.x & 63) == 0) s.count3[flip][threadIdx.x >> 6] = (uint64_t)a | (uint64_t)b << 16 | (uint64_t)c << 32;
+        __syncthreads();
+        uint64_t r = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) r += s.count3[flip][i];
+        flip ^= 1;
+        a = (int)(r & 0xffff);
+        b = (int)(r >> 16 & 0xffff);
+        c = (int)(r >> 32);
+    }
     // Sets the bar from one candidate of each thread, the best that it has: as high
-    // as W threads, or a few more, still pass.  Bisection of the upper halves of the
+    // as W threads, or a few more, still pass (false: fewer have one).  Bisection of the upper halves of the
     // ordered keys between the block's ends.
-    __device__ void raise(double key) {
+    __device__ bool raise(double key) {
         const unsigned u = key > -INFINITY ? (unsigned)(ordered(key) >> 32) : 0u;
-        unsigned hi = reduce_lanes(u, 64, Larger()), lo = reduce_lanes(u ? u : ~0u, 64, Smaller());
+        unsigned hi = reduce_lanes(u, 6, Larger()), lo = reduce_lanes(u ? u : ~0u, 6, Smaller());
         int live = lanes(u != 0);
         if constexpr (kWaves > 1) {
             if ((threadIdx.x & 63) == 0) {
@@ -145,17 +184,21 @@ struct Best {
         } else {
             __syncthreads();
         }
-        if (live < W) return;
-        const int most = W + W / 4;
-        while (lo < hi) {
-            const unsigned mid = hi - (hi - lo) / 2;
-            const int c = sum(lanes(u >= mid));
-            if (c >= W) lo = mid;
-            else hi = mid - 1;
-            if (c >= W && c <= most) break;
+        if (live < W) return false;
+        const int most = W + max(W / 2, 8);
+        while (lo < hi) {   // W reach lo, fewer reach hi + 1; three probes between them to a turn
+            const unsigned step = (hi - lo) / 4, t1 = lo + step + 1, t2 = t1 + step, t3 = min(t2 + step, hi);
+            int c1 = lanes(u >= t1), c2 = lanes(u >= t2), c3 = lanes(u >= t3);
+            sum3(c1, c2, c3);
+            const unsigned t = c3 >= W ? t3 : c2 >= W ? t2 : c1 >= W ? t1 : lo;
+            const int c = c3 >= W ? c3 : c2 >= W ? c2 : c1 >= W ? c1 : INT32_MAX;
+            if (c3 < W) hi = (c2 >= W ? t3 : c1 >= W ? t2 : t1) - 1;
+            lo = t;
+            if (c <= most) break;
         }
         bar = unordered((uint64_t)lo << 32);
         bar_idx = INT32_MAX;
+        return true;
     }
     // A score below which no score + off passes: the bar less off, by more than the roundings of either may be.
     __device__ float least_score(double off) const {
@@ -181,12 +224,13 @@ struct Best {
     __device__ bool offered() {
         __syncthreads();
         n = s.tail;
-        if (n <= CAP) return true;
+        return n <= CAP;
+    }
+    __device__ void clear() {
         __syncthreads();
         if (threadIdx.x == 0) s.tail = 0;
         n = 0;
         __syncthreads();
-        return false;
     }
     // one candidate of each thread (key -inf: none), however many pass
     __device__ void take(double key, int32_t idx) {
@@ -266,16 +310,16 @@ struct Best {
         if (n > kMaxWidth && n > W) keep_best();
         __syncthreads();
         // several threads to an entry, which share the comparisons
-        int parts = 1;
-        while (parts < 16 && parts * 2 * n <= NT) parts *= 2;
-        const int p = threadIdx.x & (parts - 1);
-        for (int i0 = 0; i0 < n; i0 += NT / parts) {
-            const int i = i0 + threadIdx.x / parts;
+        int share = 0;
+        while (share < 4 && n << (share + 1) <= NT) ++share;
+        const int p = threadIdx.x & ((1 << share) - 1);
+        for (int i0 = 0; i0 < n; i0 += NT >> share) {
+            const int i = i0 + (threadIdx.x >> share);
             const double k = i < n ? s.key[i] : 0.0;
             const int32_t x = i < n ? s.idx[i] : 0;
             int r = 0;
-            for (int j = p; j < n; j += parts) r += s.key[j] > k || (s.key[j] == k && s.idx[j] < x);
-            r = (int)reduce_lanes((unsigned)r, parts, Plus());
+            for (int j = p; j < n; j += 1 << share) r += s.key[j] > k || (s.key[j] == k && s.idx[j] < x);
+            r = (int)reduce_lanes((unsigned)r, share, Plus());
             if (i < n && p == 0 && r < W) each(r, k, x);
         }
         return min(n, W);
@@ -288,12 +332,12 @@ __device__ __forceinline__ float score(const BeamArgs &A, int64_t row, int64_t c
 }
 
 template <typename B>
-__device__ __forceinline__ void write_beams(const BeamArgs &A, int64_t b, B &best) {
+__device__ __forceinline__ void write_beams(const BeamArgs &A, int64_t b, B &best, const uint8_t *done) {
     const int n = best.ranked([&](int r, double key, int32_t idx) {
         const int32_t v = idx / A.S;
         A.total[b * A.W + r] = (float)key;
         A.parent[b * A.W + r] = v;
-        A.slice[b * A.W + r] = A.done && A.done[b * A.V + v] ? -1 : idx - v * A.S;
+        A.slice[b * A.W + r] = done[v] ? -1 : idx - v * A.S;
     });
     for (int r = n + threadIdx.x; r < A.W; r += blockDim.x) {
         A.total[b * A.W + r] = -INFINITY;
@@ -301,9 +345,9 @@ __device__ __forceinline__ void write_beams(const BeamArgs &A, int64_t b, B &bes
     }
 }
 
-// four columns from c of a row of n (past its end: -inf), at any element
+// four columns of a row of n from c, at any element (past its end: -inf)
 template <typename T>
-__device__ __forceinline__ void load_four(const T *row, int64_t c, int64_t n, float (&v)[4]) {
+__device__ __forceinline__ void load_four(const T *row, int c, int n, float (&v)[4]) {
     typedef typename Quad<T>::raw raw;
     if (c + 4 <= n) {
         raw r;
@@ -314,23 +358,47 @@ __device__ __forceinline__ void load_four(const T *row, int64_t c, int64_t n, fl
         for (int i = 0; i < 4; ++i) v[i] = c + i < n ? Quad<T>::get1(row[c + i]) : -INFINITY;
     }
 }
-
-// Column of a row's thread j of `lanes`, and its k-th four columns: the lanes of a
-// wavefront take 256 (or 4 lanes) consecutive ones at a time, a wavefront 1,024.
-__device__ __forceinline__ int64_t column(int j, int lanes, int k) {
-    return lanes < 64 ? 4 * (j + lanes * k) : (int64_t)(j >> 6) * 1024 + k * 256 + (j & 63) * 4;
+// Column of the k-th four of thread j of a row's 2^shift: the lanes of a wavefront take
+// 256 (or four each) consecutive ones at a time, a wavefront 1,024.
+__device__ __forceinline__ int column(int j, int shift, int k) {
+    return shift < 6 ? 4 * (j + (k << shift)) : (j >> 6) * 1024 + k * 256 + (j & 63) * 4;
 }
 
-// maximum of a thread's 16 scores; whether a NaN or +inf is among them
-__device__ __forceinline__ float own_max(const float (&x)[16], bool &bad) {
-    float m = x[0];
+// A thread's 16 columns of a row of n, or of its part from c0.
+template <typename T>
+__device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift, int n, float (&x)[16]) {
+    if (shift >= 6 && c0 + (16 << shift) <= n) {   // (one address, and no ends to look at)
+        typedef typename Quad<T>::raw raw;
+        const T *p = row + c0 + column(j, shift, 0);
+        raw r[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        bad = bad || !(x[i] < INFINITY);
-        m = fmaxf(m, x[i]);
+        for (int k = 0; k < 4; ++k) __builtin_memcpy(&r[k], p + 256 * k, sizeof(raw));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) Quad<T>::get(r[k], *reinterpret_cast<float(*)[4]>(x + 4 * k));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) load_four(row, c0 + column(j, shift, k), n, *reinterpret_cast<float(*)[4]>(x + 4 * k));
     }
-    return m;
 }
+
+__device__ __forceinline__ float max4(const float *x) { return max2(max3(x[0], x[1], x[2]), x[3]); }
+// maximum of a thread's 16 scores, +inf if a NaN is among them; four[k]: of its k-th four
+__device__ __forceinline__ float own_max(const float (&x)[16], float (&four)[4]) {
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) nan = nan || __builtin_isunordered(x[i], x[i + 1]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) four[k] = max4(x + 4 * k);
+    return nan ? INFINITY : max2(max3(four[0], four[1], four[2]), four[3]);
+}
+// Maximum and sum of a row's scores from `lanes` threads of 16 each, into all of them:
+// several wavefronts of a row each relative to their own maximum, then joined.  The
+// maximum is infinite, and the sum means nothing, where the row has no probabilities.
+template <int NT>
+struct RowSum {
+    float max[NT / 64];
+    double sum[NT / 64];
+};
 // e^x for x <= 0, within a few roundings of 64 bits; below -700 that of -700 (a
 // sum with a term of 1 in it does not see either).  2^(n + f) with |f| <= 1/2: n by
 // adding 1.5 2^52, whose last bits it then is, 2^f = 1 + f q(f) by interpolation of q
@@ -346,8 +414,8 @@ __device__ __forceinline__ double exp_below(double x) {
     double p = q[10];
 #pragma unroll
     for (int i = 9; i >= 0; --i) p = fma(p, f, q[i]);
-    const uint64_t u = (uint64_t)__double_as_longlong(fma(p, f, 1.0));
-    return __longlong_as_double((long long)(u + ((uint64_t)__double_as_longlong(t) << 52)));
+    p = fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
 // sum of e^(x - m), m finite, in 64 bits
 __device__ __forceinline__ double own_sum(const float (&x)[16], float m) {
@@ -357,54 +425,61 @@ __device__ __forceinline__ double own_sum(const float (&x)[16], float m) {
     return s;
 }
 
+template <int NT, bool ALL>   // ALL: every wavefront of the row takes the results, else its first
+__device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const int shift, RowSum<NT> &part) {
+    const int in_wave = min(shift, 6);
+    m = reduce_lanes(m, in_wave, Larger());
+    double sum = 0.0;
+    if (m > -INFINITY && m < INFINITY) sum = own_sum(x, m);
+    sum = reduce_lanes(sum, in_wave, Plus());
+    if constexpr (NT > 64) {
+        if (shift > 6) {
+            if ((threadIdx.x & 63) == 0) {
+                part.max[threadIdx.x >> 6] = m;
+                part.sum[threadIdx.x >> 6] = sum;
+            }
+            __syncthreads();
+            if (!ALL && (threadIdx.x & ((1 << shift) - 1)) >= 64) return sum;
+            // (a lane to each of the row's wavefronts)
+            const int w = (threadIdx.x >> shift << (shift - 6)) + (threadIdx.x & ((1 << (shift - 6)) - 1));
+            const float own = part.max[w];
+            m = reduce_lanes(own, shift - 6, Larger());
+            sum = 0.0;
+            if (m > -INFINITY && m < INFINITY) sum = part.sum[w] * exp_below((double)own - (double)m);
+            sum = reduce_lanes(sum, shift - 6, Plus());
+        }
+    }
+    return sum;
+}
+
 // Searches whose scores fit one block's registers, 16 to a thread.
 template <typename T, int NT, int CAP>
 __global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
     using B = Best<NT, CAP>;
     __shared__ typename B::Shared shared;
-    __shared__ float wave_max[NT / 64];
-    __shared__ double wave_sum[NT / 64];
+    __shared__ RowSum<NT> part;
+    __shared__ uint8_t finished[kMaxWidth];
     const int64_t b = blockIdx.x;
-    const int v = threadIdx.x / A.lanes, j = threadIdx.x % A.lanes;
+    const int v = threadIdx.x >> A.shift, j = threadIdx.x & ((1 << A.shift) - 1);
     B best(shared, A.W);
-    float total = -INFINITY;
+    float total = -INFINITY, x[16];
     bool done = false;
-    if (v < A.V) {
+    if (v < A.V) {   // (nothing waits for another load, though some beams' scores are not needed)
         total = A.total_in[b * A.V + v];
         done = A.done && A.done[b * A.V + v];
+        const T *row = static_cast<const T *>(A.x) + (b * A.V + v) * A.xs;
+        load_row(row, 0, j, A.shift, A.S, x);
+        if (j == 0) finished[v] = done;
     }
     const bool live = total - total == 0.f;
-    float x[16];
-    if (live && !done) {
-        const T *row = static_cast<const T *>(A.x) + (b * A.V + v) * A.xs;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) load_four(row, column(j, A.lanes, k), A.S, *reinterpret_cast<float(*)[4]>(x + 4 * k));
-    } else {
+    if (!live || done) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = -INFINITY;
     }
-    bool bad = false;
-    const float own = own_max(x, bad);
-    // the row's maximum and sum; several wavefronts of a row each relative to their own, then joined
-    const int in_wave = min(A.lanes, 64);
-    float m = reduce_lanes(bad ? INFINITY : own, in_wave, Larger());
-    double sum = m > -INFINITY && m < INFINITY ? own_sum(x, m) : 0.0;
-    sum = reduce_lanes(sum, in_wave, Plus());
-    if constexpr (NT > 64) {
-        if (A.lanes > 64) {
-            if ((threadIdx.x & 63) == 0) {
-                wave_max[threadIdx.x >> 6] = m;
-                wave_sum[threadIdx.x >> 6] = sum;
-            }
-            __syncthreads();
-            const int w0 = v * (A.lanes / 64), w1 = w0 + A.lanes / 64;
-            m = -INFINITY;
-            for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
-            sum = 0.0;
-            if (m > -INFINITY && m < INFINITY)
-                for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp_below((double)wave_max[w] - (double)m);
-        }
-    }
+    float four[4];
+    const float own = own_max(x, four);
+    float m = own;
+    const double sum = row_sum<NT, true>(x, m, A.shift, part);
     // what is added to the scores; a finished beam is its first slice alone
     double off = 0.0;
     float top = own;
@@ -425,81 +500,66 @@ __global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
     best.offer(count, [&](auto put) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            if (x[i] >= least && x[i] > -INFINITY) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
+            if (x[i] >= least && x[i] > -INFINITY) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.shift, i / 4) + i % 4);
     });
     if (!best.offered()) {
+        best.clear();
 #pragma unroll 1
         for (int i = 0; i < 16; ++i) {
             float xi = x[0];
 #pragma unroll
             for (int q = 1; q < 16; ++q) xi = q == i ? x[q] : xi;
-            best.take(top > -INFINITY ? (double)xi + off : -INFINITY, v * A.S + (int32_t)column(j, A.lanes, i / 4) + i % 4);
+            best.take(top > -INFINITY ? (double)xi + off : -INFINITY, v * A.S + (int32_t)column(j, A.shift, i / 4) + i % 4);
         }
     }
-    write_beams(A, b, best);
+    write_beams(A, b, best, finished);
 }
 
 // Rows in parts: a part's maximum and sum, and the maximum of every group of its
-// columns, from one reading of the scores.
-template <typename T>
+// columns, from one reading of the scores.  GROUP: 0, or that of rows of a block each
+// (2^8 threads), whose reductions then are of fixed sizes.
+template <typename T, int GROUP>
 __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
-    __shared__ float wave_max[4];
-    __shared__ double wave_sum[4];
-    const int per = 256 / A.lanes;   // rows of a block, or one of its parts
-    const uint32_t item = blockIdx.x * per + threadIdx.x / A.lanes, at = item / (uint32_t)A.segs;
-    const int64_t row = at;
-    const int32_t seg = (int32_t)(item - at * A.segs);
-    const int j = threadIdx.x % A.lanes;
-    const int64_t c0 = (int64_t)seg * 4096;
-    bool live = row < rows;
-    if (live) {
-        const float t = A.total_in[row];
-        live = t - t == 0.f && !(A.done && A.done[row]);
+    __shared__ RowSum<256> part;
+    const int shift = GROUP ? 8 : A.shift, group = GROUP ? GROUP : A.group;
+    const int j = threadIdx.x & ((1 << shift) - 1);
+    // (several rows to a block have one part each)
+    const uint32_t item = (blockIdx.x << (8 - shift)) + (threadIdx.x >> shift);
+    const uint32_t of = A.segs == 1 ? item : blockIdx.x / (uint32_t)A.segs;
+    const int64_t row = of;
+    const int32_t c0 = (int32_t)(item - of * A.segs) * 4096;
+    float t = -INFINITY, x[16], four[4];
+    bool done = false;
+    if (row < rows) {   // (nothing waits for another load, though some beams' scores are not needed)
+        t = A.total_in[row];
+        done = A.done && A.done[row];
+        load_row(static_cast<const T *>(A.x) + row * A.xs, c0, j, shift, A.S, x);
     }
-    float x[16];
-    if (live) {
-        const T *p = static_cast<const T *>(A.x) + row * A.xs;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) load_four(p, c0 + column(j, A.lanes, k), A.S, *reinterpret_cast<float(*)[4]>(x + 4 * k));
-    } else {
+    const bool live = t - t == 0.f && !done;
+    if (!live) {
+        if (GROUP) return;   // (the block's one row)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = -INFINITY;
     }
-    bool bad = false;
-    const float own = own_max(x, bad);
-    const int in_wave = min(A.lanes, 64);
-    float m = reduce_lanes(bad ? INFINITY : own, in_wave, Larger());
-    double sum = m > -INFINITY && m < INFINITY ? own_sum(x, m) : 0.0;
-    sum = reduce_lanes(sum, in_wave, Plus());
-    if (live) {   // groups' maxima (not used where the row turns out to have no candidates)
+    float m = own_max(x, four);
+    if (live) {   // groups' maxima (not looked at where the row has no candidates)
         float *g = A.group_max + row * A.groups;
-        if (A.group == 1024) {
-            const float w = reduce_lanes(own, 64, Larger());
-            const int64_t c = c0 + column(j, A.lanes, 0);
-            if ((j & 63) == 0 && c < A.S) g[c / 1024] = w;
+        if (group == 10) {
+            const float w = reduce_lanes(m, 6, Larger());
+            const int c = c0 + column(j, shift, 0);
+            if ((j & 63) == 0 && c < A.S) g[c >> 10] = w;
         } else {
-            const int wide = A.group / 4;   // lanes to a group
+            const int wide = group - 2;   // 2^wide lanes to a group
+            const int c = c0 + column(j, shift, 0);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float w = reduce_lanes(fmaxf(fmaxf(x[4 * k], x[4 * k + 1]), fmaxf(x[4 * k + 2], x[4 * k + 3])), wide, Larger());
-                const int64_t c = c0 + column(j, A.lanes, k);
-                if ((j & (wide - 1)) == 0 && c < A.S) g[c / A.group] = w;
+                const float w = reduce_lanes(four[k], wide, Larger());
+                const int ck = GROUP ? c + 256 * k : c0 + column(j, shift, k);
+                if ((j & ((1 << wide) - 1)) == 0 && ck < A.S) g[ck >> group] = w;
             }
         }
     }
-    if (A.lanes > 64) {
-        if ((threadIdx.x & 63) == 0) {
-            wave_max[threadIdx.x >> 6] = m;
-            wave_sum[threadIdx.x >> 6] = sum;
-        }
-        __syncthreads();
-        const int w0 = threadIdx.x / A.lanes * (A.lanes / 64), w1 = w0 + A.lanes / 64;
-        m = -INFINITY;
-        for (int w = w0; w < w1; ++w) m = fmaxf(m, wave_max[w]);
-        sum = 0.0;
-        if (m > -INFINITY && m < INFINITY)
-            for (int w = w0; w < w1; ++w) sum += wave_sum[w] * exp_below((double)wave_max[w] - (double)m);
-    }
+    const double sum = row_sum<256, false>(x, m, shift, part);
     if (live && j == 0) {
         A.seg_max[item] = m;
         A.seg_sum[item] = sum;
@@ -520,10 +580,11 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
     B best(shared, A.W);
     if (threadIdx.x == 0) n_listed = 0;
     // a row by as many threads as it has parts, at most a wavefront
-    int wide = 1;
-    while (wide < 64 && wide < A.segs) wide *= 2;
-    for (int v0 = 0; v0 < A.V; v0 += 1024 / wide) {
-        const int v = v0 + threadIdx.x / wide, i0 = threadIdx.x & (wide - 1);
+    int share = 0;
+    while (share < 6 && 1 << share < A.segs) ++share;
+    const int wide = 1 << share;
+    for (int v0 = 0; v0 < A.V; v0 += 1024 >> share) {
+        const int v = v0 + (threadIdx.x >> share), i0 = threadIdx.x & (wide - 1);
         const int64_t row = b * A.V + v;
         float t = -INFINITY;
         bool fin = false;
@@ -540,13 +601,13 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
         float m = m0;
         if (read)
             for (int i = i0 + wide; i < A.segs; i += wide) m = fmaxf(m, pm[i]);
-        m = reduce_lanes(m, wide, Larger());
+        m = reduce_lanes(m, share, Larger());
         const bool some = m > -INFINITY && m < INFINITY;
         double s = some && m0 > -INFINITY ? s0 * exp_below((double)m0 - (double)m) : 0.0;
         if (some)
             for (int i = i0 + wide; i < A.segs; i += wide)
                 if (pm[i] > -INFINITY) s += ps[i] * exp_below((double)pm[i] - (double)m);
-        s = reduce_lanes(s, wide, Plus());
+        s = reduce_lanes(s, share, Plus());
         if (v < A.V && i0 == 0) {
             off[v] = some ? (double)t - ((double)m + log(s)) : fin && t - t == 0.f ? (double)t : -INFINITY;
             done[v] = fin;
@@ -587,59 +648,69 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
     };
     double top = -INFINITY;
     groups([&](int32_t, double key) { top = key > top ? key : top; });
-    best.raise(top);
-    const int shift = 31 - __clz(A.group), within = A.group - 1;
-    // the candidate at place e of the group `id`
-    auto candidate = [&](int32_t id, int32_t e, double &key, int32_t &idx) {
-        const int32_t v = id / A.groups;
-        const int32_t c = ((id - v * A.groups) << shift) + e;
-        key = -INFINITY;
-        idx = v * A.S + c;
-        if (c >= A.S || !(off[v] > -INFINITY)) return;
-        if (done[v]) key = c == 0 ? off[v] : -INFINITY;
-        else key = (double)score<T>(A, b * A.V + v, c) + off[v];
-    };
-    bool fits = true;
-    if (best.passes(top, -1)) {
-        groups([&](int32_t i, double key) {
-            if (key > -INFINITY && best.passes(key, -1)) {
-                const int at = atomicAdd(&n_listed, 1);
-                if (at < kListed) listed[at] = i;
-            }
-        });
-    }
-    __syncthreads();
-    const int n = n_listed;
-    if (n <= kListed) {
-        for (int32_t e = threadIdx.x; e < n << shift; e += 1024) {
-            double key;
-            int32_t idx;
-            candidate(listed[e >> shift], e & within, key, idx);
-            if (key > -INFINITY && best.passes(key, idx)) best.offer(1, [&](auto put) { put(key, idx); });
+    if (best.raise(top)) {
+        // the groups that reach the bar, then their candidates
+        if (best.passes(top, -1)) {
+            groups([&](int32_t i, double key) {
+                if (key > -INFINITY && best.passes(key, -1)) {
+                    const int at = atomicAdd(&n_listed, 1);
+                    if (at < kListed) listed[at] = i;
+                }
+            });
         }
-        fits = best.offered();
-    }
-    if (n > kListed || !fits) {   // too many at the bar: everything in turn, eight of each thread at a time
-        const int64_t places = (int64_t)total << shift;
-        for (int64_t e0 = threadIdx.x; e0 - threadIdx.x < places; e0 += 8192) {
-            double key[8];
-            int32_t idx[8];
-            int c = 0;
+        __syncthreads();
+        const int n = n_listed, places = min(n, kListed) << A.group;
+        for (int32_t e0 = threadIdx.x; e0 < places; e0 += 4096) {
+            float x[4];
+            double o[4];
+            int32_t idx[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int64_t e = e0 + 1024 * k;
-                key[k] = -INFINITY;
-                idx[k] = 0;
-                if (e < places) candidate((int32_t)(e >> shift), (int32_t)e & within, key[k], idx[k]);
+            for (int k = 0; k < 4; ++k) {
+                const int32_t e = e0 + 1024 * k, id = e < places ? listed[e >> A.group] : 0, v = id / A.groups;
+                const int32_t c = ((id - v * A.groups) << A.group) + (e & ((1 << A.group) - 1));
+                const bool is = e < places && c < A.S && (!done[v] || c == 0);
+                x[k] = !is ? -INFINITY : done[v] ? 0.f : score<T>(A, b * A.V + v, c);
+                o[k] = off[v];
+                idx[k] = v * A.S + c;
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) c += B::lanes(best.passes(key[k], idx[k]));
-            if (best.sum(c) == 0) continue;
+            for (int k = 0; k < 4; ++k) {
+                const double key = (double)x[k] + o[k];
+                if (x[k] > -INFINITY && best.passes(key, idx[k])) best.offer(1, [&](auto put) { put(key, idx[k]); });
+            }
+        }
+        if (best.offered() && n <= kListed) {
+            write_beams(A, b, best, done);
+            return;
+        }
+        best.clear();
+    }
+    // Too few groups to set a bar, or too many candidates at it: the rows that have candidates, one after the other,
+    // four columns of each thread at a time.
+    for (int32_t v = 0; v < A.V; ++v) {
+        const double o = off[v];
+        if (!(o > -INFINITY)) continue;
+        const int32_t S = done[v] ? 1 : A.S;
+        for (int32_t c0 = 0; c0 < S; c0 += 4096) {
+            double key[4];
+            int passing = 0;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) best.take(key[k], idx[k]);
+            for (int k = 0; k < 4; ++k) {
+                const int32_t c = c0 + 1024 * k + threadIdx.x;
+                key[k] = c >= S ? -INFINITY : done[v] ? o : (double)score<T>(A, b * A.V + v, c) + o;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) passing += B::lanes(best.passes(key[k], v * A.S + c0 + 1024 * k + threadIdx.x));
+            if (best.sum(passing) == 0) continue;
+            for (int k = 0; k < 4; ++k) {
+                double q = key[0];
+#pragma unroll
+                for (int i = 1; i < 4; ++i) q = i == k ? key[i] : q;
+                best.take(q, v * A.S + c0 + 1024 * k + (int32_t)threadIdx.x);
+            }
         }
     }
-    write_beams(A, b, best);
+    write_beams(A, b, best, done);
 }
 
 // -------------------------------------------------------------------- reorder
@@ -714,23 +785,24 @@ inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) =
 // The way that a level goes: one launch where each search's scores fit the registers
 // of a block, else rows in parts and a launch that joins them.
 struct Way {
-    int32_t lanes, segs, group, groups;
+    int32_t shift, segs, group, groups;
     bool whole;
     int64_t blocks;   // of the parts
 };
 Way way(int32_t n, int32_t V, int32_t W, int32_t S) {
     Way w{};
-    for (w.lanes = 1; w.lanes < 1024 && 16 * w.lanes < S; w.lanes *= 2) {}
-    w.whole = 16 * w.lanes >= S && V * w.lanes <= 1024;
+    while (w.shift < 10 && 16 << w.shift < S) ++w.shift;
+    w.whole = 16 << w.shift >= S && V << w.shift <= 1024;
     if (w.whole) return w;
-    w.lanes = std::min(w.lanes, 256);
+    w.shift = std::min(w.shift, 8);
     w.segs = (int32_t)((S + 4095ll) / 4096);
-    // groups: few enough to be looked at twice by one block, and so many that a row's own best set a bar
-    const int32_t most = w.lanes >= 64 ? 1024 : 4 * w.lanes;
-    for (w.group = 16; 4 * w.group <= most && (int64_t)4 * w.group * W <= S && (int64_t)V * (S / w.group) > 16384;) w.group *= 4;
-    w.groups = (S + w.group - 1) / w.group;
-    const int64_t per = 256 / w.lanes, items = (int64_t)n * V * w.segs;
-    w.blocks = (items + per - 1) / per;
+    // Groups: of their V S / 2^g maxima each is looked at twice, of about W of them all 2^g scores are read again, at
+    // about equal costs where 4^g is some 3 V S / W.
+    const int32_t most = w.shift >= 6 ? 10 : w.shift + 2;
+    for (w.group = 4; w.group + 2 <= most && ((int64_t)W << (2 * w.group + 2)) < (int64_t)3 * V * S;) w.group += 2;
+    w.groups = (int32_t)((S + (1ll << w.group) - 1) >> w.group);
+    const int64_t items = (int64_t)n * V * w.segs;
+    w.blocks = (items + (256 >> w.shift) - 1) >> (8 - w.shift);
     return w;
 }
 size_t carve(int32_t n, int32_t V, const Way &w, void *base, BeamArgs *A) {
@@ -746,13 +818,19 @@ size_t carve(int32_t n, int32_t V, const Way &w, void *base, BeamArgs *A) {
 template <typename T>
 void launch_select(const BeamArgs &A, const Way &w, int32_t n, hipStream_t st) {
     if (w.whole) {
-        const int threads = A.V * A.lanes;
+        const int threads = A.V << A.shift;
         if (threads <= 64) beam_whole<T, 64, 320><<<n, 64, 0, st>>>(A);
         else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A);
         else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A);
         return;
     }
-    beam_parts<T><<<(unsigned)w.blocks, 256, 0, st>>>(A, (int64_t)n * A.V);
+    const int64_t rows = (int64_t)n * A.V;
+    const unsigned blocks = (unsigned)w.blocks;
+    if (w.shift < 8) beam_parts<T, 0><<<blocks, 256, 0, st>>>(A, rows);
+    else if (w.group == 4) beam_parts<T, 4><<<blocks, 256, 0, st>>>(A, rows);
+    else if (w.group == 6) beam_parts<T, 6><<<blocks, 256, 0, st>>>(A, rows);
+    else if (w.group == 8) beam_parts<T, 8><<<blocks, 256, 0, st>>>(A, rows);
+    else beam_parts<T, 10><<<blocks, 256, 0, st>>>(A, rows);
     beam_join<T><<<n, 1024, 0, st>>>(A);
 }
 
@@ -831,7 +909,7 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
     A.x = scores; A.xs = score_stride;
     A.total_in = total_in; A.done = done;
     A.total = total; A.parent = parent; A.slice = slice;
-    A.lanes = w.lanes; A.segs = w.segs; A.group = w.group; A.groups = w.groups;
+    A.shift = w.shift; A.segs = w.segs; A.group = w.group; A.groups = w.groups;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (dtype == TAG_BF16) launch_select<uint16_t>(A, w, n_search, stream);
     else launch_select<float>(A, w, n_search, stream);
