@@ -116,7 +116,7 @@ struct Plus {
 template <int NT, int CAP>
 struct Best {
     static_assert(CAP % NT == 0 && CAP >= NT + kMaxWidth, "room for a candidate of each thread beside the best W");
-    static constexpr int kWaves = NT / 64, kOwn = CAP / NT;
+    static constexpr int kWaves = NT / 64, kOwn = CAP / NT, kRanked = CAP < 512 ? CAP : 512;
     struct Shared {
         double key[CAP];
         int32_t idx[CAP];
@@ -124,12 +124,16 @@ struct Best {
         uint64_t count3[2][kWaves];
         unsigned ends[2][kWaves];
         int32_t tail;
+        __attribute__((aligned(16))) unsigned half[kRanked];
+        int32_t same[kRanked];
     };
     Shared &s;
     const int W;
     double bar = -INFINITY;      // a candidate passes above it, or at it up to the index
     int32_t bar_idx = -1;
     int n = 0, flip = 0;         // entries of the list
+    uint64_t base = 0;           // keys less base, without `drop` bits, fit 32 bits
+    int drop = 32;
 
     // (a barrier follows before the first candidate: raise's)
     __device__ Best(Shared &s_, int w) : s(s_), W(w) {
@@ -185,6 +189,7 @@ struct Best {
             __syncthreads();
         }
         if (live < W) return false;
+        const unsigned best = hi;
         const int most = W + max(W / 2, 8);
         while (lo < hi) {   // W reach lo, fewer reach hi + 1; three probes between them to a turn
             const unsigned step = (hi - lo) / 4, t1 = lo + step + 1, t2 = t1 + step, t3 = min(t2 + step, hi);
@@ -196,7 +201,9 @@ struct Best {
             lo = t;
             if (c <= most) break;
         }
-        bar = unordered((uint64_t)lo << 32);
+        base = (uint64_t)lo << 32;
+        drop = max(0, 32 - __clzll(((uint64_t)best << 32 | 0xffffffffull) - base));
+        bar = unordered(base);
         bar_idx = INT32_MAX;
         return true;
     }
@@ -304,23 +311,56 @@ struct Best {
         bar = unordered(K);
         bar_idx = last;
     }
-    // each(rank, key, index) of the best, at most W; returns how many
+    // each(rank, key, index) of the best, at most W; returns how many.  An entry's rank is
+    // the number of better ones, counted by 32 bits of the ordered keys (of the range
+    // between the bar and the best), four at a time and shared by several threads;
+    // where these are equal, the entries themselves decide.
     template <typename Each>
     __device__ int ranked(Each each) {
-        if (n > kMaxWidth && n > W) keep_best();
+        if (n > kRanked) keep_best();
         __syncthreads();
-        // several threads to an entry, which share the comparisons
+        for (int i = threadIdx.x; i < (n + 3) / 4 * 4; i += NT) {
+            const uint64_t u = i < n ? ordered(s.key[i]) : 0ull;
+            s.half[i] = u > base ? (unsigned)((u - base) >> drop) : 0u;
+        }
+        for (int i = threadIdx.x; i < n; i += NT) s.same[i] = 0;
+        __syncthreads();
         int share = 0;
         while (share < 4 && n << (share + 1) <= NT) ++share;
         const int p = threadIdx.x & ((1 << share) - 1);
-        for (int i0 = 0; i0 < n; i0 += NT >> share) {
-            const int i = i0 + (threadIdx.x >> share);
-            const double k = i < n ? s.key[i] : 0.0;
-            const int32_t x = i < n ? s.idx[i] : 0;
-            int r = 0;
-            for (int j = p; j < n; j += 1 << share) r += s.key[j] > k || (s.key[j] == k && s.idx[j] < x);
-            r = (int)reduce_lanes((unsigned)r, share, Plus());
-            if (i < n && p == 0 && r < W) each(r, k, x);
+        constexpr int kTurns = (kRanked + NT - 1) / NT;
+        int rank[kTurns];
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int i = t * (NT >> share) + (threadIdx.x >> share);
+            if (t * (NT >> share) >= n) break;
+            const unsigned h = i < n ? s.half[i] : ~0u;
+            unsigned r = 0;
+            for (int j = 4 * p; j < n; j += 4 << share) {
+                const uint4 o = *reinterpret_cast<const uint4 *>(s.half + j);
+                r += (o.x > h) + (o.y > h) + (o.z > h) + (o.w > h);
+            }
+            rank[t] = (int)reduce_lanes(r, share, Plus());
+            if (i < n && p == 0) atomicAdd(&s.same[rank[t]], 1);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t) {
+            const int i = t * (NT >> share) + (threadIdx.x >> share);
+            if (i >= n || p != 0) continue;
+            int r = rank[t];
+            const double k = s.key[i];
+            const int32_t x = s.idx[i];
+            if (s.same[r] > 1) {
+                const unsigned h = s.half[i];
+                for (int j = 0; j < n; j += 4) {
+                    const uint4 o = *reinterpret_cast<const uint4 *>(s.half + j);
+                    if (o.x != h && o.y != h && o.z != h && o.w != h) continue;
+                    for (int q = j; q < min(j + 4, n); ++q)
+                        if (s.half[q] == h) r += s.key[q] > k || (s.key[q] == k && s.idx[q] < x);
+                }
+            }
+            if (r < W) each(r, k, x);
         }
         return min(n, W);
     }
@@ -575,10 +615,20 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
     __shared__ B::Shared shared;
     __shared__ double off[kMaxWidth];   // -inf: no candidates
     __shared__ uint8_t done[kMaxWidth];
-    __shared__ int32_t listed[kListed], n_listed;
+    __shared__ int32_t list_column[kListed], n_listed;
+    __shared__ uint8_t list_row[kListed];
     const int64_t b = blockIdx.x;
     B best(shared, A.W);
     if (threadIdx.x == 0) n_listed = 0;
+    constexpr int kHeld = 16;   // groups' maxima in a thread's registers
+    const int32_t total = A.V * A.groups;
+    const float *maxima = A.group_max + b * total;
+    float held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) {
+        const int32_t i = threadIdx.x + 1024 * k;
+        held[k] = i < total ? maxima[i] : -INFINITY;
+    }
     // a row by as many threads as it has parts, at most a wavefront
     int share = 0;
     while (share < 6 && 1 << share < A.segs) ++share;
@@ -613,22 +663,25 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
             done[v] = fin;
         }
     }
-    __syncthreads();
-    // every group's best candidate: each(group, key)
-    const int32_t total = A.V * A.groups, up = 1024 / A.groups, rest = 1024 % A.groups;
-    const float *maxima = A.group_max + b * total;
+    // every group's best candidate: each(row, group of the row, key), the first kHeld of a thread from registers
+    const int32_t up = 1024 / A.groups, rest = 1024 % A.groups;
+    __syncthreads();   // (the rows' offsets)
     auto groups = [&](auto each) {
-        constexpr int U = 8;
-        int32_t v = threadIdx.x / A.groups, g = threadIdx.x % A.groups;
-        for (int32_t i = threadIdx.x; i < total; i += U * 1024) {
-            float m[U];
-            int32_t row[U];
-            bool first[U];
+        int32_t v = threadIdx.x / A.groups, g = threadIdx.x - v * A.groups;
+        for (int32_t i0 = threadIdx.x; i0 < total; i0 += 1024 * kHeld) {
+            float m[kHeld];
 #pragma unroll
-            for (int k = 0; k < U; ++k) {
-                m[k] = i + 1024 * k < total ? maxima[i + 1024 * k] : -INFINITY;
-                row[k] = v;
-                first[k] = g == 0;
+            for (int k = 0; k < kHeld; ++k) {
+                const int32_t i = i0 + 1024 * k;
+                m[k] = i0 < 1024 ? held[k] : i < total ? maxima[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int k = 0; k < kHeld; ++k) {
+                if (i0 + 1024 * k >= total) break;
+                const double o = off[v];   // (what stands there for rows without candidates is not looked at)
+                double key = -INFINITY;
+                if (o > -INFINITY) key = done[v] ? (g == 0 ? o : -INFINITY) : (double)m[k] + o;
+                each(v, g, key);
                 v += up;
                 g += rest;
                 if (g >= A.groups) {
@@ -636,47 +689,44 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
                     ++v;
                 }
             }
-#pragma unroll
-            for (int k = 0; k < U; ++k) {
-                if (i + 1024 * k >= total) continue;
-                const double o = off[row[k]];
-                double key = -INFINITY;   // (what stands there for rows without candidates is not looked at)
-                if (o > -INFINITY) key = done[row[k]] ? (first[k] ? o : -INFINITY) : (double)m[k] + o;
-                each(i + 1024 * k, key);
-            }
         }
     };
     double top = -INFINITY;
-    groups([&](int32_t, double key) { top = key > top ? key : top; });
+    groups([&](int32_t, int32_t, double key) { top = key > top ? key : top; });
     if (best.raise(top)) {
         // the groups that reach the bar, then their candidates
         if (best.passes(top, -1)) {
-            groups([&](int32_t i, double key) {
+            groups([&](int32_t v, int32_t g, double key) {
                 if (key > -INFINITY && best.passes(key, -1)) {
                     const int at = atomicAdd(&n_listed, 1);
-                    if (at < kListed) listed[at] = i;
+                    if (at < kListed) {
+                        list_row[at] = (uint8_t)v;
+                        list_column[at] = g << A.group;
+                    }
                 }
             });
         }
         __syncthreads();
         const int n = n_listed, places = min(n, kListed) << A.group;
-        for (int32_t e0 = threadIdx.x; e0 < places; e0 += 4096) {
-            float x[4];
-            double o[4];
-            int32_t idx[4];
+        for (int32_t e0 = threadIdx.x; e0 < places; e0 += 8192) {
+            float x[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int32_t e = e0 + 1024 * k, id = e < places ? listed[e >> A.group] : 0, v = id / A.groups;
-                const int32_t c = ((id - v * A.groups) << A.group) + (e & ((1 << A.group) - 1));
-                const bool is = e < places && c < A.S && (!done[v] || c == 0);
-                x[k] = !is ? -INFINITY : done[v] ? 0.f : score<T>(A, b * A.V + v, c);
-                o[k] = off[v];
-                idx[k] = v * A.S + c;
+            for (int k = 0; k < 8; ++k) {
+                const int32_t e = e0 + 1024 * k;
+                x[k] = -INFINITY;
+                if (e < places) {
+                    const int32_t v = list_row[e >> A.group], c = list_column[e >> A.group] + (e & ((1 << A.group) - 1));
+                    if (done[v]) x[k] = c == 0 ? 0.f : -INFINITY;
+                    else if (c < A.S) x[k] = score<T>(A, b * A.V + v, c);
+                }
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const double key = (double)x[k] + o[k];
-                if (x[k] > -INFINITY && best.passes(key, idx[k])) best.offer(1, [&](auto put) { put(key, idx[k]); });
+            for (int k = 0; k < 8; ++k) {
+                const int32_t e = e0 + 1024 * k;
+                if (!(x[k] > -INFINITY)) continue;
+                const int32_t v = list_row[e >> A.group], c = list_column[e >> A.group] + (e & ((1 << A.group) - 1));
+                const double key = (double)x[k] + off[v];
+                if (best.passes(key, v * A.S + c)) best.offer(1, [&](auto put) { put(key, v * A.S + c); });
             }
         }
         if (best.offered() && n <= kListed) {
