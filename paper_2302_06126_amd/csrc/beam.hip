@@ -115,18 +115,28 @@ struct Plus {
 // result does not depend on the order in which they came.
 template <int NT, int CAP>
 struct Best {
+    static_assert(NT == 64 || NT == 256 || NT == 1024, "1, 4 or 16 wavefronts");
     static_assert(CAP % NT == 0 && CAP >= NT + kMaxWidth, "room for a candidate of each thread beside the best W");
-    static constexpr int kWaves = NT / 64, kOwn = CAP / NT, kRanked = CAP < 512 ? CAP : 512;
+    static constexpr int kThreads = NT, kWaves = NT / 64, kOwn = CAP / NT, kRanked = CAP < 512 ? CAP : 512;
     struct Shared {
         double key[CAP];
         int32_t idx[CAP];
-        int32_t count[2][kWaves];
-        uint64_t count3[2][kWaves];
+        unsigned count[2][kWaves];
         unsigned ends[2][kWaves];
         int32_t tail;
         __attribute__((aligned(16))) unsigned half[kRanked];
         int32_t same[kRanked];
     };
+    // (a search of one wavefront shares its block with others)
+    static __device__ __forceinline__ int tid() { return threadIdx.x % NT; }
+    static __device__ __forceinline__ void sync() {
+        if constexpr (NT > 64) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
     Shared &s;
     const int W;
     double bar = -INFINITY;      // a candidate passes above it, or at it up to the index
@@ -137,33 +147,18 @@ struct Best {
 
     // (a barrier follows before the first candidate: raise's)
     __device__ Best(Shared &s_, int w) : s(s_), W(w) {
-        if (threadIdx.x == 0) s.tail = 0;
+        if (tid() == 0) s.tail = 0;
     }
     __device__ bool passes(double key, int32_t idx) const { return key > bar || (key == bar && idx <= bar_idx); }
     static __device__ int lanes(bool b) { return __popcll(__ballot(b)); }
     // sum over the wavefronts of a number that each wavefront's lanes share
     __device__ int sum(int v) {
         if constexpr (kWaves == 1) return v;
-        if ((threadIdx.x & 63) == 0) s.count[flip][threadIdx.x >> 6] = v;
-        __syncthreads();
-        int r = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) r += s.count[flip][i];
+        if ((tid() & 63) == 0) s.count[flip][tid() >> 6] = (unsigned)v;
+        sync();
+        const unsigned r = reduce_lanes(s.count[flip][tid() & (kWaves - 1)], kWaves == 16 ? 4 : 2, Plus());
         flip ^= 1;   // (written again only after the next barrier, which follows these reads)
-        return r;
-    }
-    // the same of three numbers up to NT
-    __device__ void sum3(int &a, int &b, int &c) {
-        if constexpr (kWaves == 1) return;
-        if ((threadIdx.x & 63) == 0) s.count3[flip][threadIdx.x >> 6] = (uint64_t)a | (uint64_t)b << 16 | (uint64_t)c << 32;
-        __syncthreads();
-        uint64_t r = 0;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) r += s.count3[flip][i];
-        flip ^= 1;
-        a = (int)(r & 0xffff);
-        b = (int)(r >> 16 & 0xffff);
-        c = (int)(r >> 32);
+        return __builtin_amdgcn_readfirstlane((int)r);
     }
     // Sets the bar from one candidate of each thread, the best that it has: as high
     // as W threads, or a few more, still pass (false: fewer have one).  Bisection of the upper halves of the
@@ -173,9 +168,9 @@ struct Best {
         unsigned hi = reduce_lanes(u, 6, Larger()), lo = reduce_lanes(u ? u : ~0u, 6, Smaller());
         int live = lanes(u != 0);
         if constexpr (kWaves > 1) {
-            if ((threadIdx.x & 63) == 0) {
-                s.ends[0][threadIdx.x >> 6] = hi;
-                s.ends[1][threadIdx.x >> 6] = lo;
+            if ((tid() & 63) == 0) {
+                s.ends[0][tid() >> 6] = hi;
+                s.ends[1][tid() >> 6] = lo;
             }
         }
         live = sum(live);   // (and its barrier)
@@ -186,15 +181,16 @@ struct Best {
                 lo = min(lo, s.ends[1][i]);
             }
         } else {
-            __syncthreads();
+            sync();
         }
         if (live < W) return false;
         const unsigned best = hi;
         const int most = W + max(W / 2, 8);
         while (lo < hi) {   // W reach lo, fewer reach hi + 1; three probes between them to a turn
             const unsigned step = (hi - lo) / 4, t1 = lo + step + 1, t2 = t1 + step, t3 = min(t2 + step, hi);
-            int c1 = lanes(u >= t1), c2 = lanes(u >= t2), c3 = lanes(u >= t3);
-            sum3(c1, c2, c3);
+            // (fewer than 1,024 each: some thread is at lo or below)
+            const unsigned all = (unsigned)sum(lanes(u >= t1) | lanes(u >= t2) << 10 | lanes(u >= t3) << 20);
+            const int c1 = all & 1023, c2 = all >> 10 & 1023, c3 = all >> 20;
             const unsigned t = c3 >= W ? t3 : c2 >= W ? t2 : c1 >= W ? t1 : lo;
             const int c = c3 >= W ? c3 : c2 >= W ? c2 : c1 >= W ? c1 : INT32_MAX;
             if (c3 < W) hi = (c2 >= W ? t3 : c1 >= W ? t2 : t1) - 1;
@@ -207,19 +203,30 @@ struct Best {
         bar_idx = INT32_MAX;
         return true;
     }
-    // A score below which no score + off passes: the bar less off, by more than the roundings of either may be.
+    // A score below which no score + off passes: the bar less off, by more than the roundings of either may be
+    // (above -inf, which is no candidate).
     __device__ float least_score(double off) const {
-        if (!(bar > -INFINITY)) return -INFINITY;
+        constexpr float lowest = -3.4028234664e38f;
+        if (!(bar > -INFINITY)) return lowest;
         const double d = bar - off - 0x1p-50 * (fabs(bar) + fabs(off));
         const float f = (float)d;
-        return f - fabsf(f) * 0x1p-22f - 0x1p-140f;
+        return fmaxf(f - fabsf(f) * 0x1p-22f - 0x1p-140f, lowest);
     }
-    // A thread's candidates that are likely to fit: `each(put)` calls put(key, index) for
-    // `count` of them that pass.  Then all of them, whether they did.
+    // Candidates that are likely to fit: of each thread `count`, which each(put) gives to
+    // put(key, index).  A wavefront calls it together.  offered: all, whether they did.
     template <typename Each>
     __device__ void offer(int count, Each each) {
-        if (count == 0) return;
-        int at = atomicAdd(&s.tail, count);
+        int before = 0, all = 0;
+        for (int b = 0;; ++b) {   // (over lanes, bit by bit: counts are small)
+            if (__ballot(count >> b) == 0) break;
+            const uint64_t m = __ballot(count >> b & 1);
+            before += __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0)) << b;
+            all += __popcll(m) << b;
+        }
+        if (all == 0) return;
+        int at = 0;
+        if ((tid() & 63) == 0) at = atomicAdd(&s.tail, all);
+        at = __builtin_amdgcn_readfirstlane(at) + before;
         each([&](double key, int32_t idx) {
             if (at < CAP) {
                 s.key[at] = key;
@@ -229,15 +236,15 @@ struct Best {
         });
     }
     __device__ bool offered() {
-        __syncthreads();
+        sync();
         n = s.tail;
         return n <= CAP;
     }
     __device__ void clear() {
-        __syncthreads();
-        if (threadIdx.x == 0) s.tail = 0;
+        sync();
+        if (tid() == 0) s.tail = 0;
         n = 0;
-        __syncthreads();
+        sync();
     }
     // one candidate of each thread (key -inf: none), however many pass
     __device__ void take(double key, int32_t idx) {
@@ -252,10 +259,10 @@ struct Best {
     __device__ void append(bool is, double key, int32_t idx) {
         const uint64_t m = __ballot(is);
         if (m == 0) return;
-        const int lane = threadIdx.x & 63;
         int at = 0;
-        if (lane == 0) at = atomicAdd(&s.tail, __popcll(m));
-        at = __shfl(at, 0, 64) + __popcll(m & ((1ull << lane) - 1ull));
+        if ((tid() & 63) == 0) at = atomicAdd(&s.tail, __popcll(m));
+        at = __builtin_amdgcn_readfirstlane(at) +
+             __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0));
         if (is) {
             s.key[at] = key;
             s.idx[at] = idx;
@@ -263,12 +270,12 @@ struct Best {
     }
     // leaves the best W of a list of more
     __device__ void keep_best() {
-        __syncthreads();
+        sync();
         uint64_t u[kOwn];
         int32_t idx[kOwn];
 #pragma unroll
         for (int r = 0; r < kOwn; ++r) {
-            const int at = threadIdx.x + NT * r;
+            const int at = tid() + NT * r;
             u[r] = at < n ? ordered(s.key[at]) : 0ull;
             idx[r] = at < n ? s.idx[at] : 0;
         }
@@ -301,9 +308,9 @@ struct Best {
                 if (sum(c) < need) last += 1 << b;
             }
         }
-        __syncthreads();   // (of one wavefront, sum has none)
-        if (threadIdx.x == 0) s.tail = 0;
-        __syncthreads();
+        sync();   // (of one wavefront, sum has none)
+        if (tid() == 0) s.tail = 0;
+        sync();
 #pragma unroll
         for (int r = 0; r < kOwn; ++r)
             append(u[r] > K || (u[r] == K && u[r] != 0 && idx[r] <= last), unordered(u[r]), idx[r]);
@@ -318,21 +325,21 @@ struct Best {
     template <typename Each>
     __device__ int ranked(Each each) {
         if (n > kRanked) keep_best();
-        __syncthreads();
-        for (int i = threadIdx.x; i < (n + 3) / 4 * 4; i += NT) {
+        sync();
+        for (int i = tid(); i < (n + 3) / 4 * 4; i += NT) {
             const uint64_t u = i < n ? ordered(s.key[i]) : 0ull;
             s.half[i] = u > base ? (unsigned)((u - base) >> drop) : 0u;
         }
-        for (int i = threadIdx.x; i < n; i += NT) s.same[i] = 0;
-        __syncthreads();
+        for (int i = tid(); i < n; i += NT) s.same[i] = 0;
+        sync();
         int share = 0;
         while (share < 4 && n << (share + 1) <= NT) ++share;
-        const int p = threadIdx.x & ((1 << share) - 1);
+        const int p = tid() & ((1 << share) - 1);
         constexpr int kTurns = (kRanked + NT - 1) / NT;
         int rank[kTurns];
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
-            const int i = t * (NT >> share) + (threadIdx.x >> share);
+            const int i = t * (NT >> share) + (tid() >> share);
             if (t * (NT >> share) >= n) break;
             const unsigned h = i < n ? s.half[i] : ~0u;
             unsigned r = 0;
@@ -343,10 +350,10 @@ struct Best {
             rank[t] = (int)reduce_lanes(r, share, Plus());
             if (i < n && p == 0) atomicAdd(&s.same[rank[t]], 1);
         }
-        __syncthreads();
+        sync();
 #pragma unroll
         for (int t = 0; t < kTurns; ++t) {
-            const int i = t * (NT >> share) + (threadIdx.x >> share);
+            const int i = t * (NT >> share) + (tid() >> share);
             if (i >= n || p != 0) continue;
             int r = rank[t];
             const double k = s.key[i];
@@ -379,7 +386,7 @@ __device__ __forceinline__ void write_beams(const BeamArgs &A, int64_t b, B &bes
         A.parent[b * A.W + r] = v;
         A.slice[b * A.W + r] = done[v] ? -1 : idx - v * A.S;
     });
-    for (int r = n + threadIdx.x; r < A.W; r += blockDim.x) {
+    for (int r = n + B::tid(); r < A.W; r += B::kThreads) {
         A.total[b * A.W + r] = -INFINITY;
         A.parent[b * A.W + r] = A.slice[b * A.W + r] = -1;
     }
@@ -407,12 +414,13 @@ __device__ __forceinline__ int column(int j, int shift, int k) {
 // A thread's 16 columns of a row of n, or of its part from c0.
 template <typename T>
 __device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift, int n, float (&x)[16]) {
-    if (shift >= 6 && c0 + (16 << shift) <= n) {   // (one address, and no ends to look at)
+    if (c0 + (16 << shift) <= n) {   // (one address, and no ends to look at)
         typedef typename Quad<T>::raw raw;
         const T *p = row + c0 + column(j, shift, 0);
+        const int step = shift < 6 ? 4 << shift : 256;
         raw r[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) __builtin_memcpy(&r[k], p + 256 * k, sizeof(raw));
+        for (int k = 0; k < 4; ++k) __builtin_memcpy(&r[k], p + step * k, sizeof(raw));
 #pragma unroll
         for (int k = 0; k < 4; ++k) Quad<T>::get(r[k], *reinterpret_cast<float(*)[4]>(x + 4 * k));
     } else {
@@ -422,16 +430,33 @@ __device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift,
 }
 
 __device__ __forceinline__ float max4(const float *x) { return max2(max3(x[0], x[1], x[2]), x[3]); }
-// maximum of a thread's 16 scores, +inf if a NaN is among them; four[k]: of its k-th four
+// maximum of a thread's scores, +inf if a NaN is among them; four[k]: of its k-th four
 __device__ __forceinline__ float own_max(const float (&x)[16], float (&four)[4]) {
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < 16; i += 2) nan = nan || __builtin_isunordered(x[i], x[i + 1]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) four[k] = max4(x + 4 * k);
-    return nan ? INFINITY : max2(max3(four[0], four[1], four[2]), four[3]);
+    return nan ? INFINITY : max4(four);
 }
-// Maximum and sum of a row's scores from `lanes` threads of 16 each, into all of them:
+// x[i], bit by bit of i (an index that is not known, and selects that stand for one, would
+// put x in memory)
+template <int E>
+__device__ __forceinline__ float pick(const float (&x)[E], int i) {
+    unsigned h[E];
+#pragma unroll
+    for (int k = 0; k < E; ++k) h[k] = __float_as_uint(x[k]);
+#pragma unroll
+    for (int n = E / 2; n > 0; n /= 2) {
+        const unsigned m = 0u - (i & 1);
+#pragma unroll
+        for (int k = 0; k < E / 2; ++k)
+            if (k < n) h[k] = (h[2 * k + 1] & m) | (h[2 * k] & ~m);
+        i >>= 1;
+    }
+    return __uint_as_float(h[0]);
+}
+// Maximum and sum of a row's scores from 2^shift threads of 16 each, into all of them:
 // several wavefronts of a row each relative to their own maximum, then joined.  The
 // maximum is infinite, and the sum means nothing, where the row has no probabilities.
 template <int NT>
@@ -443,7 +468,7 @@ struct RowSum {
 // sum with a term of 1 in it does not see either).  2^(n + f) with |f| <= 1/2: n by
 // adding 1.5 2^52, whose last bits it then is, 2^f = 1 + f q(f) by interpolation of q
 // at eleven Chebyshev points (2e-17 off).  18 instructions, of the fp32 rate: 42,496 x
-// 256 scores 30 -> TIME us against the library's exp.
+// 256 scores 31 -> 26 us against the library's exp.
 __device__ __forceinline__ double exp_below(double x) {
     constexpr double q[11] = {0.6931471805599453,    0.24022650695910097,   0.0555041086648216,    0.009618129107606888,
                               0.0013333558146416936, 0.0001540353044173605, 1.525273382983612e-05, 1.321544258792169e-06,
@@ -492,15 +517,21 @@ __device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const 
     return sum;
 }
 
-// Searches whose scores fit one block's registers, 16 to a thread.
+// Searches whose scores fit one block's registers; those of one wavefront, four to a
+// block.
+constexpr int whole_block(int NT) { return NT > 64 ? NT : 256; }
 template <typename T, int NT, int CAP>
-__global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
+__global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_t n) {
     using B = Best<NT, CAP>;
-    __shared__ typename B::Shared shared;
+    constexpr int kSearches = whole_block(NT) / NT;
+    __shared__ typename B::Shared shared_[kSearches];
     __shared__ RowSum<NT> part;
-    __shared__ uint8_t finished[kMaxWidth];
-    const int64_t b = blockIdx.x;
-    const int v = threadIdx.x >> A.shift, j = threadIdx.x & ((1 << A.shift) - 1);
+    __shared__ uint8_t finished_[kSearches][kMaxWidth];
+    const int64_t b = (int64_t)blockIdx.x * kSearches + threadIdx.x / NT;
+    if (b >= n) return;
+    typename B::Shared &shared = shared_[threadIdx.x / NT];
+    uint8_t *finished = finished_[threadIdx.x / NT];
+    const int v = B::tid() >> A.shift, j = B::tid() & ((1 << A.shift) - 1);
     B best(shared, A.W);
     float total = -INFINITY, x[16];
     bool done = false;
@@ -534,23 +565,20 @@ __global__ void __launch_bounds__(NT) beam_whole(BeamArgs A) {
     best.raise((double)top + off);
     // what may pass, by a bound on the scores that is a little lower (a superset will do)
     const float least = top > -INFINITY ? best.least_score(off) : __builtin_nanf("");   // (nothing is at or above that)
-    int count = 0;
+    unsigned mask = 0;   // the first in bit 15
 #pragma unroll
-    for (int i = 0; i < 16; ++i) count += x[i] >= least && x[i] > -INFINITY;
-    best.offer(count, [&](auto put) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (x[i] >= least && x[i] > -INFINITY) put((double)x[i] + off, v * A.S + (int32_t)column(j, A.shift, i / 4) + i % 4);
+    for (int i = 0; i < 16; ++i) mask = mask + mask + (x[i] >= least);
+    auto index = [&](int i) { return v * A.S + column(j, A.shift, i / 4) + i % 4; };
+    best.offer(__popc(mask), [&](auto put) {
+        for (unsigned m = mask; m; m &= m - 1) {
+            const int i = 16 - __ffs((int)m);
+            put((double)pick(x, i) + off, index(i));
+        }
     });
     if (!best.offered()) {
         best.clear();
 #pragma unroll 1
-        for (int i = 0; i < 16; ++i) {
-            float xi = x[0];
-#pragma unroll
-            for (int q = 1; q < 16; ++q) xi = q == i ? x[q] : xi;
-            best.take(top > -INFINITY ? (double)xi + off : -INFINITY, v * A.S + (int32_t)column(j, A.shift, i / 4) + i % 4);
-        }
+        for (int i = 0; i < 16; ++i) best.take(top > -INFINITY ? (double)pick(x, i) + off : -INFINITY, index(i));
     }
     write_beams(A, b, best, finished);
 }
@@ -646,8 +674,13 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
         const float *pm = A.seg_max + row * A.segs;
         const double *ps = A.seg_sum + row * A.segs;
         // (the first part of each thread's at once)
-        const float m0 = read && i0 < A.segs ? pm[i0] : -INFINITY;
-        const double s0 = read && i0 < A.segs ? ps[i0] : 0.0;
+        float m0 = -INFINITY;
+        double s0 = 0.0;
+        if (v < A.V && i0 < A.segs) {   // (what stands there for a beam that does not read its scores is dropped)
+            m0 = pm[i0];
+            s0 = ps[i0];
+        }
+        if (!read) m0 = -INFINITY;
         float m = m0;
         if (read)
             for (int i = i0 + wide; i < A.segs; i += wide) m = fmaxf(m, pm[i]);
@@ -708,7 +741,7 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
         }
         __syncthreads();
         const int n = n_listed, places = min(n, kListed) << A.group;
-        for (int32_t e0 = threadIdx.x; e0 < places; e0 += 8192) {
+        for (int32_t e0 = threadIdx.x; e0 - (int32_t)threadIdx.x < places; e0 += 8192) {
             float x[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -720,14 +753,19 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
                     else if (c < A.S) x[k] = score<T>(A, b * A.V + v, c);
                 }
             }
+            unsigned mask = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int32_t e = e0 + 1024 * k;
-                if (!(x[k] > -INFINITY)) continue;
-                const int32_t v = list_row[e >> A.group], c = list_column[e >> A.group] + (e & ((1 << A.group) - 1));
-                const double key = (double)x[k] + off[v];
-                if (best.passes(key, v * A.S + c)) best.offer(1, [&](auto put) { put(key, v * A.S + c); });
+                if (x[k] > -INFINITY && best.passes((double)x[k] + off[list_row[e >> A.group]], -1)) mask |= 1u << k;
             }
+            best.offer(__popc(mask), [&](auto put) {
+                for (unsigned m = mask; m; m &= m - 1) {
+                    const int k = __ffs((int)m) - 1;
+                    const int32_t e = e0 + 1024 * k, v = list_row[e >> A.group];
+                    put((double)pick(x, k) + off[v], v * A.S + list_column[e >> A.group] + (e & ((1 << A.group) - 1)));
+                }
+            });
         }
         if (best.offered() && n <= kListed) {
             write_beams(A, b, best, done);
@@ -869,9 +907,10 @@ template <typename T>
 void launch_select(const BeamArgs &A, const Way &w, int32_t n, hipStream_t st) {
     if (w.whole) {
         const int threads = A.V << A.shift;
-        if (threads <= 64) beam_whole<T, 64, 320><<<n, 64, 0, st>>>(A);
-        else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A);
-        else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A);
+        const unsigned four = (unsigned)((n + 3) / 4);
+        if (threads <= 64) beam_whole<T, 64, 320><<<four, 256, 0, st>>>(A, n);
+        else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A, n);
+        else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A, n);
         return;
     }
     const int64_t rows = (int64_t)n * A.V;
