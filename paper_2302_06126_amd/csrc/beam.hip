@@ -802,21 +802,19 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
 }
 
 // -------------------------------------------------------------------- reorder
-constexpr int kItems = 16;                    // 16-byte pieces (or bytes of a row's end) per thread
-constexpr int kBlockItems = 256 * kItems;
-
 struct StateArgs {
     const char *in;
     char *out;
     int64_t in_search, in_beam, out_search, out_beam;
     int64_t first;                // first block
     int64_t wide;                 // 16-byte pieces of a row
-    int32_t blocks;               // blocks per search: of the wide pieces, then one of the row's last bytes if there are any
+    int32_t blocks, wide_blocks;  // blocks per search: of the wide pieces, then of the row's last bytes if there are any
     int32_t tail;                 // these bytes
 };
 constexpr int kStates = 16;       // arrays to a launch
 struct ReorderArgs {
-    int32_t V, W, cols, n_states; // cols: pieces of a row per block, a power of two
+    int32_t V, W, n_states;
+    int32_t cols, tail_cols;      // pieces (bytes at the end) of a row per block, powers of two
     const int32_t *parent;
     StateArgs s[kStates];
 };
@@ -825,28 +823,30 @@ typedef unsigned piece __attribute__((ext_vector_type(4), aligned(1)));
 
 // Columns [c0, c0 + cols) of every row of a search, all read before the first is
 // written: out may be in.
-template <typename P>
+template <int ITEMS, typename P>
 __device__ __forceinline__ void reorder_columns(const ReorderArgs &A, const StateArgs &S, const int32_t *from, int64_t b,
                                                 int64_t c0, int cols, int64_t end) {
-    P v[kItems];
+    P v[ITEMS];
     const int shift = 31 - __clz(cols);
     const char *in = S.in + b * S.in_search;
     char *out = S.out + b * S.out_search;
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const int i = threadIdx.x + 256 * k, w = i >> shift;
         const int64_t c = c0 + (i & (cols - 1));
         if (w < A.W && c < end && from[w] >= 0) v[k] = *reinterpret_cast<const P *>(in + from[w] * S.in_beam + c * (int64_t)sizeof(P));
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
+    for (int k = 0; k < ITEMS; ++k) {
         const int i = threadIdx.x + 256 * k, w = i >> shift;
         const int64_t c = c0 + (i & (cols - 1));
         if (w < A.W && c < end && from[w] >= 0) *reinterpret_cast<P *>(out + w * S.out_beam + c * (int64_t)sizeof(P)) = v[k];
     }
 }
 
+// ITEMS: 16-byte pieces (or bytes of a row's end) per thread.
+template <int ITEMS>
 __global__ void __launch_bounds__(256) beam_reorder(ReorderArgs A) {
     __shared__ int32_t from[kMaxWidth];
     int64_t bid = blockIdx.x;
@@ -863,8 +863,10 @@ __global__ void __launch_bounds__(256) beam_reorder(ReorderArgs A) {
         from[threadIdx.x] = p < A.V ? p : -1;
     }
     __syncthreads();
-    if (S.tail && part == S.blocks - 1) reorder_columns<uint8_t>(A, S, from, b, S.wide * 16, 16, S.wide * 16 + S.tail);
-    else reorder_columns<piece>(A, S, from, b, (int64_t)part * A.cols, A.cols, S.wide);
+    if (part >= S.wide_blocks)
+        reorder_columns<ITEMS, uint8_t>(A, S, from, b, S.wide * 16 + (part - S.wide_blocks) * A.tail_cols, A.tail_cols,
+                                        S.wide * 16 + S.tail);
+    else reorder_columns<ITEMS, piece>(A, S, from, b, (int64_t)part * A.cols, A.cols, S.wide);
 }
 
 // ---------------------------------------------------------------------- host
@@ -1048,20 +1050,25 @@ extern "C" tag_status tag_beam_reorder(int32_t n_search, int32_t width_in, int32
             if (i != j && (out[i].meets(in[j]) || (j < i && out[i].meets(out[j]))))
                 TAG_FAIL(TAG_EINVAL, "out overlaps another array of states");
     }
-    // as many pieces of a row as leave room for every row
-    int cols = kBlockItems;
-    while (cols * width > kBlockItems) cols /= 2;
+    // As many pieces of a row to a block as leave room for every row: 4 to a thread, or 16 where that gives each CU
+    // several blocks all the same (longer runs).
+    int items = 16, cols = 0, tail_cols = 0;
     int64_t blocks[64], total = 0;
-    for (int32_t i = 0; i < n_states; ++i) {
-        blocks[i] = (states[i].row_bytes / 16 + cols - 1) / cols + (states[i].row_bytes % 16 ? 1 : 0);
-        if (blocks[i] < (1 << 24) / n + 1) total += n * blocks[i];
-        else total = 1 << 24;
-        if (total >= 1 << 24) TAG_FAIL(TAG_ESHAPE, "too many or too large rows");   // (a launch has fewer than 2^32 threads)
+    for (;; items = 4) {
+        for (cols = 256 * items; cols * width > 256 * items;) cols /= 2;
+        tail_cols = std::min(cols, 16);
+        total = 0;
+        for (int32_t i = 0; i < n_states; ++i) {
+            blocks[i] = (states[i].row_bytes / 16 + cols - 1) / cols + (states[i].row_bytes % 16 + tail_cols - 1) / tail_cols;
+            total += std::min<int64_t>(blocks[i], 1 << 24) * n;
+        }
+        if (items == 4 || total >= 1024) break;
     }
+    if (total >= 1 << 24) TAG_FAIL(TAG_ESHAPE, "too many or too large rows");   // (a launch has fewer than 2^32 threads)
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     for (int32_t i0 = 0; i0 < n_states; i0 += kStates) {
         ReorderArgs A{};
-        A.V = width_in; A.W = width; A.cols = cols; A.parent = parent;
+        A.V = width_in; A.W = width; A.cols = cols; A.tail_cols = tail_cols; A.parent = parent;
         int64_t first = 0;
         for (int32_t i = i0; i < std::min(n_states, i0 + kStates); ++i) {
             const tag_beam_state &s = states[i];
@@ -1071,10 +1078,13 @@ extern "C" tag_status tag_beam_reorder(int32_t n_search, int32_t width_in, int32
             K.in_search = n > 1 ? s.in_search : 0; K.in_beam = width_in > 1 ? s.in_beam : 0;
             K.out_search = n > 1 ? s.out_search : 0; K.out_beam = width > 1 ? s.out_beam : 0;
             K.wide = s.row_bytes / 16; K.tail = (int32_t)(s.row_bytes % 16);
+            K.wide_blocks = (int32_t)((K.wide + cols - 1) / cols);
             K.first = first; K.blocks = (int32_t)blocks[i];
             first += n * blocks[i];
         }
-        if (first > 0) beam_reorder<<<(unsigned)first, 256, 0, stream>>>(A);
+        if (first == 0) continue;
+        if (items == 16) beam_reorder<16><<<(unsigned)first, 256, 0, stream>>>(A);
+        else beam_reorder<4><<<(unsigned)first, 256, 0, stream>>>(A);
     }
     return launch_status("tag_beam_reorder");
 }

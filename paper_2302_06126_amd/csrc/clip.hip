@@ -21,6 +21,7 @@ namespace {
 constexpr int kChunkBytes = 16384, kVec = 16;   // bytes of a chunk, of a thread's access
 constexpr int kPieces = kChunkBytes / (256 * kVec);
 constexpr int kBlocks = 2048;                   // blocks of a launch, and sums in the workspace
+constexpr int kAhead = 4;                       // single elements in flight per thread
 constexpr int kWideRow = 1024;                  // from so many columns on a row is chunks of its own
 
 // elements of one array: n consecutive ones, or rows of `cols` (0: consecutive)
@@ -29,7 +30,10 @@ struct Chunk {
     char *out;
     int64_t gs, os;       // row strides in elements
     int32_t n, cols;
-    int32_t bf16, pad[5];
+    int32_t bf16;
+    uint32_t per_col;     // floor(2^32 / cols) + 1, for e / cols of e <= 8,192 and 1 < cols < 1,024 by one product
+    int32_t pad[4];
+    __device__ __forceinline__ int row(int e) const { return cols > 1 ? (int)__umulhi((unsigned)e, per_col) : e; }
 };
 static_assert(sizeof(Chunk) == 64, "an entry to a cache line's half");
 
@@ -42,30 +46,52 @@ struct ClipArgs {
     float *result;
 };
 
+typedef unsigned vec __attribute__((ext_vector_type(4)));
+typedef unsigned any_vec __attribute__((ext_vector_type(4), aligned(2)));   // 16 bytes at any element
+
 template <typename T>
-struct Wide;   // 16 bytes at any element
+struct Wide;   // elements of 16 bytes
 template <>
 struct Wide<float> {
-    typedef unsigned vec __attribute__((ext_vector_type(4), aligned(4)));
     static constexpr int N = 4;
     static __device__ __forceinline__ float get(const vec &r, int i) { return __uint_as_float(r[i]); }
-    static __device__ __forceinline__ void put(vec &r, int i, float v) { r[i] = __float_as_uint(v); }
+    static __device__ __forceinline__ vec put(const float (&v)[4]) {
+        return vec{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
     static __device__ __forceinline__ float get1(float v) { return v; }
     static __device__ __forceinline__ float put1(float v) { return v; }
 };
 template <>
 struct Wide<uint16_t> {
-    typedef unsigned vec __attribute__((ext_vector_type(4), aligned(2)));
     static constexpr int N = 8;
     static __device__ __forceinline__ float get(const vec &r, int i) {
         return __uint_as_float(i % 2 ? r[i / 2] & 0xffff0000u : r[i / 2] << 16);
     }
-    static __device__ __forceinline__ void put(vec &r, int i, float v) {
-        r[i / 2] = i % 2 ? (r[i / 2] & 0xffffu) | (unsigned)f2bf(v) << 16 : (r[i / 2] & 0xffff0000u) | f2bf(v);
+    static __device__ __forceinline__ vec put(const float (&v)[8]) {
+        return vec{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3]), pack_bf2(v[4], v[5]), pack_bf2(v[6], v[7])};
     }
     static __device__ __forceinline__ float get1(uint16_t v) { return bf2f(v); }
     static __device__ __forceinline__ uint16_t put1(float v) { return f2bf(v); }
 };
+
+// A thread's pieces of a chunk of consecutive elements, as far as they are whole (0
+// beyond); of either type, so that they can be on their way before anything else of
+// the chunk is looked at.
+struct Pieces {
+    vec v[kPieces];
+    __device__ __forceinline__ void load(const Chunk &C) {
+        const int bytes = C.cols ? 0 : C.bf16 ? 2 * C.n : 4 * C.n;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+            const int at = (threadIdx.x + 256 * k) * kVec;
+            v[k] = vec{0, 0, 0, 0};
+            if (at + kVec <= bytes) v[k] = *reinterpret_cast<const any_vec *>(C.g + at);
+        }
+    }
+};
+// the elements behind a chunk's whole pieces: first and number
+template <typename T>
+__device__ __forceinline__ int rest(const Chunk &C) { return C.n / Wide<T>::N * Wide<T>::N; }
 
 // sum of a value over the block's 256 threads, in a fixed order
 __device__ __forceinline__ double block_sum(double s) {
@@ -77,84 +103,108 @@ __device__ __forceinline__ double block_sum(double s) {
 }
 
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const Chunk &C) {
+__device__ __forceinline__ double chunk_squares(const Chunk &C, const Pieces &P) {
     using W = Wide<T>;
     const T *g = reinterpret_cast<const T *>(C.g);
     double s = 0.0;
     if (C.cols == 0) {
-        typename W::vec v[kPieces];
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            const int e = (threadIdx.x + 256 * k) * W::N;
-            v[k] = typename W::vec{0, 0, 0, 0};
-            if (e + W::N <= C.n) v[k] = *reinterpret_cast<const typename W::vec *>(g + e);
-            else
-                for (int i = 0; i < W::N; ++i)
-                    if (e + i < C.n) W::put(v[k], i, W::get1(g[e + i]));
-        }
 #pragma unroll
         for (int k = 0; k < kPieces; ++k)
 #pragma unroll
             for (int i = 0; i < W::N; ++i) {
-                const double x = W::get(v[k], i);
+                const double x = W::get(P.v[k], i);
                 s += x * x;
             }
-    } else {
-        for (int e = threadIdx.x; e < C.n; e += 256) {
-            const int r = e / C.cols;
-            const double x = W::get1(g[r * C.gs + (e - r * C.cols)]);
+        const int e = rest<T>(C) + threadIdx.x;
+        if (e < C.n) {
+            const double x = W::get1(g[e]);
             s += x * x;
+        }
+    } else {
+        for (int e0 = threadIdx.x; e0 < C.n; e0 += 256 * kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int e = e0 + 256 * k, r = C.row(e);
+                v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) s += (double)v[k] * (double)v[k];
         }
     }
     return s;
 }
 
-__global__ void __launch_bounds__(256) clip_norm(ClipArgs A) {
+// Reads bound it.  A chunk's pieces are on their way while the one before is summed,
+// its entry of the table one turn earlier.
+__global__ void __launch_bounds__(256, 6) clip_norm(ClipArgs A) {
     double s = 0.0;
-    for (int64_t c = blockIdx.x; c < A.chunks; c += gridDim.x) {
-        const Chunk C = A.table[c];
-        s += C.bf16 ? chunk_squares<uint16_t>(C) : chunk_squares<float>(C);
+    const int64_t step = gridDim.x;
+    int64_t c = blockIdx.x;   // (a block has one)
+    Chunk C = A.table[c], N = A.table[c + step < A.chunks ? c + step : c];
+    Pieces P;
+    P.load(C);
+    for (; c < A.chunks; c += step) {
+        const Chunk after = A.table[c + 2 * step < A.chunks ? c + 2 * step : c];
+        Pieces Q;
+        if (c + step < A.chunks) Q.load(N);
+        s += C.bf16 ? chunk_squares<uint16_t>(C, P) : chunk_squares<float>(C, P);
+        C = N;
+        N = after;
+        P = Q;
     }
     s = block_sum(s);
     if (threadIdx.x == 0) A.part[blockIdx.x] = s;
 }
 
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const Chunk &C, float scale) {
+__device__ __forceinline__ void chunk_scale(const Chunk &C, const Pieces &P, float scale) {
     using W = Wide<T>;
     const T *g = reinterpret_cast<const T *>(C.g);
     T *out = reinterpret_cast<T *>(C.out);
     const bool drop = scale == 0.f;   // (0 times an infinity is not 0)
+    auto scaled = [&](float x) { return drop ? 0.f : x * scale; };
     if (C.cols == 0) {
-        typename W::vec v[kPieces];
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
-            const int e = (threadIdx.x + 256 * k) * W::N;
-            if (e + W::N <= C.n) v[k] = *reinterpret_cast<const typename W::vec *>(g + e);
-        }
+            const int at = (threadIdx.x + 256 * k) * kVec;
+            float v[W::N];
 #pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-            const int e = (threadIdx.x + 256 * k) * W::N;
-            if (e + W::N <= C.n) {
-#pragma unroll
-                for (int i = 0; i < W::N; ++i) W::put(v[k], i, drop ? 0.f : W::get(v[k], i) * scale);
-                *reinterpret_cast<typename W::vec *>(out + e) = v[k];
-            } else {
-                for (int i = 0; i < W::N; ++i)
-                    if (e + i < C.n) out[e + i] = W::put1(drop ? 0.f : W::get1(g[e + i]) * scale);
-            }
+            for (int i = 0; i < W::N; ++i) v[i] = scaled(W::get(P.v[k], i));
+            if (at + kVec <= C.n * (int)sizeof(T)) __builtin_nontemporal_store((any_vec)W::put(v), reinterpret_cast<any_vec *>(C.out + at));
         }
+        const int e = rest<T>(C) + threadIdx.x;
+        if (e < C.n) out[e] = W::put1(scaled(W::get1(g[e])));
     } else {
-        for (int e = threadIdx.x; e < C.n; e += 256) {
-            const int r = e / C.cols, c = e - r * C.cols;
-            out[r * C.os + c] = W::put1(drop ? 0.f : W::get1(g[r * C.gs + c]) * scale);
+        for (int e0 = threadIdx.x; e0 < C.n; e0 += 256 * kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int e = e0 + 256 * k, r = C.row(e);
+                v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int e = e0 + 256 * k, r = C.row(e);
+                if (e < C.n) out[r * C.os + (e - r * C.cols)] = W::put1(scaled(v[k]));
+            }
         }
     }
 }
 
-// Every block forms the norm from the sums, in the same order.  The chunks go
-// backwards: the last ones that clip_norm has read are still in the caches.
-__global__ void __launch_bounds__(256) clip_apply(ClipArgs A) {
+// Every block forms the norm from the sums, in the same order, with its first chunk
+// on its way.  The chunks go backwards: the last ones that clip_norm has read are
+// still in the caches.
+__global__ void __launch_bounds__(256, 5) clip_apply(ClipArgs A) {
+    const int64_t step = gridDim.x;
+    int64_t c = A.writes ? A.chunks - 1 - blockIdx.x : -1;
+    Chunk C{}, N{};
+    Pieces P;
+    if (c >= 0) {
+        C = A.table[c];
+        N = A.table[c >= step ? c - step : c];
+        P.load(C);
+    }
     double p[kBlocks / 256], s = 0.0;
 #pragma unroll
     for (int i = 0; i < kBlocks / 256; ++i) {
@@ -170,12 +220,18 @@ __global__ void __launch_bounds__(256) clip_apply(ClipArgs A) {
         A.result[0] = rounded;
         A.result[1] = scale;
     }
-    if (A.writes == 0 || (A.writes == 2 && scale == 1.f)) return;
-    for (int64_t c = A.chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
-        const Chunk C = A.table[c];
-        if (!C.out || (scale == 1.f && C.out == C.g)) continue;
-        if (C.bf16) chunk_scale<uint16_t>(C, scale);
-        else chunk_scale<float>(C, scale);
+    if (A.writes == 2 && scale == 1.f) return;
+    for (; c >= 0; c -= step) {
+        const Chunk after = A.table[c >= 2 * step ? c - 2 * step : c];
+        Pieces Q;
+        if (c >= step) Q.load(N);
+        if (C.out && !(scale == 1.f && C.out == C.g)) {
+            if (C.bf16) chunk_scale<uint16_t>(C, P, scale);
+            else chunk_scale<float>(C, P, scale);
+        }
+        C = N;
+        N = after;
+        P = Q;
     }
 }
 
@@ -273,6 +329,7 @@ std::vector<Chunk> lay_out(const tag_clip_array *arrays, int32_t n, int64_t chun
             c.cols = (int32_t)a.cols;
             c.gs = a.g_stride;
             c.os = a.out_stride;
+            c.per_col = (uint32_t)((1ull << 32) / (uint64_t)a.cols + 1);
             for (int64_t r = 0; r < a.rows; r += rows) put(r, 0, std::min(rows, a.rows - r) * a.cols);
         }
     }
