@@ -181,7 +181,9 @@ class Mcts:
 class SearchService:
     """Device buffers for evaluating B leaves per round: packed states,
     expanded features, the GNN workspace, embeddings and priors.  A round is
-    select -> pack (host) -> features, forward, decide (GPU) -> update."""
+    select -> pack (host) -> features, forward, decide (GPU) -> update.
+    ``beam`` searches without a tree: the most probable strategies, level by
+    level."""
 
     def __init__(self, problem: SearchProblem, sp, model, B: int, device: str = "cuda"):
         import torch
@@ -248,13 +250,7 @@ class SearchService:
         with torch.cuda.stream(st):
             self.states_d.copy_(self.states_h, non_blocking=True)
             self.q_op.copy_(self.q_op_h, non_blocking=True)
-        lib = _abi.load()
-        check(lib.tag_search_features(self.problem.h, B, self.static.data_ptr(), self.states_d.data_ptr(),
-                                      self.x_op.data_ptr(), self.x_dev.data_ptr(), self.x_od.data_ptr(), sh),
-              "tag_search_features")
-        if self.own_dd:
-            check(lib.tag_search_link_features(self.problem.h, B, self.static.data_ptr(), self.states_d.data_ptr(),
-                                               self.x_dd_leaf.data_ptr(), sh), "tag_search_link_features")
+        self._features(sh)
         check(tag_gnn_forward(self.graph.handle, self.model.dims, self.model.weights, self.feats,
                               self.fwd_ws.data_ptr(), self.fwd_ws_bytes, self.E_op.data_ptr(),
                               self.E_dev.data_ptr(), sh), "tag_gnn_forward")
@@ -267,6 +263,16 @@ class SearchService:
             self.prior_h.copy_(self.prior, non_blocking=True)
         st.synchronize()
         return rewards, self.prior_h.numpy()
+
+    def _features(self, stream: int) -> None:
+        """The GNN's inputs from the packed states on the device."""
+        lib = _abi.load()
+        check(lib.tag_search_features(self.problem.h, self.B, self.static.data_ptr(), self.states_d.data_ptr(),
+                                      self.x_op.data_ptr(), self.x_dev.data_ptr(), self.x_od.data_ptr(), stream),
+              "tag_search_features")
+        if self.own_dd:
+            check(lib.tag_search_link_features(self.problem.h, self.B, self.static.data_ptr(), self.states_d.data_ptr(),
+                                               self.x_dd_leaf.data_ptr(), stream), "tag_search_link_features")
 
     def round(self, tree: Mcts, stream=None) -> np.ndarray:
         """One search round on `tree`; returns the leaves' rewards."""
@@ -311,6 +317,56 @@ class SearchService:
             return None
         return {"depth": rec["depth"].reshape(rounds, B), "path": rec["path"].reshape(rounds, B, L),
                 "reward": rec["reward"].reshape(rounds, B), "prior": rec["prior"].reshape(rounds, B, S)}
+
+    def beam(self, depth: Optional[int] = None, stream=None):
+        """Beam search with the service's B leaves (at most 256) as its beams: group by
+        group in the search order, the B most probable partial strategies under the
+        network's priors (each level's features come from the strategies so far).
+
+        Returns (paths [n, depth] int32, log_prior [n], rewards [n]), the most
+        probable first; fewer than B where there are no more strategies.  `depth`
+        stops the search after that many groups."""
+        from . import tag_gnn_forward, tag_gnn_scores
+        from .policy import Beam, Reorder
+        torch, B, S = self.torch, self.B, self.problem.n_slices
+        K = self.problem.n_groups
+        L = K if depth is None else int(depth)
+        if not 1 <= L <= K:
+            raise ValueError(f"depth must be in [1, {K}]")
+        st = torch.cuda.current_stream() if stream is None else stream
+        sh = int(st.cuda_stream)
+        with torch.cuda.stream(st):
+            level = Beam(1, B, S, device=self.dev)
+            paths = torch.zeros((B, K), dtype=torch.int32, device=self.dev)
+            scores = torch.empty((B, S), dtype=torch.float32, device=self.dev)
+            follow = Reorder([paths], 1, B)
+            total = level.start()
+        host = np.zeros((B, K), np.int32)
+        for d in range(L):
+            # (beams that are not there take the first slices: their rows do not matter)
+            _, qop = self.problem.pack(np.full(B, d, np.int32), host, self.states_h.data_ptr())
+            self.q_op_h.numpy()[:] = qop
+            with torch.cuda.stream(st):
+                self.states_d.copy_(self.states_h, non_blocking=True)
+                self.q_op.copy_(self.q_op_h, non_blocking=True)
+            self._features(sh)
+            check(tag_gnn_forward(self.graph.handle, self.model.dims, self.model.weights, self.feats,
+                                  self.fwd_ws.data_ptr(), self.fwd_ws_bytes, self.E_op.data_ptr(),
+                                  self.E_dev.data_ptr(), sh), "tag_gnn_forward")
+            check(tag_gnn_scores(self.graph.handle, self.model.dims, self.model.weights, B, self.E_op.data_ptr(),
+                                 self.E_dev.data_ptr(), self.slices, B, self.q_rep.data_ptr(), self.q_graph.data_ptr(),
+                                 self.q_op.data_ptr(), scores.data_ptr(), self.dec_ws.data_ptr(), self.dec_ws_bytes, sh),
+                  "tag_gnn_scores")
+            with torch.cuda.stream(st):
+                total, parent, choice = level(scores, total, stream=st)
+                follow(parent, stream=st)
+                paths[:, d].copy_(choice[0].clamp_min(0))
+                host = paths.cpu().numpy()   # (waits for the level)
+        with torch.cuda.stream(st):
+            log_prior, there = total[0].cpu().numpy(), parent[0].cpu().numpy() >= 0
+        n = int(there.sum())                 # (the beams that are not there come last)
+        rewards = np.array([self.problem.evaluate(host[b, :L])[0] for b in range(n)])
+        return host[:n, :L].copy(), log_prior[:n].copy(), rewards
 
     def close(self) -> None:
         self.graph.close()
