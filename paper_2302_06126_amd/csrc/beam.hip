@@ -21,7 +21,7 @@ struct BeamArgs {
     const uint8_t *done;
     float *total;
     int32_t *parent, *slice;
-    int32_t shift;                // 2^shift threads of a row, 16 columns each
+    int32_t shift, fours;         // 2^shift threads of a row, of each of which `fours` times four columns are used
     // rows in parts
     int32_t segs, group, groups;  // parts of a row; 2^group columns of a group, and groups of a row
     float *seg_max, *group_max;   // [rows][segs], [rows][groups]
@@ -405,19 +405,19 @@ __device__ __forceinline__ void load_four(const T *row, int c, int n, float (&v)
         for (int i = 0; i < 4; ++i) v[i] = c + i < n ? Quad<T>::get1(row[c + i]) : -INFINITY;
     }
 }
-// Column of the k-th four of thread j of a row's 2^shift: the lanes of a wavefront take
-// 256 (or four each) consecutive ones at a time, a wavefront 1,024.
+// Column of the k-th four of thread j of a row's 2^shift: the row's threads take four
+// each at a time, or (RUNS) each wavefront 1,024 consecutive ones, 256 at a time.
+template <bool RUNS>
 __device__ __forceinline__ int column(int j, int shift, int k) {
-    return shift < 6 ? 4 * (j + (k << shift)) : (j >> 6) * 1024 + k * 256 + (j & 63) * 4;
+    return RUNS && shift >= 6 ? (j >> 6) * 1024 + k * 256 + (j & 63) * 4 : 4 * (j + (k << shift));
 }
-
 // A thread's 16 columns of a row of n, or of its part from c0.
-template <typename T>
+template <bool RUNS, typename T>
 __device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift, int n, float (&x)[16]) {
     if (c0 + (16 << shift) <= n) {   // (one address, and no ends to look at)
         typedef typename Quad<T>::raw raw;
-        const T *p = row + c0 + column(j, shift, 0);
-        const int step = shift < 6 ? 4 << shift : 256;
+        const T *p = row + c0 + column<RUNS>(j, shift, 0);
+        const int step = RUNS && shift >= 6 ? 256 : 4 << shift;
         raw r[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) __builtin_memcpy(&r[k], p + step * k, sizeof(raw));
@@ -425,7 +425,7 @@ __device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift,
         for (int k = 0; k < 4; ++k) Quad<T>::get(r[k], *reinterpret_cast<float(*)[4]>(x + 4 * k));
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load_four(row, c0 + column(j, shift, k), n, *reinterpret_cast<float(*)[4]>(x + 4 * k));
+        for (int k = 0; k < 4; ++k) load_four(row, c0 + column<RUNS>(j, shift, k), n, *reinterpret_cast<float(*)[4]>(x + 4 * k));
     }
 }
 
@@ -482,20 +482,24 @@ __device__ __forceinline__ double exp_below(double x) {
     p = fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
-// sum of e^(x - m), m finite, in 64 bits
-__device__ __forceinline__ double own_sum(const float (&x)[16], float m) {
+// sum of e^(x - m), m finite, in 64 bits, over the first `fours` times four
+__device__ __forceinline__ double own_sum(const float (&x)[16], float m, int fours) {
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += exp_below((double)x[i] - (double)m);
+    for (int k = 0; k < 4; ++k) {
+        if (k >= fours) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += exp_below((double)x[4 * k + i] - (double)m);
+    }
     return s;
 }
 
 template <int NT, bool ALL>   // ALL: every wavefront of the row takes the results, else its first
-__device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const int shift, RowSum<NT> &part) {
+__device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const int shift, const int fours, RowSum<NT> &part) {
     const int in_wave = min(shift, 6);
     m = reduce_lanes(m, in_wave, Larger());
     double sum = 0.0;
-    if (m > -INFINITY && m < INFINITY) sum = own_sum(x, m);
+    if (m > -INFINITY && m < INFINITY) sum = own_sum(x, m, fours);
     sum = reduce_lanes(sum, in_wave, Plus());
     if constexpr (NT > 64) {
         if (shift > 6) {
@@ -539,7 +543,7 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
         total = A.total_in[b * A.V + v];
         done = A.done && A.done[b * A.V + v];
         const T *row = static_cast<const T *>(A.x) + (b * A.V + v) * A.xs;
-        load_row(row, 0, j, A.shift, A.S, x);
+        load_row<false>(row, 0, j, A.shift, A.S, x);
         if (j == 0) finished[v] = done;
     }
     const bool live = total - total == 0.f;
@@ -550,7 +554,7 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
     float four[4];
     const float own = own_max(x, four);
     float m = own;
-    const double sum = row_sum<NT, true>(x, m, A.shift, part);
+    const double sum = row_sum<NT, true>(x, m, A.shift, A.fours, part);
     // what is added to the scores; a finished beam is its first slice alone
     double off = 0.0;
     float top = own;
@@ -568,7 +572,7 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
     unsigned mask = 0;   // the first in bit 15
 #pragma unroll
     for (int i = 0; i < 16; ++i) mask = mask + mask + (x[i] >= least);
-    auto index = [&](int i) { return v * A.S + column(j, A.shift, i / 4) + i % 4; };
+    auto index = [&](int i) { return v * A.S + column<false>(j, A.shift, i / 4) + i % 4; };
     best.offer(__popc(mask), [&](auto put) {
         for (unsigned m = mask; m; m &= m - 1) {
             const int i = 16 - __ffs((int)m);
@@ -578,7 +582,7 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
     if (!best.offered()) {
         best.clear();
 #pragma unroll 1
-        for (int i = 0; i < 16; ++i) best.take(top > -INFINITY ? (double)pick(x, i) + off : -INFINITY, index(i));
+        for (int i = 0; i < 4 * A.fours; ++i) best.take(top > -INFINITY ? (double)pick(x, i) + off : -INFINITY, index(i));
     }
     write_beams(A, b, best, finished);
 }
@@ -601,7 +605,7 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
     if (row < rows) {   // (nothing waits for another load, though some beams' scores are not needed)
         t = A.total_in[row];
         done = A.done && A.done[row];
-        load_row(static_cast<const T *>(A.x) + row * A.xs, c0, j, shift, A.S, x);
+        load_row<true>(static_cast<const T *>(A.x) + row * A.xs, c0, j, shift, A.S, x);
     }
     const bool live = t - t == 0.f && !done;
     if (!live) {
@@ -614,20 +618,20 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
         float *g = A.group_max + row * A.groups;
         if (group == 10) {
             const float w = reduce_lanes(m, 6, Larger());
-            const int c = c0 + column(j, shift, 0);
+            const int c = c0 + column<true>(j, shift, 0);
             if ((j & 63) == 0 && c < A.S) g[c >> 10] = w;
         } else {
             const int wide = group - 2;   // 2^wide lanes to a group
-            const int c = c0 + column(j, shift, 0);
+            const int c = c0 + column<true>(j, shift, 0);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float w = reduce_lanes(four[k], wide, Larger());
-                const int ck = GROUP ? c + 256 * k : c0 + column(j, shift, k);
+                const int ck = GROUP ? c + 256 * k : c0 + column<true>(j, shift, k);
                 if ((j & ((1 << wide) - 1)) == 0 && ck < A.S) g[ck >> group] = w;
             }
         }
     }
-    const double sum = row_sum<256, false>(x, m, shift, part);
+    const double sum = row_sum<256, false>(x, m, shift, 4, part);
     if (live && j == 0) {
         A.seg_max[item] = m;
         A.seg_sum[item] = sum;
@@ -875,7 +879,7 @@ inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) =
 // The way that a level goes: one launch where each search's scores fit the registers
 // of a block, else rows in parts and a launch that joins them.
 struct Way {
-    int32_t shift, segs, group, groups;
+    int32_t shift, fours, segs, group, groups;
     bool whole;
     int64_t blocks;   // of the parts
 };
@@ -883,7 +887,15 @@ Way way(int32_t n, int32_t V, int32_t W, int32_t S) {
     Way w{};
     while (w.shift < 10 && 16 << w.shift < S) ++w.shift;
     w.whole = 16 << w.shift >= S && V << w.shift <= 1024;
-    if (w.whole) return w;
+    if (w.whole) {
+        // More threads to a row than its scores need: as a wavefront has them anyway, or so that the threads' best set a
+        // bar (317 searches of 37 x 12: 71 -> 9 us).
+        auto grow = [&] { return 4 << w.shift < S && V << (w.shift + 1) <= 1024 && (V << (w.shift + 1) <= 64 || V << w.shift < 2 * W); };
+        while (grow()) ++w.shift;
+        w.fours = std::min(4, (int32_t)((S + (4ll << w.shift) - 1) >> (w.shift + 2)));
+        return w;
+    }
+    w.fours = 4;
     w.shift = std::min(w.shift, 8);
     w.segs = (int32_t)((S + 4095ll) / 4096);
     // Groups: of their V S / 2^g maxima each is looked at twice, of about W of them all 2^g scores are read again, at
@@ -1000,7 +1012,7 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
     A.x = scores; A.xs = score_stride;
     A.total_in = total_in; A.done = done;
     A.total = total; A.parent = parent; A.slice = slice;
-    A.shift = w.shift; A.segs = w.segs; A.group = w.group; A.groups = w.groups;
+    A.shift = w.shift; A.fours = w.fours; A.segs = w.segs; A.group = w.group; A.groups = w.groups;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (dtype == TAG_BF16) launch_select<uint16_t>(A, w, n_search, stream);
     else launch_select<float>(A, w, n_search, stream);
