@@ -482,6 +482,28 @@ __device__ __forceinline__ double exp_below(double x) {
     p = fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
+// log x for x >= 1 (a sum with a term of 1 in it), within a few roundings of 64 bits: x =
+// 2^e m with m in [0.7, 1.42), log m = 2 atanh f for f = (m - 1) / (m + 1), |f| < 0.172, by
+// its series up to f^21 / 21.
+__device__ __forceinline__ double log_from(double x) {
+    int hi = __double2hiint(x), e = (hi >> 20) - 1023;
+    hi = (hi & 0xfffff) | 0x3ff00000;
+    if (hi >= 0x3ff6a09f) {   // (1.4142..)
+        hi -= 1 << 20;
+        ++e;
+    }
+    const double m = __hiloint2double(hi, __double2loint(x)), d = m - 1.0, b = m + 1.0;
+    double r = __builtin_amdgcn_rcp(b);
+    r = fma(r, fma(-b, r, 1.0), r);
+    r = fma(r, fma(-b, r, 1.0), r);
+    double f = d * r;
+    f = fma(r, fma(-b, f, d), f);
+    const double w = f * f;
+    double p = 1.0 / 21.0;
+#pragma unroll
+    for (int k = 19; k >= 3; k -= 2) p = fma(p, w, 1.0 / k);
+    return fma((double)e, 0.6931471805599453, fma(2.0 * f, w * p, 2.0 * f));
+}
 // sum of e^(x - m), m finite, in 64 bits, over the first `fours` times four
 __device__ __forceinline__ double own_sum(const float (&x)[16], float m, int fours) {
     double s = 0.0;
@@ -562,7 +584,7 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
         off = total;
         if (j == 0) x[0] = top = 0.f;
     } else if (m > -INFINITY && m < INFINITY) {
-        off = (double)total - ((double)m + log(sum));
+        off = (double)total - ((double)m + log_from(sum));
     } else {
         top = -INFINITY;
     }
@@ -696,7 +718,7 @@ __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
                 if (pm[i] > -INFINITY) s += ps[i] * exp_below((double)pm[i] - (double)m);
         s = reduce_lanes(s, share, Plus());
         if (v < A.V && i0 == 0) {
-            off[v] = some ? (double)t - ((double)m + log(s)) : fin && t - t == 0.f ? (double)t : -INFINITY;
+            off[v] = some ? (double)t - ((double)m + log_from(s)) : fin && t - t == 0.f ? (double)t : -INFINITY;
             done[v] = fin;
         }
     }
