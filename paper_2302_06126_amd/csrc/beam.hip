@@ -944,7 +944,9 @@ void launch_select(const BeamArgs &A, const Way &w, int32_t n, hipStream_t st) {
     if (w.whole) {
         const int threads = A.V << A.shift;
         const unsigned four = (unsigned)((n + 3) / 4);
-        if (threads <= 64) beam_whole<T, 64, 320><<<four, 256, 0, st>>>(A, n);
+        // (a wavefront ranks some 40 candidates by itself; one search of 1 x 256 slices, 64 beams after it: 14.4 us by one,
+        // 10.0 by four)
+        if (threads <= 64 && A.W <= 32) beam_whole<T, 64, 320><<<four, 256, 0, st>>>(A, n);
         else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A, n);
         else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A, n);
         return;

@@ -66,7 +66,9 @@ def test_sizes(torch, S, dtype):
         level.check(level.run(torch, W), W)
 
 
-@pytest.mark.parametrize("n,V,W,S", [(700, 4, 4, 60), (2000, 1, 2, 5), (300, 16, 16, 256), (17, 2, 256, 900)])
+@pytest.mark.parametrize("n,V,W,S", [(700, 4, 4, 60), (2000, 1, 2, 5), (300, 16, 16, 256), (17, 2, 256, 900),
+                                     (317, 37, 37, 12), (9, 5, 200, 100), (9, 4, 200, 60), (6, 10, 256, 100),
+                                     (70, 1, 33, 256), (70, 1, 64, 40), (1, 256, 256, 9000), (3, 200, 200, 4099)])
 def test_many_searches(torch, n, V, W, S):
     _say(f"[beam] n={n} V={V} W={W} S={S}")
     level = _Level(torch, n, n, V, S, done=0.1)
@@ -86,6 +88,32 @@ def test_equal_scores_go_by_beam_and_slice(torch, S, dtype):
         level.x[:, -1] = 1.0
         level.x[V // 2, :] = 1.0
         level.check(level.run(torch, W), W)
+
+
+@pytest.mark.parametrize("V,W,S", [(256, 256, 20000), (200, 200, 4099)])
+def test_equal_scores_of_long_rows(torch, V, W, S):
+    """More groups of columns at the bar than are listed."""
+    level = _Level(torch, S, 1, V, S, plain=True)
+    level.x.zero_()
+    level.t[:] = -1.5
+    level.check(level.run(torch, W), W)
+    level.t[:] = -np.linspace(1, 2, V).astype(np.float32)
+    level.check(level.run(torch, W), W)
+
+
+@pytest.mark.parametrize("V,W,S", [(200, 200, 4099), (256, 256, 17000), (64, 64, 70001), (64, 64, 256)])
+def test_one_beam_of_many(torch, V, W, S):
+    """The first level of a wide search, and one with the other beams finished."""
+    level = _Level(torch, S, 2, V, S)
+    keep = level.t[:, 3].copy()
+    level.t[:] = -np.inf
+    level.t[:, 3] = np.where(np.isfinite(keep), keep, -1.0)
+    level.check(level.run(torch, W), W)
+    level.t[0, :] = -np.arange(V, dtype=np.float32) - 40
+    level.t[0, 3] = -1.0
+    level.done[0, :] = True
+    level.done[0, 3] = False
+    level.check(level.run(torch, W), W)
 
 
 @pytest.mark.parametrize("S", [40, 3000, 40000])
