@@ -1,5 +1,19 @@
 // Beam search over the decision head's scores (include/tag_beam.h): one level's
 // selection, and the reordering of the beams' states.
+//
+// Selection.  Continuations of one beam are ordered by their scores alone; those of
+// two beams by the sums c = x + (total - log sum exp x), so that is what has to be
+// exact: rows are summed in 64 bits, which the vector unit does at the rate of
+// single fp32 operations, with exponentials of 18 instructions each.  They are half
+// of all instructions, and bound the large calls rather than memory (44 MB of fp32
+// scores would take 9 us, their exponentials 6 on all SIMDs).  Scores are read once.
+//
+// What is best is found without sorting.  Every thread (or group of columns) has a
+// best candidate of its own; W of these at least reach the bar that bisection finds
+// among them, so W candidates at least pass it, and hardly more: only those are
+// listed, and ranked by counting.  That holds for any input: a list that overflows
+// (equal scores, say) is cut back to its best W, in an order that ties do not leave
+// open, as often as it fills.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -161,8 +175,9 @@ struct Best {
         return __builtin_amdgcn_readfirstlane((int)r);
     }
     // Sets the bar from one candidate of each thread, the best that it has: as high
-    // as W threads, or a few more, still pass (false: fewer have one).  Bisection of the upper halves of the
-    // ordered keys between the block's ends.
+    // as W threads, or a few more, still pass (false: fewer have one).  Bisection of
+    // the upper halves of the ordered keys between the block's ends, about five turns
+    // of one barrier each.
     __device__ bool raise(double key) {
         const unsigned u = key > -INFINITY ? (unsigned)(ordered(key) >> 32) : 0u;
         unsigned hi = reduce_lanes(u, 6, Larger()), lo = reduce_lanes(u ? u : ~0u, 6, Smaller());
@@ -425,7 +440,8 @@ __device__ __forceinline__ void load_row(const T *row, int c0, int j, int shift,
         for (int k = 0; k < 4; ++k) Quad<T>::get(r[k], *reinterpret_cast<float(*)[4]>(x + 4 * k));
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load_four(row, c0 + column<RUNS>(j, shift, k), n, *reinterpret_cast<float(*)[4]>(x + 4 * k));
+        for (int k = 0; k < 4; ++k)
+            load_four(row, c0 + column<RUNS>(j, shift, k), n, *reinterpret_cast<float(*)[4]>(x + 4 * k));
     }
 }
 
@@ -517,7 +533,8 @@ __device__ __forceinline__ double own_sum(const float (&x)[16], float m, int fou
 }
 
 template <int NT, bool ALL>   // ALL: every wavefront of the row takes the results, else its first
-__device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const int shift, const int fours, RowSum<NT> &part) {
+__device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const int shift, const int fours,
+                                          RowSum<NT> &part) {
     const int in_wave = min(shift, 6);
     m = reduce_lanes(m, in_wave, Larger());
     double sum = 0.0;
@@ -544,7 +561,12 @@ __device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const 
 }
 
 // Searches whose scores fit one block's registers; those of one wavefront, four to a
-// block.
+// block.  One search of 64 x 256 9.0 us on its one CU: a chain of load 0.6, sums 3.3, bar
+// 1.6, list 1.4, ranks 1.2.  2,656 of 16 x 256 bf16 22.5 us: 6 us a thousand beyond the
+// first 5, vector issue and waits (9.8 million instructions of wavefronts, 3.1 of them
+// exponentials).  Measured and not kept there: 64 scores to a thread (6.3 million
+// instructions, but three wavefronts to a SIMD do not hide one another's waits: 24
+// us), 32 to a thread (21.6).
 constexpr int whole_block(int NT) { return NT > 64 ? NT : 256; }
 template <typename T, int NT, int CAP>
 __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_t n) {
@@ -611,7 +633,9 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
 
 // Rows in parts: a part's maximum and sum, and the maximum of every group of its
 // columns, from one reading of the scores.  GROUP: 0, or that of rows of a block each
-// (2^8 threads), whose reductions then are of fixed sizes.
+// (2^8 threads), whose reductions then are of fixed sizes (64 x 262,140 fp32 22.9 -> 21.1
+// us).  67 MB in 18 us, 3.7 TB/s: vector issue, some 470 instructions to a wavefront's
+// 1,024 scores, 290 of them exponentials.
 template <typename T, int GROUP>
 __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
     __shared__ RowSum<256> part;
@@ -661,7 +685,9 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
 }
 
 // One block per search: what each beam adds to its scores, from its parts; the bar
-// from the groups' maxima; then the candidates of the groups that reach it.
+// from the groups' maxima; then the candidates of the groups that reach it.  A chain
+// of waits on one CU: 8 searches of 8 x 262,140 13.7 us (offsets 3.2, groups 1.8, bar
+// 1.3, scores of about 11 groups 5, ranks 1), 5 of 200 x 4,099 26.5 (some 270 groups).
 constexpr int kListed = 2048;   // groups
 template <typename T>
 __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
@@ -860,18 +886,22 @@ __device__ __forceinline__ void reorder_columns(const ReorderArgs &A, const Stat
     for (int k = 0; k < ITEMS; ++k) {
         const int i = threadIdx.x + 256 * k, w = i >> shift;
         const int64_t c = c0 + (i & (cols - 1));
-        if (w < A.W && c < end && from[w] >= 0) v[k] = *reinterpret_cast<const P *>(in + from[w] * S.in_beam + c * (int64_t)sizeof(P));
+        if (w < A.W && c < end && from[w] >= 0)
+            v[k] = *reinterpret_cast<const P *>(in + from[w] * S.in_beam + c * (int64_t)sizeof(P));
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) {
         const int i = threadIdx.x + 256 * k, w = i >> shift;
         const int64_t c = c0 + (i & (cols - 1));
-        if (w < A.W && c < end && from[w] >= 0) *reinterpret_cast<P *>(out + w * S.out_beam + c * (int64_t)sizeof(P)) = v[k];
+        if (w < A.W && c < end && from[w] >= 0)
+            *reinterpret_cast<P *>(out + w * S.out_beam + c * (int64_t)sizeof(P)) = v[k];
     }
 }
 
-// ITEMS: 16-byte pieces (or bytes of a row's end) per thread.
+// ITEMS: 16-byte pieces (or bytes of a row's end) per thread.  Memory bounds it: 128
+// rows of 1.84 MB from one set of buffers to another 73 us, 360 MB at 4.9 TB/s; 64 rows
+// of 222 KB in place 7.4 us by 4 to a thread, 8.8 by 16 (215 blocks).
 template <int ITEMS>
 __global__ void __launch_bounds__(256) beam_reorder(ReorderArgs A) {
     __shared__ int32_t from[kMaxWidth];
@@ -912,8 +942,7 @@ Way way(int32_t n, int32_t V, int32_t W, int32_t S) {
     if (w.whole) {
         // More threads to a row than its scores need: as a wavefront has them anyway, or so that the threads' best set a
         // bar (317 searches of 37 x 12: 71 -> 9 us).
-        auto grow = [&] { return 4 << w.shift < S && V << (w.shift + 1) <= 1024 && (V << (w.shift + 1) <= 64 || V << w.shift < 2 * W); };
-        while (grow()) ++w.shift;
+        while (4 << w.shift < S && V << (w.shift + 1) <= 1024 && (V << (w.shift + 1) <= 64 || V << w.shift < 2 * W)) ++w.shift;
         w.fours = std::min(4, (int32_t)((S + (4ll << w.shift) - 1) >> (w.shift + 2)));
         return w;
     }
@@ -944,8 +973,8 @@ void launch_select(const BeamArgs &A, const Way &w, int32_t n, hipStream_t st) {
     if (w.whole) {
         const int threads = A.V << A.shift;
         const unsigned four = (unsigned)((n + 3) / 4);
-        // (a wavefront ranks some 40 candidates by itself; one search of 1 x 256 slices, 64 beams after it: 14.4 us by one,
-        // 10.0 by four)
+        // (a wavefront ranks some 40 candidates by itself; a search of 1 x 256 slices, 64 beams after it: 14.4 us by
+        // one, 10.0 by four)
         if (threads <= 64 && A.W <= 32) beam_whole<T, 64, 320><<<four, 256, 0, st>>>(A, n);
         else if (threads <= 256) beam_whole<T, 256, 512><<<n, 256, 0, st>>>(A, n);
         else beam_whole<T, 1024, 2048><<<n, 1024, 0, st>>>(A, n);
@@ -972,7 +1001,8 @@ tag_status check_select(int32_t n, int32_t V, int32_t W, int32_t S) {
     if (S < 1) TAG_FAIL(TAG_EINVAL, "need n_slices >= 1");
     if ((int64_t)V * S > (1 << 30)) TAG_FAIL(TAG_ESHAPE, "at most 2^30 continuations of a search");
     // (a launch has fewer than 2^32 threads)
-    if (n >= 1 << 22 || (n > 0 && way(n, V, W, S).blocks >= 1 << 24)) TAG_FAIL(TAG_ESHAPE, "too many scores for a launch");
+    if (n >= 1 << 22 || (n > 0 && way(n, V, W, S).blocks >= 1 << 24))
+        TAG_FAIL(TAG_ESHAPE, "too many scores for a launch");
     return TAG_OK;
 }
 
@@ -1017,7 +1047,8 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
         TAG_FAIL(TAG_EINVAL, "an array is not aligned to its elements");
     const int64_t rows = (int64_t)n_search * width_in;
     const size_t wide = (size_t)n_search * width * 4;
-    const Area in[3] = {flat_area(scores, ((rows - 1) * score_stride + n_slices) * el), flat_area(done, rows), flat_area(total_in, rows * 4)};
+    const Area in[3] = {flat_area(scores, ((rows - 1) * score_stride + n_slices) * el), flat_area(done, rows),
+                        flat_area(total_in, rows * 4)};
     const Area out[3] = {flat_area(parent, wide), flat_area(slice, wide), flat_area(total, wide)};
     for (int o = 0; o < 3; ++o) {
         for (int i = 0; i < 3; ++i)
@@ -1030,7 +1061,8 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
     const Way w = way(n_search, width_in, width, n_slices);
     const size_t need = carve(n_search, width_in, w, nullptr, &A);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_beam_workspace)");
-    if (need && (!workspace || !aligned(workspace, 16))) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
+    if (need && (!workspace || !aligned(workspace, 16)))
+        TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
     carve(n_search, width_in, w, workspace, &A);
     A.V = width_in; A.W = width; A.S = n_slices;
     A.x = scores; A.xs = score_stride;
@@ -1063,7 +1095,8 @@ extern "C" tag_status tag_beam_reorder(int32_t n_search, int32_t width_in, int32
         const int64_t most = (int64_t)1 << 46;   // (products below stay in 64 bits)
         if (s.row_bytes > most || s.in_beam > most || s.out_beam > most || s.in_search > most || s.out_search > most)
             TAG_FAIL(TAG_ESHAPE, "rows and strides of at most 2^46 bytes");
-        if (std::max(s.in_search, s.out_search) > ((int64_t)1 << 61) / n) TAG_FAIL(TAG_ESHAPE, "searches span at most 2^61 bytes");
+        if (std::max(s.in_search, s.out_search) > ((int64_t)1 << 61) / n)
+            TAG_FAIL(TAG_ESHAPE, "searches span at most 2^61 bytes");
         const int64_t span = (width - 1) * s.out_beam + s.row_bytes;
         if ((width > 1 && s.out_beam < s.row_bytes) || (n > 1 && s.out_search < span &&
             !(s.out_search >= s.row_bytes && (width == 1 || s.out_beam >= (n - 1) * s.out_search + s.row_bytes))))
