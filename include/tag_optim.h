@@ -131,7 +131,7 @@ tag_status tag_clip_prepare(const tag_clip_array *arrays, int32_t n_arrays, void
 /* Clips.  max_norm >= 0 (infinity: the norm alone, scale 1).  result: DEVICE [2],
  * norm and scale. */
 tag_status tag_clip_workspace(size_t *bytes);
-tag_status tag_clip(const tag_clip_plan *plan, float max_norm, float *result, void *workspace, size_t ws_bytes,
+tag_status tag_clip(const tag_clip_plan *plan, double max_norm, float *result, void *workspace, size_t ws_bytes,
                     void *hip_stream);
 
 #ifdef __cplusplus

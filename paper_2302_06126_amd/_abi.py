@@ -263,7 +263,7 @@ def load() -> C.CDLL:
     lib.tag_clip_table_bytes.argtypes = [C.POINTER(tag_clip_array), S, szp]
     lib.tag_clip_prepare.argtypes = [C.POINTER(tag_clip_array), S, vp, C.c_size_t, vp, C.POINTER(tag_clip_plan)]
     lib.tag_clip_workspace.argtypes = [szp]
-    lib.tag_clip.argtypes = [C.POINTER(tag_clip_plan), C.c_float, vp, vp, C.c_size_t, vp]
+    lib.tag_clip.argtypes = [C.POINTER(tag_clip_plan), C.c_double, vp, vp, C.c_size_t, vp]
     for name in TRAIN_EXPORTS:
         getattr(lib, name).restype = S
     lib.tag_gnn_decide_full_workspace.argtypes = [vp, C.POINTER(tag_model_dims), S, S, szp]

@@ -22,6 +22,7 @@ constexpr int kChunkBytes = 16384, kVec = 16;   // bytes of a chunk, of a thread
 constexpr int kPieces = kChunkBytes / (256 * kVec);
 constexpr int kBlocks = 2048;                   // blocks of a launch, and sums in the workspace
 constexpr int kAhead = 4;                       // single elements in flight per thread
+constexpr int kNarrow = 256 * kAhead;           // of narrow rows, a chunk is what a block has in flight at once
 constexpr int kWideRow = 1024;                  // from so many columns on a row is chunks of its own
 
 // elements of one array: n consecutive ones, or rows of `cols` (0: consecutive)
@@ -31,7 +32,7 @@ struct Chunk {
     int64_t gs, os;       // row strides in elements
     int32_t n, cols;
     int32_t bf16;
-    uint32_t per_col;     // floor(2^32 / cols) + 1, for e / cols of e <= 8,192 and 1 < cols < 1,024 by one product
+    uint32_t per_col;     // floor(2^32 / cols) + 1, for e / cols of e <= 1,024 and 1 < cols < 1,024 by one product
     int32_t pad[4];
     __device__ __forceinline__ int row(int e) const { return cols > 1 ? (int)__umulhi((unsigned)e, per_col) : e; }
 };
@@ -42,7 +43,7 @@ struct ClipArgs {
     int64_t chunks;
     int32_t sums, writes;
     double *part;
-    float max_norm;
+    double max_norm;
     float *result;
 };
 
@@ -121,16 +122,14 @@ __device__ __forceinline__ double chunk_squares(const Chunk &C, const Pieces &P)
             s += x * x;
         }
     } else {
-        for (int e0 = threadIdx.x; e0 < C.n; e0 += 256 * kAhead) {
-            float v[kAhead];
+        float v[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int e = e0 + 256 * k, r = C.row(e);
-                v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
-            }
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) s += (double)v[k] * (double)v[k];
+        for (int k = 0; k < kAhead; ++k) {
+            const int e = threadIdx.x + 256 * k, r = C.row(e);
+            v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
         }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) s += (double)v[k] * (double)v[k];
     }
     return s;
 }
@@ -138,7 +137,8 @@ __device__ __forceinline__ double chunk_squares(const Chunk &C, const Pieces &P)
 // Reads bound it: 435 MB in 97 us, 4.5 TB/s (70 where the last call's results went past
 // the caches and left a part of them there).  A chunk's pieces are on their way
 // while the one before is summed, its entry of the table one turn earlier (114 us
-// without).  1,200 tensors of 27 MB 10.2 us: two round trips to a block.
+// without).  1,200 tensors of 27 MB 7.6 us: two round trips to a block (10.2 with narrow
+// rows in chunks of 16 KiB, several turns of single elements each).
 __global__ void __launch_bounds__(256, 6) clip_norm(ClipArgs A) {
     double s = 0.0;
     const int64_t step = gridDim.x;
@@ -178,18 +178,16 @@ __device__ __forceinline__ void chunk_scale(const Chunk &C, const Pieces &P, flo
         const int e = rest<T>(C) + threadIdx.x;
         if (e < C.n) out[e] = W::put1(scaled(W::get1(g[e])));
     } else {
-        for (int e0 = threadIdx.x; e0 < C.n; e0 += 256 * kAhead) {
-            float v[kAhead];
+        float v[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int e = e0 + 256 * k, r = C.row(e);
-                v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
-            }
+        for (int k = 0; k < kAhead; ++k) {
+            const int e = threadIdx.x + 256 * k, r = C.row(e);
+            v[k] = e < C.n ? W::get1(g[r * C.gs + (e - r * C.cols)]) : 0.f;
+        }
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                const int e = e0 + 256 * k, r = C.row(e);
-                if (e < C.n) out[r * C.os + (e - r * C.cols)] = W::put1(scaled(v[k]));
-            }
+        for (int k = 0; k < kAhead; ++k) {
+            const int e = threadIdx.x + 256 * k, r = C.row(e);
+            if (e < C.n) out[r * C.os + (e - r * C.cols)] = W::put1(scaled(v[k]));
         }
     }
 }
@@ -218,7 +216,7 @@ __global__ void __launch_bounds__(256, 5) clip_apply(ClipArgs A) {
     for (int i = 0; i < kBlocks / 256; ++i) s += p[i];
     const double norm = sqrt(block_sum(s));
     const float rounded = (float)norm;
-    const float scale = !(rounded < INFINITY) ? 0.f : norm > (double)A.max_norm ? (float)((double)A.max_norm / norm) : 1.f;
+    const float scale = !(rounded < INFINITY) ? 0.f : norm > A.max_norm ? (float)(A.max_norm / norm) : 1.f;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         A.result[0] = rounded;
         A.result[1] = scale;
@@ -253,7 +251,7 @@ int64_t chunks_of(const tag_clip_array &a) {
     const int64_t per = chunk_elements(a);
     if (is_flat(a)) return (a.rows * a.cols + per - 1) / per;
     if (is_wide(a)) return a.rows * ((a.cols + per - 1) / per);
-    const int64_t rows = per / a.cols;
+    const int64_t rows = kNarrow / a.cols;
     return (a.rows + rows - 1) / rows;
 }
 
@@ -328,7 +326,7 @@ std::vector<Chunk> lay_out(const tag_clip_array *arrays, int32_t n, int64_t chun
             for (int64_t r = 0; r < a.rows; ++r)
                 for (int64_t e = 0; e < a.cols; e += per) put(r, e, std::min(per, a.cols - e));
         } else {
-            const int64_t rows = per / a.cols;
+            const int64_t rows = kNarrow / a.cols;
             c.cols = (int32_t)a.cols;
             c.gs = a.g_stride;
             c.os = a.out_stride;
@@ -390,13 +388,13 @@ extern "C" tag_status tag_clip_workspace(size_t *bytes) {
     return TAG_OK;
 }
 
-extern "C" tag_status tag_clip(const tag_clip_plan *plan, float max_norm, float *result, void *workspace,
+extern "C" tag_status tag_clip(const tag_clip_plan *plan, double max_norm, float *result, void *workspace,
                                size_t ws_bytes, void *hip_stream) {
     clear_error();
     if (!plan || !result) TAG_FAIL(TAG_EINVAL, "plan and result must be non-NULL");
     if (plan->chunks < 0 || plan->chunks > kMaxChunks || (plan->chunks && !plan->table) || plan->writes < 0 || plan->writes > 2)
         TAG_FAIL(TAG_EINVAL, "plan is not one of tag_clip_prepare");
-    if (!(max_norm >= 0.f)) TAG_FAIL(TAG_EINVAL, "max_norm must be >= 0");
+    if (!(max_norm >= 0.0)) TAG_FAIL(TAG_EINVAL, "max_norm must be >= 0");
     if ((uintptr_t)result % 4) TAG_FAIL(TAG_EINVAL, "result is not aligned to its elements");
     if (ws_bytes < kBlocks * sizeof(double)) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_clip_workspace)");
     if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");

@@ -36,7 +36,6 @@ def _check(torch, call, before, outs, limit, untouched=()):
     n = sum(t.numel() for t in before)
     want = _norm(before)
     _near(norm, want, n)
-    limit = float(np.float32(limit))
     if want > limit:
         _near(scale, limit / want, n)
     else:
