@@ -28,7 +28,7 @@ extern "C" {
  * candidate c = total_v, which counts as slice 0 where ties are broken.  The
  * `width` best candidates of all beams of a search, best first, equal ones in
  * the order of (beam, slice), become its new beams:
- *   total   c, rounded to fp32          parent  v
+ *   total   c, rounded to fp32 (below its range: -inf)     parent  v
  *   slice   a, or -1 of a finished beam
  * A beam has no candidates if its total is not finite, or if a NaN or +inf
  * stands among its scores (which a finished beam may have); what is left

@@ -200,7 +200,7 @@ struct Best {
         }
         if (live < W) return false;
         const unsigned best = hi;
-        const int most = W + max(W / 2, 8);
+        const int most = W + max(W / 4, 2);
         while (lo < hi) {   // W reach lo, fewer reach hi + 1; three probes between them to a turn
             const unsigned step = (hi - lo) / 4, t1 = lo + step + 1, t2 = t1 + step, t3 = min(t2 + step, hi);
             // (fewer than 1,024 each: some thread is at lo or below)
