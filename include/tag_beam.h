@@ -41,7 +41,8 @@ extern "C" {
  *   done      [n_search][width_in], or NULL: none is finished
  *   total     [n_search][width] fp32; may be total_in where width_in = width
  *   parent, slice  [n_search][width] int32
- * width and width_in are at most 256, width_in * S at most 2^30 (TAG_ESHAPE).
+ * width and width_in are at most 256, width_in * S at most 2^30, n_search *
+ * width_in * stride at most 2^58 (TAG_ESHAPE).
  * A call is bitwise repeatable.
  */
 tag_status tag_beam_workspace(int32_t n_search, int32_t width_in, int32_t width, int32_t n_slices, size_t *bytes);

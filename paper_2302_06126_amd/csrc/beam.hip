@@ -1046,6 +1046,8 @@ extern "C" tag_status tag_beam_select(int32_t n_search, int32_t width_in, int32_
     if (!aligned(scores, el) || !aligned(total_in, 4) || !aligned(total, 4) || !aligned(parent, 4) || !aligned(slice, 4))
         TAG_FAIL(TAG_EINVAL, "an array is not aligned to its elements");
     const int64_t rows = (int64_t)n_search * width_in;
+    if (rows > 1 && score_stride > ((int64_t)1 << 58) / rows)   // (products below, and the kernels', stay in 64 bits)
+        TAG_FAIL(TAG_ESHAPE, "scores span at most 2^58 elements");
     const size_t wide = (size_t)n_search * width * 4;
     const Area in[3] = {flat_area(scores, ((rows - 1) * score_stride + n_slices) * el), flat_area(done, rows),
                         flat_area(total_in, rows * 4)};
