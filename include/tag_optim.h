@@ -80,14 +80,21 @@ typedef struct tag_muon_group {
 typedef struct tag_muon_options {
     float lr, momentum, weight_decay;   /* lr >= 0, momentum in [0, 1), weight_decay >= 0 */
     int32_t nesterov;
-    const float *clip;             /* NULL, or DEVICE {norm, scale} as tag_clip writes them for these gradients: the   */
-                                   /* step takes scale g for g (one more rounding of fp32); with a norm that is not    */
-                                   /* finite it leaves weights and momentum as they are                                */
 } tag_muon_options;
 
 tag_status tag_muon_workspace(const tag_muon_group *groups, int32_t n_groups, size_t *bytes);
 tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
                          const tag_muon_options *options, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * The step from clipped gradients, which stay as they are.  clip: DEVICE
+ * {norm, scale} as tag_clip writes them for these gradients.  The step takes
+ * scale g for g (one more rounding of fp32); with a norm that is not finite it
+ * leaves weights and momentum as they are.
+ */
+tag_status tag_muon_step_clipped(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
+                                 const tag_muon_options *options, const float *clip, void *workspace,
+                                 size_t ws_bytes, void *hip_stream);
 
 /*
  * Clipping by the global norm, over all elements of all arrays of a plan:

@@ -43,7 +43,7 @@ EXPORTS += ("tag_beam_workspace", "tag_beam_select", "tag_beam_reorder")
 TRAIN_EXPORTS = ("tag_train_workspace", "tag_train_step", "tag_train_balance_workspace", "tag_train_step_balanced",
                  # include/tag_optim.h
                  "tag_orthogonalise_workspace", "tag_orthogonalise", "tag_muon_workspace", "tag_muon_step",
-                 "tag_clip_table_bytes", "tag_clip_prepare", "tag_clip_workspace", "tag_clip")
+                 "tag_muon_step_clipped", "tag_clip_table_bytes", "tag_clip_prepare", "tag_clip_workspace", "tag_clip")
 
 # kernel stages (include/tag_profile.h)
 STAGE_NAMES = ("graph_build", "encode", "transform", "agg_op_op", "agg_op_dev", "agg_dev_op", "agg_dev_merge",
@@ -133,8 +133,7 @@ class tag_muon_group(C.Structure):
 
 
 class tag_muon_options(C.Structure):
-    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32),
-                ("clip", C.c_void_p)]
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("nesterov", C.c_int32)]
 
 
 class tag_clip_array(C.Structure):
@@ -260,6 +259,8 @@ def load() -> C.CDLL:
     lib.tag_muon_workspace.argtypes = [C.POINTER(tag_muon_group), S, szp]
     lib.tag_muon_step.argtypes = [C.POINTER(tag_muon_group), S, C.POINTER(tag_newton_schulz),
                                   C.POINTER(tag_muon_options), vp, C.c_size_t, vp]
+    lib.tag_muon_step_clipped.argtypes = [C.POINTER(tag_muon_group), S, C.POINTER(tag_newton_schulz),
+                                          C.POINTER(tag_muon_options), vp, vp, C.c_size_t, vp]
     lib.tag_clip_table_bytes.argtypes = [C.POINTER(tag_clip_array), S, szp]
     lib.tag_clip_prepare.argtypes = [C.POINTER(tag_clip_array), S, vp, C.c_size_t, vp, C.POINTER(tag_clip_plan)]
     lib.tag_clip_workspace.argtypes = [szp]

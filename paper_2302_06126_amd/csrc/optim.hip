@@ -1009,6 +1009,7 @@ tag_status check_ns(const tag_newton_schulz *ns) {
 struct Options {
     tag_newton_schulz ns;
     tag_muon_options muon;
+    const float *clip;   // (of the clipped step)
 };
 
 // block numbers of a kernel's groups: n of them, the rest past the grid
@@ -1050,7 +1051,7 @@ template <typename T, bool MUON>
 void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, const Options &o, hipStream_t st) {
     NormSet N{};
     N.lr = o.muon.lr; N.momentum = o.muon.momentum; N.decay = o.muon.weight_decay; N.nesterov = o.muon.nesterov != 0;
-    N.clip = o.muon.clip;
+    N.clip = o.clip;
     // matrices of at most 64 x 256 alone: one launch for all of them
     int32_t wide = 0;
     for (int i = 0; i < n; ++i) wide = std::max(wide, mats[i].np > 64 ? INT32_MAX : mats[i].mp);
@@ -1090,7 +1091,7 @@ void run_set(const Group *mats, int32_t n, const Group *plain, int32_t n_plain, 
     PrepSet P{};
     P.eps = o.ns.eps; P.momentum = N.momentum; P.nesterov = N.nesterov; P.clip = N.clip;
     EndSet E{};
-    E.a = o.ns.a; E.b = o.ns.b; E.c = o.ns.c; E.lr = o.muon.lr; E.decay = o.muon.weight_decay; E.clip = o.muon.clip;
+    E.a = o.ns.a; E.b = o.ns.b; E.c = o.ns.c; E.lr = o.muon.lr; E.decay = o.muon.weight_decay; E.clip = o.clip;
     for (int i = 0; i < n; ++i) {
         const Group &G = mats[i];
         PrepGroup &K = P.g[i];
@@ -1230,7 +1231,7 @@ extern "C" tag_status tag_orthogonalise(const tag_ortho_group *groups, int32_t n
         TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_orthogonalise_workspace)");
     if (!workspace || (uintptr_t)workspace % 16) TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const Options o{*ns, {}};
+    const Options o{*ns, {}, nullptr};
     if (dtype == TAG_BF16) run_groups<uint16_t, false>(groups, n_groups, o, workspace, stream);
     else run_groups<float, false>(groups, n_groups, o, workspace, stream);
     return launch_status("tag_orthogonalise");
@@ -1245,10 +1246,12 @@ extern "C" tag_status tag_muon_workspace(const tag_muon_group *groups, int32_t n
     return TAG_OK;
 }
 
-extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
-                                    const tag_muon_options *options, void *workspace, size_t ws_bytes,
-                                    void *hip_stream) {
-    clear_error();
+namespace {
+
+// clip: NULL without
+tag_status muon_step(const char *name, const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
+                     const tag_muon_options *options, const float *clip, void *workspace, size_t ws_bytes,
+                     void *hip_stream) {
     tag_status st = check_muon_groups(groups, n_groups, true);
     if (st == TAG_OK) st = check_ns(ns);
     if (st != TAG_OK) return st;
@@ -1257,11 +1260,28 @@ extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_grou
     if (!(options->momentum >= 0.f && options->momentum < 1.f)) TAG_FAIL(TAG_EINVAL, "momentum must be in [0, 1)");
     if (!(options->weight_decay >= 0.f) || !std::isfinite(options->weight_decay))
         TAG_FAIL(TAG_EINVAL, "weight_decay must be finite and >= 0");
-    if ((uintptr_t)options->clip % 4) TAG_FAIL(TAG_EINVAL, "clip must be aligned to its elements");
     const size_t need = workspace_of(groups, n_groups);
     if (need > ws_bytes) TAG_FAIL(TAG_ENOSPACE, "workspace too small (see tag_muon_workspace)");
     if (need && (!workspace || (uintptr_t)workspace % 16))
         TAG_FAIL(TAG_EINVAL, "workspace must be non-NULL and 16-byte aligned");
-    run_groups<float, true>(groups, n_groups, Options{*ns, *options}, workspace, static_cast<hipStream_t>(hip_stream));
-    return launch_status("tag_muon_step");
+    run_groups<float, true>(groups, n_groups, Options{*ns, *options, clip}, workspace,
+                            static_cast<hipStream_t>(hip_stream));
+    return launch_status(name);
+}
+
+}  // namespace
+
+extern "C" tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
+                                    const tag_muon_options *options, void *workspace, size_t ws_bytes,
+                                    void *hip_stream) {
+    clear_error();
+    return muon_step("tag_muon_step", groups, n_groups, ns, options, nullptr, workspace, ws_bytes, hip_stream);
+}
+
+extern "C" tag_status tag_muon_step_clipped(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
+                                            const tag_muon_options *options, const float *clip, void *workspace,
+                                            size_t ws_bytes, void *hip_stream) {
+    clear_error();
+    if (!clip || (uintptr_t)clip % 4) TAG_FAIL(TAG_EINVAL, "clip must be non-NULL and aligned to its elements");
+    return muon_step("tag_muon_step_clipped", groups, n_groups, ns, options, clip, workspace, ws_bytes, hip_stream);
 }

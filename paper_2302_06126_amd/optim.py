@@ -228,7 +228,6 @@ class Muon:
         if max_norm is not None:
             self.clip = Clip([g for _, g in self.params], max_norm, out=False)
             self.norm = self.clip.norm
-            self.options.clip = _ptr(self.clip.result)
 
     @classmethod
     def of(cls, trainer, **kw):
@@ -248,9 +247,11 @@ class Muon:
         if lr is not None:
             self.options.lr = float(lr)
         try:
+            name, clip = "tag_muon_step", ()
             if self.clip is not None:
                 self.clip(stream=stream)
-            _launch(self.device, "tag_muon_step", self._g, len(self.params), C.byref(self._ns), C.byref(self.options),
+                name, clip = "tag_muon_step_clipped", (_ptr(self.clip.result),)
+            _launch(self.device, name, self._g, len(self.params), C.byref(self._ns), C.byref(self.options), *clip,
                     _ptr(self.ws), self.ws_bytes, _raw_stream(stream, self.device))
         except TagError:   # (a rate that was refused is not kept)
             self.options.lr = was
