@@ -88,9 +88,9 @@ tag_status tag_muon_step(const tag_muon_group *groups, int32_t n_groups, const t
 
 /*
  * The step from clipped gradients, which stay as they are.  clip: DEVICE
- * {norm, scale} as tag_clip writes them for these gradients.  The step takes
- * scale g for g (one more rounding of fp32); with a norm that is not finite it
- * leaves weights and momentum as they are.
+ * {norm, scale} as tag_clip writes them for these gradients, no part of a w or
+ * m.  The step takes scale g for g (one more rounding of fp32); with a norm that
+ * is not finite it leaves weights and momentum as they are.
  */
 tag_status tag_muon_step_clipped(const tag_muon_group *groups, int32_t n_groups, const tag_newton_schulz *ns,
                                  const tag_muon_options *options, const float *clip, void *workspace,

@@ -1205,6 +1205,21 @@ tag_status check_muon_groups(const tag_muon_group *g, int32_t n, bool arrays) {
     return TAG_OK;
 }
 
+// whether the eight bytes at p share one with an element of the array
+bool holds(const tag_matrices &a, int32_t count, int32_t rows, int32_t cols, const float *p) {
+    const int64_t row = rows > 1 ? a.row_stride : 0, mat = count > 1 ? a.matrix_stride : 0;
+    for (int k = 0; k < 2; ++k) {
+        if ((uintptr_t)(p + k) < (uintptr_t)a.base) continue;
+        const int64_t d = (int64_t)(((uintptr_t)(p + k) - (uintptr_t)a.base) / 4);
+        if (d >= (count - 1) * mat + (rows - 1) * row + cols) continue;
+        for (int64_t i = 0; i < count && d >= i * mat; ++i) {   // d = i mat + j row + k with j < rows, k < cols
+            const int64_t r = d - i * mat, j = row > 0 ? std::min<int64_t>(r / row, rows - 1) : 0;
+            if (r - j * row < cols) return true;
+        }
+    }
+    return false;
+}
+
 }  // namespace
 }  // namespace tag
 
@@ -1255,6 +1270,12 @@ tag_status muon_step(const char *name, const tag_muon_group *groups, int32_t n_g
     tag_status st = check_muon_groups(groups, n_groups, true);
     if (st == TAG_OK) st = check_ns(ns);
     if (st != TAG_OK) return st;
+    // (every launch of the step looks at them)
+    for (int32_t i = 0; clip && i < n_groups; ++i) {
+        const tag_muon_group &g = groups[i];
+        if (holds(g.w, g.count, g.rows, g.cols, clip) || holds(g.m, g.count, g.rows, g.cols, clip))
+            TAG_FAIL(TAG_EINVAL, "clip must not be part of a w or m");
+    }
     if (!options) TAG_FAIL(TAG_EINVAL, "options must be non-NULL");
     if (!(options->lr >= 0.f) || !std::isfinite(options->lr)) TAG_FAIL(TAG_EINVAL, "lr must be finite and >= 0");
     if (!(options->momentum >= 0.f && options->momentum < 1.f)) TAG_FAIL(TAG_EINVAL, "momentum must be in [0, 1)");

@@ -40,10 +40,30 @@ def _clipped(abi, clip=CLIP, options=True, ws=1 << 28, nb=16, **kw):
     return abi.load().tag_muon_step_clipped(g, 1, C.byref(ns), C.byref(o) if options else None, clip, ws, nb, None)
 
 
+WIDE = dict(count=3, rows=70, cols=90, row=100, mat=7000)
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(), ENOSPACE), (dict(clip=None), EINVAL), (dict(clip=CLIP + 2), EINVAL), (dict(options=False), EINVAL),
-    (dict(clip=G), ENOSPACE),
+    # among weights or momentum, which the step writes while it looks at them; beside them; among the gradients
+    (dict(clip=W), EINVAL), (dict(clip=M), EINVAL), (dict(clip=W + 4 * (70 * 90 - 1)), EINVAL), (dict(clip=M - 4), EINVAL),
+    (dict(clip=W - 8), ENOSPACE), (dict(clip=W + 4 * 70 * 90), ENOSPACE), (dict(clip=G), ENOSPACE),
+    # and between their rows and matrices
+    (dict(clip=W + 4 * 92, **WIDE), ENOSPACE), (dict(clip=W + 4 * 89, **WIDE), EINVAL),
+    (dict(clip=W + 4 * 99, **WIDE), EINVAL), (dict(clip=W + 4 * (7000 + 6 * 100 + 90), **WIDE), ENOSPACE),
+    (dict(clip=M + 4 * (14000 + 69 * 100 + 89), **WIDE), EINVAL), (dict(clip=M + 4 * (14000 + 69 * 100 + 90), **WIDE), ENOSPACE),
 ])
 def test_clipped_step_refuses(abi, kw, status):
     assert _clipped(abi, **kw) == status
     assert abi.load().tag_last_error()
+
+
+def test_clip_in_another_group(abi):
+    g, ns = _group(abi)
+    two = (abi.tag_muon_group * 2)(g[0], g[0])
+    two[1].w.base, two[1].m.base = CLIP - 4 * 90, 1 << 27
+    two[1].plain = 1
+    o = abi.tag_muon_options(0.1, 0.9, 0.0, 1)
+    step = abi.load().tag_muon_step_clipped
+    assert step(two, 2, C.byref(ns), C.byref(o), CLIP, 1 << 28, 16, None) == EINVAL
+    assert step(two, 2, C.byref(ns), C.byref(o), 1 << 30, 1 << 28, 16, None) == ENOSPACE
