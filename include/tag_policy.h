@@ -7,10 +7,11 @@
  * Rows are queries, columns the S slices of a table.  Conventions follow
  * tag.h: caller-owned DEVICE buffers, asynchronous on hip_stream, arguments
  * validated before anything is enqueued, no allocation.  Row strides are in
- * elements and at least S; rows may start at any element.  A workspace is
- * scratch for the duration of a call (calls that share one must be ordered);
- * nothing in it needs to start at zero.  But where a call says so, no array that
- * it writes overlaps another of its arrays.
+ * elements and at least S; rows may start at any element, and span at most 2^58
+ * (number of rows times stride, TAG_ESHAPE).  A workspace is scratch for the
+ * duration of a call (calls that share one must be ordered); nothing in it needs
+ * to start at zero.  But where a call says so, no array that it writes overlaps
+ * another of its arrays.
  */
 #ifndef TAG_POLICY_H
 #define TAG_POLICY_H

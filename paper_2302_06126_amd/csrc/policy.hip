@@ -230,6 +230,9 @@ struct Span {
     bool meets(const Span &o) const { return b < e && o.b < o.e && b < o.e && o.b < e; }
 };
 
+// rows so far apart that products of these numbers (and of an element's bytes) may leave 64 bits
+inline bool far_apart(int64_t rows, int64_t stride) { return rows > 1 && stride > ((int64_t)1 << 58) / rows; }
+
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 tag_status check_rows(int32_t Q, int32_t S, int32_t dtype) {
@@ -273,6 +276,10 @@ extern "C" tag_status tag_constrain(int32_t n_query, int32_t n_slices, int32_t d
     if (c.n_history > (1 << 30)) TAG_FAIL(TAG_ESHAPE, "at most 2^30 history entries");
     if (c.history && c.history_stride != 0 && c.history_stride < c.n_history)
         TAG_FAIL(TAG_EINVAL, "history_stride must be 0 or cover a row");
+    if (far_apart(n_query, score_stride) || (constrained && far_apart(n_query, constrained_stride)) ||
+        (prior && far_apart(n_query, prior_stride)) || (c.allow && far_apart(n_query, c.allow_stride)) ||
+        (c.bias && far_apart(n_query, c.bias_stride)) || (c.n_history > 0 && far_apart(n_query, c.history_stride)))
+        TAG_FAIL(TAG_ESHAPE, "rows span at most 2^58 elements");
     if (!aligned(scores, el) || !aligned(constrained, el) || !aligned(prior, 4) || !aligned(c.bias, 4) ||
         !aligned(c.allow, 4) || !aligned(c.history, 4) || !aligned(c.history_len, 4) || !aligned(c.repetition, 4) ||
         !aligned(c.presence, 4) || !aligned(c.frequency, 4) || !aligned(argmax, 4) || !aligned(best, 4))
@@ -749,6 +756,8 @@ extern "C" tag_status tag_balance(int32_t n_query, int32_t n_slices, int32_t dty
         TAG_FAIL(TAG_EINVAL, "scores, mask, grad, loss, count, load and workspace must be non-NULL");
     if (score_stride < n_slices || grad_stride < n_slices)
         TAG_FAIL(TAG_EINVAL, "a row stride is below the number of slices");
+    if (far_apart(n_query, score_stride) || far_apart(n_query, grad_stride))
+        TAG_FAIL(TAG_ESHAPE, "rows span at most 2^58 elements");
     if (accumulate && dtype != TAG_F32) TAG_FAIL(TAG_EINVAL, "accumulate needs TAG_F32");
     const size_t el = dtype == TAG_BF16 ? 2 : 4;
     if (!aligned(scores, el) || !aligned(grad, el) || !aligned(mask, 8) || !aligned(loss, 4) || !aligned(count, 4) ||
