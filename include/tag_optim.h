@@ -39,7 +39,8 @@ typedef struct tag_newton_schulz {
 } tag_newton_schulz;
 
 /* `count` matrices of one shape: matrix i, row r, column c of an array at
- * base[i matrix_stride + r row_stride + c] (strides in elements). */
+ * base[i matrix_stride + r row_stride + c] (strides in elements; count times
+ * matrix_stride and rows times row_stride at most 2^58, TAG_ESHAPE). */
 typedef struct tag_matrices {
     void *base;
     int64_t row_stride, matrix_stride;

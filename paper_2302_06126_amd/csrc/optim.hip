@@ -933,6 +933,9 @@ tag_status check_array(const tag_matrices &a, int32_t count, int32_t rows, int32
     if ((uintptr_t)a.base % el) TAG_FAIL(TAG_EINVAL, std::string(what) + " must be aligned to its elements");
     if ((rows > 1 && a.row_stride < cols) || (count > 1 && a.matrix_stride < 0))
         TAG_FAIL(TAG_EINVAL, std::string(what) + ": a row stride is below the number of columns, or a stride negative");
+    // (products of these, here, in overlap and in the kernels, stay in 64 bits)
+    if ((rows > 1 && a.row_stride > ((int64_t)1 << 58) / rows) || (count > 1 && a.matrix_stride > ((int64_t)1 << 58) / count))
+        TAG_FAIL(TAG_ESHAPE, std::string(what) + ": rows and matrices span at most 2^58 elements");
     if (!written || count == 1) return TAG_OK;
     const int64_t span = (rows - 1) * (rows > 1 ? a.row_stride : 0) + cols;
     const bool apart = a.matrix_stride >= span;
