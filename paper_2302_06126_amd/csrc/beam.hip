@@ -4,9 +4,10 @@
 // Selection.  Continuations of one beam are ordered by their scores alone; those of
 // two beams by the sums c = x + (total - log sum exp x), so that is what has to be
 // exact: rows are summed in 64 bits, which the vector unit does at the rate of
-// single fp32 operations, with exponentials of 18 instructions each.  They are half
-// of all instructions, and bound the large calls rather than memory (44 MB of fp32
-// scores would take 9 us, their exponentials 6 on all SIMDs).  Scores are read once.
+// single fp32 operations, with exponentials of 18 instructions each: 288 to a
+// wavefront's 1,024 scores, of 887 vector instructions (2,656 searches of 16 x 256) where
+// a search fits a block, of 446 (64 rows of 262,140) where rows go in parts.  Vector
+// issue and waits bound the large calls rather than memory.  Scores are read once.
 //
 // What is best is found without sorting.  Every thread (or group of columns) has a
 // best candidate of its own; W of these at least reach the bar that bisection finds
@@ -480,11 +481,15 @@ struct RowSum {
     float max[NT / 64];
     double sum[NT / 64];
 };
-// e^x for x <= 0, within a few roundings of 64 bits; below -700 that of -700 (a
-// sum with a term of 1 in it does not see either).  2^(n + f) with |f| <= 1/2: n by
-// adding 1.5 2^52, whose last bits it then is, 2^f = 1 + f q(f) by interpolation of q
-// at eleven Chebyshev points (2e-17 off).  18 instructions, of the fp32 rate: 42,496 x
-// 256 scores 31 -> 26 us against the library's exp.
+// e^x for x <= 0; below -700 that of -700 (a sum with a term of 1 in it does not see
+// either).  2^(n + f) with |f| <= 1/2: n by adding 1.5 2^52, whose last bits it then is,
+// 2^f = 1 + f q(f) by interpolation of q at eleven Chebyshev points (2e-17 off).  18
+// instructions, of the fp32 rate: 42,496 x 256 scores 31 -> 26 us against the
+// library's exp.  It is off by (1.4 + |x| / 7.8) 2^-53 of itself (3.2 million values
+// against 128 bits: 3.7 at 20, 89 at 690), since log2 e is one number and its own
+// rounding counts x times.  In a sum of S terms, the largest 1, that is ln S / 7.8
+// roundings at most: with p = e^x / sum e^x, sum p |x| is the entropy of p less log
+// sum e^x, and so at most ln S.
 __device__ __forceinline__ double exp_below(double x) {
     constexpr double q[11] = {0.6931471805599453,    0.24022650695910097,   0.0555041086648216,    0.009618129107606888,
                               0.0013333558146416936, 0.0001540353044173605, 1.525273382983612e-05, 1.321544258792169e-06,
@@ -561,12 +566,12 @@ __device__ __forceinline__ double row_sum(const float (&x)[16], float &m, const 
 }
 
 // Searches whose scores fit one block's registers; those of one wavefront, four to a
-// block.  One search of 64 x 256 9.0 us on its one CU: a chain of load 0.6, sums 3.3, bar
-// 1.6, list 1.4, ranks 1.2.  2,656 of 16 x 256 bf16 22.5 us: 6 us a thousand beyond the
-// first 5, vector issue and waits (9.8 million instructions of wavefronts, 3.1 of them
-// exponentials).  Measured and not kept there: 64 scores to a thread (6.3 million
-// instructions, but three wavefronts to a SIMD do not hide one another's waits: 24
-// us), 32 to a thread (21.6).
+// block.  One search of 64 x 256 9.1 us on its one CU: a chain of loads, sums, bar, list
+// and ranks.  2,656 of 16 x 256 bf16 22.5 us: vector issue (9.4 million instructions of
+// wavefronts, 3.1 of them exponentials, 17.5 us at four cycles and 2.1 GHz on all
+// SIMDs) and waits.  Measured and not kept there: 64 scores to a thread (24 us), 32
+// (21.6).  Searches of one row and one beam go the same way: 40,000 of 1 x 256 48 us,
+// where memory would take 8.
 constexpr int whole_block(int NT) { return NT > 64 ? NT : 256; }
 template <typename T, int NT, int CAP>
 __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_t n) {
@@ -634,8 +639,8 @@ __global__ void __launch_bounds__(whole_block(NT)) beam_whole(BeamArgs A, int32_
 // Rows in parts: a part's maximum and sum, and the maximum of every group of its
 // columns, from one reading of the scores.  GROUP: 0, or that of rows of a block each
 // (2^8 threads), whose reductions then are of fixed sizes (64 x 262,140 fp32 22.9 -> 21.1
-// us).  67 MB in 18 us, 3.7 TB/s: vector issue, some 470 instructions to a wavefront's
-// 1,024 scores, 290 of them exponentials.
+// us).  67 MB in 17.9 us, 3.7 TB/s: vector issue, 446 instructions to a wavefront's 1,024
+// scores, 288 of them exponentials (13.6 us at four cycles and 2.1 GHz on all SIMDs).
 template <typename T, int GROUP>
 __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
     __shared__ RowSum<256> part;
@@ -686,8 +691,15 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
 
 // One block per search: what each beam adds to its scores, from its parts; the bar
 // from the groups' maxima; then the candidates of the groups that reach it.  A chain
-// of waits on one CU: 8 searches of 8 x 262,140 13.7 us (offsets 3.2, groups 1.8, bar
-// 1.3, scores of about 11 groups 5, ranks 1), 5 of 200 x 4,099 26.5 (some 270 groups).
+// of waits on one CU: 8 searches of 8 x 262,140 12.8 us, 5 of 200 x 4,099 26.4, 2 of 256
+// x 31,000 63.  127 VGPRs (1,024 threads leave 128), 4 VGPRs and 41 SGPRs spilled (20
+// bytes of scratch a lane).
+// The bar is set from one candidate of each thread; where fewer than W threads have
+// one, rows go one after the other instead.  A finished beam's stands in its first group
+// of columns, and group i is thread i mod 1,024's, so where a row has a multiple of 64
+// groups (4,096 slices in groups of 64) all finished beams belong to 16 threads or
+// fewer: 256 beams of 4,096 slices, 254 of them finished, take 536 us that way, those of
+// 4,099 slices (65 groups) 35.
 constexpr int kListed = 2048;   // groups
 template <typename T>
 __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {

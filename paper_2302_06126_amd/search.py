@@ -321,7 +321,8 @@ class SearchService:
     def beam(self, depth: Optional[int] = None, stream=None):
         """Beam search with the service's B leaves (at most 256) as its beams: group by
         group in the search order, the B most probable partial strategies under the
-        network's priors (each level's features come from the strategies so far).
+        network's priors (each level's features come from the strategies so far; every
+        level evaluates B leaves, also where there are fewer strategies).
 
         Returns (paths [n, depth] int32, log_prior [n], rewards [n]), the most
         probable first; fewer than B where there are no more strategies.  `depth`
