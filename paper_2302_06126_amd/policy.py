@@ -277,6 +277,8 @@ class Reorder:
         else:
             raise ValueError(f"states must have the shape [{self.n * width}, ...] or [{self.n}, {width}, ...], not "
                              f"{list(shape)}")
+        if t.numel() == 0:
+            return 0, 0, 0
         row = 1
         for size, step in zip(shape[:lead - 1:-1], stride[:lead - 1:-1]):
             if size != 1 and step != row:
