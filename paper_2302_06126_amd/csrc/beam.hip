@@ -696,10 +696,10 @@ __global__ void __launch_bounds__(256) beam_parts(BeamArgs A, int64_t rows) {
 // bytes of scratch a lane).
 // The bar is set from one candidate of each thread; where fewer than W threads have
 // one, rows go one after the other instead.  A finished beam's stands in its first group
-// of columns, and group i is thread i mod 1,024's, so where a row has a multiple of 64
-// groups (4,096 slices in groups of 64) all finished beams belong to 16 threads or
-// fewer: 256 beams of 4,096 slices, 254 of them finished, take 536 us that way, those of
-// 4,099 slices (65 groups) 35.
+// of columns, and group i is thread i mod 1,024's, so where a row's groups are a
+// multiple of 2^k all finished beams belong to 2^(10 - k) threads: 256 beams of 4,096
+// slices (64 groups), 254 of them finished, take 536 us that way, of 8,192 (32 groups)
+// 548, while those of 4,099 (65 groups) take 35.
 constexpr int kListed = 2048;   // groups
 template <typename T>
 __global__ void __launch_bounds__(1024) beam_join(BeamArgs A) {
